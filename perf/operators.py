@@ -2,15 +2,16 @@
 8-bit activation checkpoint and the weight gradient that reads it.
 
 An MX tensor is a matrix of `lines` x `length` elements whose lines are cut into blocks of 32.  A block has one scale, a power of
-two held as a byte (exponent + 127), and 32 codes: E2M1 (two to a byte, the earlier in the low half) or E4M3 (one to a byte).  A line
-takes pitch(length) = length rounded up to 512 elements; what lies behind its end is zero.  E2M1's exponent is floor(log2(max)) - 2,
-larger magnitudes saturate at 6; E4M3's is the smallest one with max <= 448 * 2^exponent.  Codes are the nearest ones, ties to the even code.
+two held as a byte (exponent + 127): the smallest s with max <= 7 s.  In 4 bits an element is one E2M1 code h, the nearest to x / s; in
+8 bits it is two, h and the nearest to what is left at an eighth of the scale: x ~ s (h + l / 8).  Ties go to the even code, magnitudes
+above 6 saturate.  Codes lie two to a byte, the earlier element in the low half, the second codes of 8 bits in a plane of their own
+behind the first; a line takes pitch(length) = length rounded up to 512 elements, and what lies behind its end is zero.
 
 A case says by "op" what runs:
   quantize    x [M x K] -> its values as an MX tensor along rows and as one along columns, from one read
-  checkpoint  x [M x K] -> saved as E4M3 along columns (a block is 32 tokens of one channel), and restored
+  checkpoint  x [M x K] -> saved in 8 bits along columns (a block is 32 tokens of one channel), and restored
   gemm        two MX operands at hand -> their product [M x N] over K
-  linear      tokens [M x K] through a layer whose weights are at hand in MXFP4 -> [M x N]
+  linear      tokens [M x K] through a layer whose weights are at hand in 4 bits -> [M x N]
   wgrad       output gradient [M x N] and a checkpoint of the activations at hand -> dW [K x N] in fp32
   step        activations, master weights and output gradient -> Y, dA and dW: weights quantized along both axes, forward pass with
               its checkpoint, backward pass
@@ -28,9 +29,9 @@ own = False
 BLOCK, PITCH = 32, 512
 
 
-def _case(name, op, M, K, N=0, dtype="bf16", fmt="e2m1", grad="e2m1", act="channels"):
-    """fmt: the activations' format (gemm: the left operand's); grad: the output gradient's format along tokens (gemm: the right operand's)."""
-    return {"name": name, "op": op, "M": M, "K": K, "N": N, "dtype": dtype, "fmt": fmt, "grad": grad, "act": act}
+def _case(name, op, M, K, N=0, dtype="bf16", bits=4, grad=4, act="channels"):
+    """bits: of the activations (gemm: of the left operand, quantize: along rows); grad: of the output gradient along tokens (gemm: of the right operand)."""
+    return {"name": name, "op": op, "M": M, "K": K, "N": N, "dtype": dtype, "bits": bits, "grad": grad, "act": act}
 
 
 def listed():
@@ -38,7 +39,7 @@ def listed():
         # one token through a square 7B projection whose weights are quantized already: decoding, where latency counts
         _case("serve-1x4096x4096", "linear", 1, 4096, 4096),
         # a batch of decoding sequences through the 7B gate projection, activations kept in 8 bits
-        _case("serve-24x4096x11008-a8", "linear", 24, 4096, 11008, fmt="e4m3"),
+        _case("serve-24x4096x11008-a8", "linear", 24, 4096, 11008, bits=8),
         # a 1.3B feed-forward product between operands that are at hand, output width no multiple of a tile
         _case("gemm-8192x2048x5504", "gemm", 8192, 2048, 5504),
         # the largest product: the 7B attention input projection over a training batch
@@ -54,7 +55,7 @@ def listed():
         # the 7B output projection's weight gradient
         _case("wgrad-8192x4096x4096", "wgrad", 8192, 4096, 4096),
         # odd everything, output gradient in 8 bits as well
-        _case("wgrad-1055x1376x2080-g8", "wgrad", 1055, 1376, 2080, grad="e4m3"),
+        _case("wgrad-1055x1376x2080-g8", "wgrad", 1055, 1376, 2080, grad=8),
         # a 1.3B feed-forward layer's whole training step
         _case("step-8192x2048x5504", "step", 8192, 2048, 5504),
         # the smallest configuration's step, fp32 masters
@@ -84,8 +85,8 @@ def draw(rng):
             "K": size(256, 13824, 8),
             "N": 0 if op in ("quantize", "checkpoint") else size(256, 15360, 8),
             "dtype": "f32" if f32 else "bf16",
-            "fmt": "e4m3" if op in ("linear", "gemm", "step", "quantize") and rng.random() < 0.3 else "e2m1",
-            "grad": "e4m3" if op in ("wgrad", "step", "gemm") and rng.random() < 0.3 else "e2m1",
+            "bits": 8 if op in ("linear", "gemm", "step", "quantize") and rng.random() < 0.3 else 4,
+            "grad": 8 if op in ("wgrad", "step", "gemm") and rng.random() < 0.3 else 4,
             "act": "student-t" if rng.random() < 0.3 else "channels",
         }
         if _cost(c) <= most:
@@ -98,62 +99,56 @@ def _pitch(n):
     return (n + PITCH - 1) // PITCH * PITCH
 
 
-def _scaled(x, fmt):
-    """fp32 x [lines x length] -> grid values (what the codes stand for before scaling) and exponents of its blocks, both padded to the pitch."""
+def _nearest(v):
+    """v rounded to E2M1's values, ties to the even code, saturating."""
+    step = torch.ldexp(torch.ones_like(v), (torch.frexp(v)[1] - 1).clamp(min=0) - 1)
+    return (torch.round(v / step) * step).clamp(-6.0, 6.0)
+
+
+def _scaled(x, bits):
+    """fp32 x [lines x length] -> what the codes of each plane stand for before scaling and the blocks' exponents, padded to the pitch."""
     lines, length = x.shape
     p = _pitch(length)
     if p != length:
         x = torch.nn.functional.pad(x, (0, p - length))
     x = x.reshape(lines, p // BLOCK, BLOCK)
-    amax = x.abs().amax(dim=2, keepdim=True)
-    m, e = torch.frexp(amax)                                   # amax = m * 2^e, m in [0.5, 1)
-    if fmt == "e2m1":
-        e, low, mant, top = e - 3, 0, 1, 6.0
-    else:
-        e, low, mant, top = e - 9 + (m > 0.875).to(e.dtype), -6, 3, 448.0
-    e = torch.where(amax > 0, e.clamp(-126, 127), torch.full_like(e, -126))
+    m, e = torch.frexp(x.abs().amax(dim=2, keepdim=True))      # the largest magnitude is m * 2^e, m in [0.5, 1)
+    e = e - 3 + (m > 0.875).to(e.dtype)                        # 7 = 0.875 * 2^3
+    least = -126 if bits == 4 else -123
+    e = torch.where(m > 0, e.clamp(least, 127), torch.full_like(e, least))
     v = torch.ldexp(x, -e)
-    step = torch.ldexp(torch.ones_like(v), (torch.frexp(v)[1] - 1).clamp(min=low) - mant)
-    v = (torch.round(v / step) * step).clamp(-top, top)
-    return v.reshape(lines, p), e.reshape(lines, p // BLOCK)
+    high = _nearest(v)
+    planes = [high] if bits == 4 else [high, _nearest((v - high) * 8.0)]
+    return [t.reshape(lines, p) for t in planes], e.reshape(lines, p // BLOCK)
 
 
-def _values(x, fmt):
-    """x as its MX codes along the last axis hold it, fp32, length of x."""
-    lines, length = x.shape
-    v, e = _scaled(x.float(), fmt)
+def _joined(planes, e, length):
+    v = planes[0] if len(planes) == 1 else planes[0] + planes[1] / 8.0
+    lines = v.shape[0]
     return torch.ldexp(v.reshape(lines, -1, BLOCK), e.unsqueeze(2)).reshape(lines, -1)[:, :length]
 
 
-_GRID = {"e2m1": [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0],
-         "e4m3": [m * 2.0 ** -9 for m in range(8)] + [(8 + m) * 2.0 ** (e - 10) for e in range(1, 16) for m in range(8)][:-1]}
+def _values(x, bits):
+    """x as its MX codes along the last axis hold it, fp32."""
+    return _joined(*_scaled(x.float(), bits), x.shape[1])
 
 
-def _encode(x, fmt):
+_E2M1 = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+
+
+def _encode(x, bits):
     """(codes, scales) of x along its last axis: bytes, as the framework lays them out."""
-    v, e = _scaled(x.float(), fmt)
-    grid = torch.tensor(_GRID[fmt], device=x.device)
-    code = torch.bucketize(v.abs(), grid).to(torch.uint8)
-    sign = (v < 0).to(torch.uint8)
-    if fmt == "e2m1":
-        code = code | (sign << 3)
-        code = code[:, 0::2] | (code[:, 1::2] << 4)
-    else:
-        code = code | (sign << 7)
-    return code.contiguous(), (e + 127).to(torch.uint8)
+    planes, e = _scaled(x.float(), bits)
+    v = torch.stack(planes) if bits == 8 else planes[0]
+    code = torch.bucketize(v.abs(), torch.tensor(_E2M1, device=x.device)).to(torch.uint8) | ((v < 0).to(torch.uint8) << 3)
+    return code[..., 0::2] | (code[..., 1::2] << 4), (e + 127).to(torch.uint8)
 
 
-def _decode(codes, scales, fmt, length):
+def _decode(codes, scales, bits, length):
     """fp32 values of an MX tensor."""
-    if fmt == "e2m1":
-        c = torch.stack([codes & 15, codes >> 4], dim=2).reshape(codes.shape[0], -1).to(torch.int32)
-        mag, neg = c & 7, c >> 3
-    else:
-        c = codes.to(torch.int32)
-        mag, neg = c & 127, c >> 7
-    v = torch.tensor(_GRID[fmt], device=codes.device)[mag] * (1 - 2 * neg)
-    e = scales.to(torch.int32) - 127
-    return torch.ldexp(v.reshape(codes.shape[0], -1, BLOCK), e.unsqueeze(2)).reshape(codes.shape[0], -1)[:, :length]
+    c = torch.stack([codes & 15, codes >> 4], dim=-1).flatten(-2).to(torch.int32)
+    v = torch.tensor(_E2M1, device=codes.device)[c & 7] * (1 - 2 * (c >> 3))
+    return _joined([v] if bits == 4 else list(v), scales.to(torch.int32) - 127, length)
 
 
 def _dtype(case):
@@ -183,14 +178,14 @@ def prepare(case, seed):
     if op in ("quantize", "checkpoint", "linear", "step"):
         s["x"] = x
     if op == "gemm":
-        s["l"] = _encode(x, case["fmt"])
+        s["l"] = _encode(x, case["bits"])
         s["r"] = _encode((normal(N, K) * 0.02).to(dt), case["grad"])
         s["Y"] = torch.empty(M, N, device="cuda", dtype=dt)
     if op == "linear":
-        s["r"] = _encode((normal(N, K) * 0.02).to(dt), "e2m1")
+        s["r"] = _encode((normal(N, K) * 0.02).to(dt), 4)
         s["Y"] = torch.empty(M, N, device="cuda", dtype=dt)
     if op == "wgrad":
-        s["saved"] = _encode(x.t(), "e4m3")
+        s["saved"] = _encode(x.t(), 8)
     if op in ("wgrad", "step"):
         s["dY"] = (normal(M, N) * 0.01).to(dt)
         s["dW"] = torch.empty(K, N, device="cuda", dtype=torch.float32)
@@ -205,19 +200,19 @@ def _run_plain(s):
     case = s["case"]
     op, M, K, N, dt = case["op"], case["M"], case["K"], case["N"], _dtype(case)
     if op == "quantize":
-        return {"rows": _values(s["x"], case["fmt"]).to(torch.bfloat16), "cols": _values(s["x"].t(), "e2m1").t().to(torch.bfloat16).contiguous()}
+        return {"rows": _values(s["x"], case["bits"]).to(torch.bfloat16), "cols": _values(s["x"].t(), 4).t().to(torch.bfloat16).contiguous()}
     if op == "checkpoint":
-        return {"x": _values(s["x"].t(), "e4m3").t().to(dt).contiguous()}
+        return {"x": _values(s["x"].t(), 8).t().to(dt).contiguous()}
     if op == "gemm":
-        return {"Y": (_decode(*s["l"], case["fmt"], K) @ _decode(*s["r"], case["grad"], K).t()).to(dt)}
+        return {"Y": (_decode(*s["l"], case["bits"], K) @ _decode(*s["r"], case["grad"], K).t()).to(dt)}
     if op == "linear":
-        return {"Y": (_values(s["x"], case["fmt"]) @ _decode(*s["r"], "e2m1", K).t()).to(dt)}
+        return {"Y": (_values(s["x"], case["bits"]) @ _decode(*s["r"], 4, K).t()).to(dt)}
     if op == "wgrad":
-        return {"dW": _decode(*s["saved"], "e4m3", M) @ _values(s["dY"].t(), case["grad"]).t()}
+        return {"dW": _decode(*s["saved"], 8, M) @ _values(s["dY"].t(), case["grad"]).t()}
     x, W, dY = s["x"], s["W"], s["dY"]
-    return {"Y": (_values(x, case["fmt"]) @ _values(W.t(), "e2m1").t()).to(dt),
-            "dA": (_values(dY, "e2m1") @ _values(W, "e2m1").t()).to(dt),
-            "dW": _values(x.t(), "e4m3") @ _values(dY.t(), case["grad"]).t()}
+    return {"Y": (_values(x, case["bits"]) @ _values(W.t(), 4).t()).to(dt),
+            "dA": (_values(dY, 4) @ _values(W, 4).t()).to(dt),
+            "dW": _values(x.t(), 8) @ _values(dY.t(), case["grad"]).t()}
 
 
 def _run_own(s):
@@ -225,25 +220,24 @@ def _run_own(s):
 
     case = s["case"]
     op, M, K, N, dt = case["op"], case["M"], case["K"], case["N"], _dtype(case)
-    fmt = {"e2m1": b.FP4_FMT_E2M1, "e4m3": b.FP4_FMT_E4M3}
     if op == "quantize":
-        rows, cols = b.mx_quantize_both(s["x"], fmt[case["fmt"]], b.FP4_FMT_E2M1)
+        rows, cols = b.mx_quantize_both(s["x"], case["bits"], 4)
         return {"rows": b.mx_dequantize(rows, torch.bfloat16), "cols": b.mx_dequantize(cols, torch.bfloat16)}
     if op == "checkpoint":
         return {"x": b.mx_dequantize(b.mx_checkpoint_save(s["x"]), dt)}
     if op == "gemm":
-        b.mx_gemm(b.MxTensor(*s["l"], fmt[case["fmt"]], K), b.MxTensor(*s["r"], fmt[case["grad"]], K), out=s["Y"])
+        b.mx_gemm(b.MxTensor(*s["l"], K), b.MxTensor(*s["r"], K), out=s["Y"])
         return {"Y": s["Y"]}
     if op == "linear":
-        b.mx_linear_fwd(s["x"], b.MxTensor(*s["r"], b.FP4_FMT_E2M1, K), act_fmt=fmt[case["fmt"]], Y=s["Y"])
+        b.mx_linear_fwd(s["x"], b.MxTensor(*s["r"], K), act_bits=case["bits"], Y=s["Y"])
         return {"Y": s["Y"]}
     if op == "wgrad":
-        b.mx_linear_bwd_wgrad(s["dY"], b.MxTensor(*s["saved"], b.FP4_FMT_E4M3, M, transposed=True), grad_fmt=fmt[case["grad"]], dW=s["dW"])
+        b.mx_linear_bwd_wgrad(s["dY"], b.MxTensor(*s["saved"], M, transposed=True), grad_bits=case["grad"], dW=s["dW"])
         return {"dW": s["dW"]}
     wq = b.mx_prepare_weights(s["W"])
     saved = b.mx_checkpoint(M, K)
-    b.mx_linear_fwd(s["x"], wq.fwd, act_fmt=fmt[case["fmt"]], saved=saved, Y=s["Y"])
-    b.mx_linear_bwd(s["dY"], saved, wq.bwd, grad_fmt=fmt[case["grad"]], dA=s["dA"], dW=s["dW"])
+    b.mx_linear_fwd(s["x"], wq.fwd, act_bits=case["bits"], saved=saved, Y=s["Y"])
+    b.mx_linear_bwd(s["dY"], saved, wq.bwd, grad_bits=case["grad"], dA=s["dA"], dW=s["dW"])
     return {"Y": s["Y"], "dA": s["dA"], "dW": s["dW"]}
 
 
@@ -255,72 +249,70 @@ def work(case):
     """Inputs once, outputs once; codes that one call leaves for the next are written once and read once."""
     op, M, K, N = case["op"], float(case["M"]), float(case["K"]), float(case["N"])
     e = 2.0 if case["dtype"] == "bf16" else 4.0
-    width = {"e2m1": 0.5 + 1 / 32, "e4m3": 1.0 + 1 / 32}        # bytes of an element with its share of the scale
-    left, right = width[case["fmt"]], width[case["grad"]]
+    width = {4: 0.5 + 1 / 32, 8: 1.0 + 1 / 32}                  # bytes of an element with its share of the scale
+    left, right = width[case["bits"]], width[case["grad"]]
     if op == "quantize":
-        return {"bytes": M * K * (e + 2 * (left + width["e2m1"]) + 4.0), "flops": 4.0 * M * K}
+        return {"bytes": M * K * (e + 2 * (left + width[4]) + 4.0), "flops": 4.0 * M * K}
     if op == "checkpoint":
-        return {"bytes": M * K * (2 * e + 2 * width["e4m3"]), "flops": 2.0 * M * K}
+        return {"bytes": M * K * (2 * e + 2 * width[8]), "flops": 2.0 * M * K}
     if op == "gemm":
         return {"bytes": M * K * left + K * N * right + M * N * e, "flops": 2.0 * M * K * N}
     if op == "linear":
-        return {"bytes": M * K * e + K * N * width["e2m1"] + M * N * e, "flops": 2.0 * M * K * N}
+        return {"bytes": M * K * e + K * N * width[4] + M * N * e, "flops": 2.0 * M * K * N}
     if op == "wgrad":
-        return {"bytes": M * K * width["e4m3"] + M * N * e + 4.0 * K * N, "flops": 2.0 * M * K * N}
-    return {"bytes": e * (2 * M * K + K * N + 2 * M * N) + 4.0 * K * N + 2 * M * K * width["e4m3"] + 4 * K * N * width["e2m1"], "flops": 6.0 * M * K * N}
+        return {"bytes": M * K * width[8] + M * N * e + 4.0 * K * N, "flops": 2.0 * M * K * N}
+    return {"bytes": e * (2 * M * K + K * N + 2 * M * N) + 4.0 * K * N + 2 * M * K * width[8] + 4 * K * N * width[4], "flops": 6.0 * M * K * N}
 
 
 # ---- once more from the definition, in 64 bits, by tables ----------------------------------------------------------------------
 
-def _by_table(x, fmt):
-    """fp64 values of x [lines x length] under a scale for every 32 elements of a line, found among the format's magnitudes."""
+def _by_table(x, bits):
+    """fp64 values of x [lines x length] under a scale for every 32 elements of a line, codes found among E2M1's magnitudes."""
     lines, length = x.shape
     whole = -(-length // BLOCK) * BLOCK
     b = torch.zeros(lines, whole, dtype=torch.float64, device=x.device)
     b[:, :length] = x.double()
     b = b.reshape(-1, BLOCK)
-    top = b.abs().max(dim=1).values
-    if fmt == "e2m1":                 # the exponent field of a double is its floor(log2)
-        e = ((top.view(torch.int64) >> 52) - 1023) - 2
-        pos = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
-    else:                             # the smallest power of two not below top / 448
-        r = (top / 448.0).view(torch.int64)
-        e = (r >> 52) - 1023 + ((r & ((1 << 52) - 1)) != 0).to(torch.int64)
-        pos = [(c & 7) * 2.0 ** -9 if c < 8 else (1 + (c & 7) / 8) * 2.0 ** ((c >> 3) - 7) for c in range(127)]
-    e = e.clamp(-126, 127)
-    scale = ((e + 1023) << 52).view(torch.float64).unsqueeze(1)
-    grid = torch.tensor(pos, dtype=torch.float64, device=x.device)
+    r = (b.abs().max(dim=1).values / 7.0).view(torch.int64)       # the smallest power of two not below max / 7, by the bits of a double
+    e = (r >> 52) - 1023 + ((r & ((1 << 52) - 1)) != 0).to(torch.int64)
+    scale = ((e.clamp(-126 if bits == 4 else -123, 127) + 1023) << 52).view(torch.float64).unsqueeze(1)
+    grid = torch.tensor(_E2M1, dtype=torch.float64, device=x.device)
     mid = (grid[1:] + grid[:-1]) / 2
-    a = b.abs() / scale
-    down, up = torch.bucketize(a, mid), torch.bucketize(a, mid, right=True)      # they differ on a midpoint: the even one of the two
-    code = torch.where(down % 2 == 0, down, up)
-    return (torch.copysign(grid[code], b) * scale).reshape(lines, whole)[:, :length]
+
+    def code_values(v):
+        down, up = torch.bucketize(v.abs(), mid), torch.bucketize(v.abs(), mid, right=True)   # they differ on a midpoint: the even one of the two
+        return torch.copysign(grid[torch.where(down % 2 == 0, down, up)], v)
+
+    v = code_values(b / scale) * scale
+    if bits == 8:
+        v = v + code_values((b - v) / (scale / 8.0)) * (scale / 8.0)
+    return v.reshape(lines, whole)[:, :length]
 
 
-def _table_decode(codes, scales, fmt, length):
-    if fmt == "e2m1":
-        half = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, 0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0], dtype=torch.float64, device=codes.device)
-        v = torch.empty(codes.shape[0], 2 * codes.shape[1], dtype=torch.float64, device=codes.device)
-        v[:, 0::2], v[:, 1::2] = half[(codes & 15).long()], half[(codes >> 4).long()]
-    else:
-        v = codes.view(torch.float8_e4m3fn).to(torch.float64)
-    scale = (scales.long() - 127 + 1023 << 52).view(torch.float64)
-    return (v * scale.repeat_interleave(BLOCK, dim=1))[:, :length]
+def _table_decode(codes, scales, bits, length):
+    both = torch.tensor(_E2M1 + [-m for m in _E2M1], dtype=torch.float64, device=codes.device)
+    scale = (scales.long() - 127 + 1023 << 52).view(torch.float64).repeat_interleave(BLOCK, dim=1)
+    total = 0.0
+    for plane, part in ((codes, 1.0),) if bits == 4 else ((codes[0], 1.0), (codes[1], 0.125)):
+        v = torch.empty(plane.shape[0], 2 * plane.shape[1], dtype=torch.float64, device=codes.device)
+        v[:, 0::2], v[:, 1::2] = both[(plane & 15).long()], both[(plane >> 4).long()]
+        total = total + part * v * scale
+    return total[:, :length]
 
 
 def exact(case, seed):
     s = prepare(case, seed)
     op, M, K, N = case["op"], case["M"], case["K"], case["N"]
     if op == "quantize":
-        return {"rows": _by_table(s["x"], case["fmt"]), "cols": _by_table(s["x"].t(), "e2m1").t()}
+        return {"rows": _by_table(s["x"], case["bits"]), "cols": _by_table(s["x"].t(), 4).t()}
     if op == "checkpoint":
-        return {"x": _by_table(s["x"].t(), "e4m3").t()}
+        return {"x": _by_table(s["x"].t(), 8).t()}
     if op == "gemm":
-        return {"Y": _table_decode(*s["l"], case["fmt"], K) @ _table_decode(*s["r"], case["grad"], K).t().contiguous()}
+        return {"Y": _table_decode(*s["l"], case["bits"], K) @ _table_decode(*s["r"], case["grad"], K).t().contiguous()}
     if op == "linear":
-        return {"Y": _by_table(s["x"], case["fmt"]) @ _table_decode(*s["r"], "e2m1", K).t().contiguous()}
+        return {"Y": _by_table(s["x"], case["bits"]) @ _table_decode(*s["r"], 4, K).t().contiguous()}
     if op == "wgrad":
-        return {"dW": _table_decode(*s["saved"], "e4m3", M) @ _by_table(s["dY"].t(), case["grad"]).t().contiguous()}
-    return {"Y": _by_table(s["x"], case["fmt"]) @ _by_table(s["W"].t(), "e2m1").t().contiguous(),
-            "dA": _by_table(s["dY"], "e2m1") @ _by_table(s["W"], "e2m1").t().contiguous(),
-            "dW": _by_table(s["x"].t(), "e4m3") @ _by_table(s["dY"].t(), case["grad"]).t().contiguous()}
+        return {"dW": _table_decode(*s["saved"], 8, M) @ _by_table(s["dY"].t(), case["grad"]).t().contiguous()}
+    return {"Y": _by_table(s["x"], case["bits"]) @ _by_table(s["W"].t(), 4).t().contiguous(),
+            "dA": _by_table(s["dY"], 4) @ _by_table(s["W"], 4).t().contiguous(),
+            "dW": _by_table(s["x"].t(), 8) @ _by_table(s["dY"].t(), case["grad"]).t().contiguous()}
