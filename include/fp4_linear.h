@@ -97,7 +97,11 @@ typedef enum {
   FP4_OP_SPMM = 5,     /* (M=P rows of S, K=Q, N)                                        */
   FP4_OP_PREPARE = 6,  /* fp4_prepare_weights (M ignored)                                 */
   FP4_OP_FWD_MIXED = 7,/* fp4_linear_fwd_mixed                                            */
-  FP4_OP_BWD = 8       /* fp4_linear_bwd                                                  */
+  FP4_OP_BWD = 8,      /* fp4_linear_bwd                                                  */
+  FP4_OP_MX_FWD = 9,   /* mx_linear_fwd                                                   */
+  FP4_OP_MX_DGRAD = 10,/* mx_linear_bwd_dgrad                                             */
+  FP4_OP_MX_WGRAD = 11,/* mx_linear_bwd_wgrad                                             */
+  FP4_OP_MX_BWD = 12   /* mx_linear_bwd                                                   */
 } fp4_op;
 
 /* What the forward pass leaves for the weight-gradient pass (Sec. 3.1 needs the
@@ -287,6 +291,72 @@ int fp4_linear_fwd_mixed(const void* A, const void* W, fp4_dtype dt, int64_t M, 
 int fp4_linear_fwd_granularity(const void* A, const void* W, fp4_dtype dt, int64_t M, int64_t K, int64_t N,
                                int act_tensorwise, int wgt_tensorwise, double alpha, void* Y,
                                const fp4_fwd_ctx* saved, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- microscaled (MX) operands: one power-of-two scale for every 32 elements along the contraction ----
+ * The block-scaled form of the layer.  An outlier costs its own block its precision and nothing else, so there is no clamp and no
+ * residual product; the matrix cores take the scales themselves; and the activations are kept for the weight gradient in 8 bits, as
+ * the very operand that product reads.
+ *
+ * fp4_mx: a matrix of `lines` x `length` elements along the contraction, an element in 4 bits (one E2M1 code h) or in 8 (two, h and l).
+ *   codes   [bits / 4 planes][lines x mx_pitch(length)] E2M1 codes, two to a byte, the earlier element in bits 3:0; the second plane
+ *           holds l
+ *   scales  [lines x mx_pitch(length) / 32] bytes: exponent + 127 of the block's scale s; 255 makes the whole block NaN
+ *   value   s h, or s (h + l / 8)
+ *   Elements behind `length` hold the code 0 under a finite scale, and the scales of 8 bits are at least 4 (mx_quantize leaves them so;
+ *   a tensor from elsewhere has to hold them so too).  Buffers are 16-byte aligned.
+ * mx_pitch: length rounded up to a multiple of 512 (-1 for a negative length).
+ * Scale of a block with largest magnitude m: the smallest power of two with m <= 7 s, its exponent held in [-126, 127] (8 bits:
+ * [-123, 127]).  h is the nearest code to x / s, l the nearest to 8 (x / s - h); ties to the even code, magnitudes above 6 saturate, the
+ * sign stays on zero.  Unlike elsewhere in this library inputs need not be finite: an infinity or a NaN makes its block NaN, and with it
+ * whatever is computed from the block.
+ * Any number of rows and columns will do (0 does nothing); leading dimensions are multiples of 8 and base pointers 16-byte aligned as
+ * everywhere.  Dimensions above 2^21 are refused with FP4_ERR_LIMIT. */
+typedef struct {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t lines, length;
+  int32_t bits;         /* 4 or 8 */
+} fp4_mx;
+
+int64_t mx_pitch(int64_t length);
+
+/* x [rows x cols], leading dimension ld -> an MX tensor along the rows (lines = rows, length = cols), one along the columns
+ * (transposed: lines = cols, length = rows), or both from one read of x.  Either may be NULL, not both.  No workspace. */
+int mx_quantize(const void* x, fp4_dtype dt, int64_t rows, int64_t cols, int64_t ld, const fp4_mx* along_rows,
+                const fp4_mx* along_cols, void* stream);
+
+/* The values of an MX tensor: x [lines x length], or with transposed != 0 x [length x lines].  Exact in either type, down to its
+ * smallest numbers. */
+int mx_dequantize(const fp4_mx* t, int transposed, void* x, fp4_dtype dt, int64_t ld, void* stream);
+
+/* out[P x Q] = l . rt^T (+ addend) over their common length, P = l->lines, Q = rt->lines, each operand in 4 or 8 bits; fp32 sums.
+ * addend: optional fp32 [P x Q] with out's leading dimension, added before the rounding of out; may be out itself where that is fp32.
+ * A length of 0 gives the addend, or zeros. */
+int mx_gemm(const fp4_mx* l, const fp4_mx* rt, const float* addend, void* out, fp4_dtype out_dt, int64_t ldo, void* stream);
+
+/* Forward: Y [M x N] = Q(A) Q(W), A [M x K] quantized here along its rows to act_bits, W along its columns by the caller (mx_quantize
+ * along_cols of the masters [K x N]: lines N, length K), once per weight version.  Y has A's type.
+ * saved: optional checkpoint of the activations for the weight gradient, filled here: A along its columns (lines K, length M), from
+ * the same read, in saved->bits.  mx_dequantize(saved, 1, ..) gives the activations back.  NULL: none is kept. */
+int mx_linear_fwd(const void* A, fp4_dtype dt, int64_t M, int64_t K, int64_t N, int64_t lda, int act_bits, const fp4_mx* W,
+                  void* Y, int64_t ldy, const fp4_mx* saved, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Activation gradient: dA [M x K] = Q(dY) Q(W)^T, dY [M x N] quantized here along its rows to 4 bits, W along its rows by the caller
+ * (lines K, length N).  dA has dY's type. */
+int mx_linear_bwd_dgrad(const void* dY, fp4_dtype dt, int64_t M, int64_t K, int64_t N, int64_t ldy, const fp4_mx* W, void* dA,
+                        int64_t lda, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Weight gradient: dW [K x N] = saved . Q(dY), contracting over the tokens: the checkpoint of mx_linear_fwd (lines K, length M) as it
+ * lies, dY quantized here along its columns to grad_bits.  dW is fp32; accumulate != 0 adds to what it holds (several micro-batches a
+ * step).  With no tokens dW becomes 0, or stays as it is. */
+int mx_linear_bwd_wgrad(const void* dY, fp4_dtype dt, int64_t M, int64_t K, int64_t N, int64_t ldy, const fp4_mx* saved,
+                        int grad_bits, int accumulate, float* dW, int64_t ldw, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/* Both gradients, the same bits as the two calls, dY read once. */
+int mx_linear_bwd(const void* dY, fp4_dtype dt, int64_t M, int64_t K, int64_t N, int64_t ldy, const fp4_mx* W, const fp4_mx* saved,
+                  int grad_bits, void* dA, int64_t lda, int accumulate, float* dW, int64_t ldw, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 /* One 4-bit code per output byte (for inspecting packed tensors). */
 int fp4_unpack(const uint8_t* codes, int64_t rows, int64_t cols, uint8_t* one_per_byte,

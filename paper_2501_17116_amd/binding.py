@@ -20,6 +20,7 @@ FP4_F32, FP4_BF16 = 0, 1
 FP4_AXIS_ROW, FP4_AXIS_COL, FP4_AXIS_TENSOR = 0, 1, 2
 FP4_OCC_TENSOR, FP4_OCC_TOKEN = 0, 1
 FP4_OP_QUANTIZE, FP4_OP_OCC, FP4_OP_FWD, FP4_OP_DGRAD, FP4_OP_WGRAD, FP4_OP_SPMM, FP4_OP_PREPARE, FP4_OP_FWD_MIXED, FP4_OP_BWD = range(9)
+FP4_OP_MX_FWD, FP4_OP_MX_DGRAD, FP4_OP_MX_WGRAD, FP4_OP_MX_BWD = range(9, 13)
 FP4_FMT_E2M1, FP4_FMT_E4M3 = 0, 1
 
 _lib = None
@@ -39,6 +40,10 @@ class fp4_fwd_ctx(C.Structure):
 
 class fp4_weight_cache(C.Structure):
     _fields_ = [("qWt", C.c_void_p), ("gamma_W", C.c_void_p), ("qWk", C.c_void_p), ("gamma_Wk", C.c_void_p)]
+
+
+class fp4_mx(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("lines", C.c_int64), ("length", C.c_int64), ("bits", C.c_int32)]
 
 
 def lib() -> C.CDLL:
@@ -84,6 +89,18 @@ def lib() -> C.CDLL:
         L.fp4_linear_fwd_granularity.argtypes = [vp, vp, i32, i64, i64, i64, i32, i32, f64, vp, C.POINTER(fp4_fwd_ctx), vp, sz,
                                                  vp]
         L.fp4_linear_fwd_granularity.restype = i32
+        mx = C.POINTER(fp4_mx)
+        L.mx_pitch.restype = i64
+        L.mx_pitch.argtypes = [i64]
+        L.mx_quantize.argtypes = [vp, i32, i64, i64, i64, mx, mx, vp]
+        L.mx_dequantize.argtypes = [mx, i32, vp, i32, i64, vp]
+        L.mx_gemm.argtypes = [mx, mx, vp, vp, i32, i64, vp]
+        L.mx_linear_fwd.argtypes = [vp, i32, i64, i64, i64, i64, i32, mx, vp, i64, mx, vp, sz, vp]
+        L.mx_linear_bwd_dgrad.argtypes = [vp, i32, i64, i64, i64, i64, mx, vp, i64, vp, sz, vp]
+        L.mx_linear_bwd_wgrad.argtypes = [vp, i32, i64, i64, i64, i64, mx, i32, i32, vp, i64, vp, sz, vp]
+        L.mx_linear_bwd.argtypes = [vp, i32, i64, i64, i64, i64, mx, mx, i32, vp, i64, i32, vp, i64, vp, sz, vp]
+        for name in ("mx_quantize", "mx_dequantize", "mx_gemm", "mx_linear_fwd", "mx_linear_bwd_dgrad", "mx_linear_bwd_wgrad", "mx_linear_bwd"):
+            getattr(L, name).restype = i32
         L.fp8_host_round_codes.argtypes = [vp, i64, vp]
         for name in ("fp8_quantize", "fp4_gemm_mixed", "fp4_linear_fwd_mixed", "fp8_host_round_codes"):
             getattr(L, name).restype = i32
@@ -514,6 +531,223 @@ def fp8_host_round_codes(x_host):
     _check(lib().fp8_host_round_codes(x.ctypes.data_as(C.c_void_p), x.size, out.ctypes.data_as(C.c_void_p)),
            "fp8_host_round_codes")
     return out
+
+
+MX_BLOCK, MX_PITCH = 32, 512
+
+
+def mx_pitch(length: int) -> int:
+    """Elements that a line of `length` takes in an MX tensor."""
+    return -(-length // MX_PITCH) * MX_PITCH
+
+
+class MxTensor:
+    """Codes and block scales of a matrix, blocks of 32 along its lines.
+
+    codes [lines, mx_pitch(length) / 2] (4 bits) or [2, lines, mx_pitch(length) / 2] (8 bits), scales [lines, mx_pitch(length) / 32],
+    uint8.  transposed: the lines are the columns of the matrix that the tensor stands for."""
+
+    __slots__ = ("codes", "scales", "bits", "lines", "length", "transposed", "c")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, length: int, transposed: bool = False):
+        _dev_check(codes, scales)
+        pitch = mx_pitch(length)
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+            raise TypeError("codes and scales must be uint8")
+        if scales.dim() != 2 or codes.shape[-1] != pitch // 2 or scales.shape[1] != pitch // MX_BLOCK or \
+                codes.shape[:-1] not in ((scales.shape[0],), (2, scales.shape[0])):
+            raise ValueError("codes %s and scales %s do not hold lines of %d elements" % (tuple(codes.shape), tuple(scales.shape), length))
+        if codes.device != scales.device:
+            raise ValueError("codes and scales must live on one device")
+        self.codes, self.scales, self.bits, self.lines, self.length, self.transposed = codes, scales, 4 * (codes.dim() - 1), scales.shape[0], length, transposed
+        self.c = fp4_mx(codes.data_ptr(), scales.data_ptr(), self.lines, length, self.bits)
+
+    @property
+    def shape(self) -> Tuple[int, int]:
+        """Of the matrix that the tensor stands for."""
+        return (self.length, self.lines) if self.transposed else (self.lines, self.length)
+
+
+def mx_empty(lines: int, length: int, bits: int = 4, transposed: bool = False, device="cuda") -> MxTensor:
+    if bits not in (4, 8):
+        raise ValueError("an MX element has 4 or 8 bits")
+    pitch = mx_pitch(length)
+    return MxTensor(torch.empty((lines, pitch // 2) if bits == 4 else (2, lines, pitch // 2), dtype=torch.uint8, device=device),
+                    torch.empty((lines, pitch // MX_BLOCK), dtype=torch.uint8, device=device), length, transposed)
+
+
+def _ld(t: torch.Tensor, name: str) -> int:
+    """Leading dimension of a matrix whose rows may lie apart."""
+    if not t.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix" % name)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s's rows must be contiguous" % name)
+    return t.stride(0) if rows > 1 and cols > 0 else max(8, -(-cols // 8) * 8)
+
+
+def _same_device(x: torch.Tensor, *mx: Optional[MxTensor]):
+    for t in mx:
+        if t is not None and t.codes.device != x.device:
+            raise ValueError("all tensors must live on one device")
+
+
+def _out(t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor, name: str) -> torch.Tensor:
+    """The caller's output, checked, or a new one; its rows begin at multiples of 16 bytes."""
+    if t is None:
+        rows, cols = shape
+        return torch.empty((rows, -(-cols // 8) * 8), dtype=dtype, device=like.device)[:, :cols]
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != like.device:
+        raise ValueError("%s must be %s %s on %s" % (name, tuple(shape), dtype, like.device))
+    return t
+
+
+def _mx_ref(t: Optional[MxTensor]):
+    return None if t is None else C.byref(t.c)
+
+
+def mx_quantize(x: torch.Tensor, axis: int, bits: int = 4, out: Optional[MxTensor] = None) -> MxTensor:
+    """x along its rows (FP4_AXIS_ROW) or along its columns, transposed (FP4_AXIS_COL)."""
+    if axis not in (FP4_AXIS_ROW, FP4_AXIS_COL):
+        raise ValueError("MX blocks lie along rows or columns")
+    ld = _ld(x, "x")
+    rows, cols = x.shape
+    lines, length = (rows, cols) if axis == FP4_AXIS_ROW else (cols, rows)
+    if out is None:
+        out = mx_empty(lines, length, bits, axis == FP4_AXIS_COL, x.device)
+    _same_device(x, out)
+    ref = _mx_ref(out)
+    _check(lib().mx_quantize(_ptr(x), _dt(x), rows, cols, ld, ref if axis == FP4_AXIS_ROW else None, ref if axis == FP4_AXIS_COL else None, _stream()),
+           "mx_quantize")
+    return out
+
+
+def mx_quantize_both(x: torch.Tensor, row_bits: int = 4, col_bits: int = 4) -> Tuple[MxTensor, MxTensor]:
+    """x along its rows and along its columns from one read."""
+    ld = _ld(x, "x")
+    rows, cols = x.shape
+    r, c = mx_empty(rows, cols, row_bits, False, x.device), mx_empty(cols, rows, col_bits, True, x.device)
+    _check(lib().mx_quantize(_ptr(x), _dt(x), rows, cols, ld, _mx_ref(r), _mx_ref(c), _stream()), "mx_quantize")
+    return r, c
+
+
+def mx_dequantize(t: MxTensor, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The matrix that t stands for, in the values of its codes."""
+    x = _out(out, t.shape, dtype, t.codes, "out")
+    _check(lib().mx_dequantize(_mx_ref(t), int(t.transposed), _ptr(x), _dt(x), _ld(x, "out"), _stream()), "mx_dequantize")
+    return x
+
+
+def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """l . rt^T over their lines' common length (+ addend)."""
+    if l.length != rt.length:
+        raise ValueError("operands disagree in the contraction's length")
+    _same_device(l.codes, rt)
+    out = _out(out, (l.lines, rt.lines), out.dtype if out is not None else out_dtype, l.codes, "out")
+    ldo = _ld(out, "out")
+    if addend is not None:
+        if tuple(addend.shape) != tuple(out.shape) or addend.dtype != torch.float32 or addend.device != out.device:
+            raise ValueError("addend must be %s float32 on %s" % (tuple(out.shape), out.device))
+        if addend.shape[0] > 1 and _ld(addend, "addend") != ldo:
+            raise ValueError("addend and out must have the same leading dimension")
+    _check(lib().mx_gemm(_mx_ref(l), _mx_ref(rt), _ptr(addend), _ptr(out), _dt(out), ldo, _stream()), "mx_gemm")
+    return out
+
+
+def mx_checkpoint(M: int, K: int, bits: int = 8, device="cuda") -> MxTensor:
+    """Room for the checkpoint of activations [M, K]: what mx_linear_fwd leaves for the weight gradient."""
+    return mx_empty(K, M, bits, True, device)
+
+
+def mx_checkpoint_save(x: torch.Tensor, bits: int = 8) -> MxTensor:
+    """The checkpoint by itself; mx_linear_fwd writes the same from the read that it makes anyway."""
+    return mx_quantize(x, FP4_AXIS_COL, bits)
+
+
+class MxWeights:
+    """Both orientations of a layer's weights W [K, N]: fwd (lines N, length K) for the forward pass, bwd (lines K, length N) for the
+    activation gradient.  Made once per weight version."""
+
+    def __init__(self, fwd: MxTensor, bwd: MxTensor):
+        self.fwd, self.bwd = fwd, bwd
+
+
+def mx_prepare_weights(W: torch.Tensor) -> MxWeights:
+    bwd, fwd = mx_quantize_both(W)
+    return MxWeights(fwd, bwd)
+
+
+def mx_linear_fwd(A: torch.Tensor, W: MxTensor, act_bits: int = 4, saved: Optional[MxTensor] = None,
+                  Y: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None) -> torch.Tensor:
+    """Y = Q(A) W; saved: an mx_checkpoint that the pass fills for the weight gradient."""
+    lda = _ld(A, "A")
+    M, K = A.shape
+    N = W.lines
+    if W.length != K:
+        raise ValueError("A [M,K] and W (lines N, length K) must agree in K")
+    if saved is not None and (saved.lines, saved.length) != (K, M):
+        raise ValueError("the checkpoint holds %d x %d activations, not %d x %d" % (saved.length, saved.lines, M, K))
+    _same_device(A, W, saved)
+    Y = _out(Y, (M, N), A.dtype, A, "Y")
+    w = _ws(workspace_bytes(FP4_OP_MX_FWD, M, K, N, _dt(A)), ws)
+    _check(lib().mx_linear_fwd(_ptr(A), _dt(A), M, K, N, lda, act_bits, _mx_ref(W), _ptr(Y), _ld(Y, "Y"), _mx_ref(saved), _ptr(w), w.numel(),
+                               _stream()), "mx_linear_fwd")
+    return Y
+
+
+def mx_linear_bwd_dgrad(dY: torch.Tensor, W: MxTensor, dA: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None) -> torch.Tensor:
+    """dA = Q(dY) W^T, W along its rows (lines K, length N)."""
+    ldy = _ld(dY, "dY")
+    M, N = dY.shape
+    K = W.lines
+    if W.length != N:
+        raise ValueError("dY [M,N] and W (lines K, length N) must agree in N")
+    _same_device(dY, W)
+    dA = _out(dA, (M, K), dY.dtype, dY, "dA")
+    w = _ws(workspace_bytes(FP4_OP_MX_DGRAD, M, K, N, _dt(dY)), ws)
+    _check(lib().mx_linear_bwd_dgrad(_ptr(dY), _dt(dY), M, K, N, ldy, _mx_ref(W), _ptr(dA), _ld(dA, "dA"), _ptr(w), w.numel(), _stream()),
+           "mx_linear_bwd_dgrad")
+    return dA
+
+
+def mx_linear_bwd_wgrad(dY: torch.Tensor, saved: MxTensor, grad_bits: int = 4, dW: Optional[torch.Tensor] = None,
+                        accumulate: bool = False, ws: Optional[Workspace] = None) -> torch.Tensor:
+    """dW (+)= saved . Q(dY), contracting over the tokens."""
+    ldy = _ld(dY, "dY")
+    M, N = dY.shape
+    K = saved.lines
+    if saved.length != M:
+        raise ValueError("dY [M,N] and the checkpoint must agree in M")
+    if accumulate and dW is None:
+        raise ValueError("accumulate needs the dW to add to")
+    _same_device(dY, saved)
+    dW = _out(dW, (K, N), torch.float32, dY, "dW")
+    w = _ws(workspace_bytes(FP4_OP_MX_WGRAD, M, K, N, _dt(dY)), ws)
+    _check(lib().mx_linear_bwd_wgrad(_ptr(dY), _dt(dY), M, K, N, ldy, _mx_ref(saved), grad_bits, int(accumulate), _ptr(dW), _ld(dW, "dW"), _ptr(w),
+                                     w.numel(), _stream()), "mx_linear_bwd_wgrad")
+    return dW
+
+
+def mx_linear_bwd(dY: torch.Tensor, saved: MxTensor, W: MxTensor, grad_bits: int = 4, dA: Optional[torch.Tensor] = None,
+                  dW: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[Workspace] = None):
+    """Both gradients, dY read once.  Returns (dA, dW)."""
+    ldy = _ld(dY, "dY")
+    M, N = dY.shape
+    K = W.lines
+    if W.length != N or (saved.lines, saved.length) != (K, M):
+        raise ValueError("dY [M,N], W (lines K, length N) and the checkpoint must agree")
+    if accumulate and dW is None:
+        raise ValueError("accumulate needs the dW to add to")
+    _same_device(dY, W, saved)
+    dA = _out(dA, (M, K), dY.dtype, dY, "dA")
+    dW = _out(dW, (K, N), torch.float32, dY, "dW")
+    w = _ws(workspace_bytes(FP4_OP_MX_BWD, M, K, N, _dt(dY)), ws)
+    _check(lib().mx_linear_bwd(_ptr(dY), _dt(dY), M, K, N, ldy, _mx_ref(W), _mx_ref(saved), grad_bits, _ptr(dA), _ld(dA, "dA"), int(accumulate),
+                               _ptr(dW), _ld(dW, "dW"), _ptr(w), w.numel(), _stream()), "mx_linear_bwd")
+    return dA, dW
 
 
 def fp4_unpack(codes: torch.Tensor) -> torch.Tensor:

@@ -85,6 +85,7 @@ int64_t fp4_spmm_scratch_words(int64_t P, int64_t Q, int64_t N, int bf16);
 int fp4_launch_spmm(const int64_t* row_ptr, const int32_t* col_idx, const float* val, int64_t capacity,
                     int64_t P, int64_t Q, const void* D, int bf16, int64_t N, float* R, int32_t* scratch,
                     hipStream_t s, bool general = false);
+size_t mx_workspace_bytes(int op, int64_t M, int64_t K, int64_t N);
 
 namespace {
 
@@ -269,6 +270,10 @@ extern "C" size_t fp4_workspace_bytes(int op, int64_t M, int64_t K, int64_t N, f
       c.take<uint16_t>((size_t)fp4_dual_axis_part_elems(M, N));
       break;
     case FP4_OP_SPMM: c.take<int32_t>((size_t)fp4_spmm_scratch_words(M, K, N, dt == FP4_BF16)); break;
+    case FP4_OP_MX_FWD:
+    case FP4_OP_MX_DGRAD:
+    case FP4_OP_MX_WGRAD:
+    case FP4_OP_MX_BWD: return mx_workspace_bytes(op, M, K, N);
     default: return 0;
   }
   return c.off + 256;

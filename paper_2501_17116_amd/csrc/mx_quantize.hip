@@ -1,0 +1,395 @@
+// Microscaled quantization along rows, along columns (transposed) and both from one read, and the way back.
+//
+// A block's scale depends on its 32 elements alone, so every pass reads its input once and is bound by memory: b + 1/2 + 1/32 bytes an
+// element for 4 bits along one axis (b = 2 bf16, 4 fp32), b + 1 + 1/32 for 8, their sum without the second b for both axes.
+//   rows: four lanes hold a block of bf16 (eight elements, 16 bytes each), so a wave takes 512 elements of a row, loads, codes and
+//         scales are contiguous, and the block's maximum is two lane exchanges away.
+//   columns: a wave takes 32 rows; the rows' 16-byte pieces go through the wave's own LDS and come back as one dword a row, a lane
+//         holding its columns' whole blocks: maxima and codes need no exchange, and the codes leave transposed.  The same pieces make
+//         the rows' blocks before they are parked, which is the whole cost of the second axis.
+#include "mx_common.h"
+
+#include <algorithm>
+
+namespace {
+
+constexpr int NO_AXIS = 0;
+
+struct QuantArgs {
+  const void* x;
+  int64_t rows, cols, ld;
+  uint8_t *row_codes, *row_scales, *col_codes, *col_scales;
+};
+
+// max with a lane of the same group of four / eight
+FP4_D uint32_t quad_max(uint32_t v) {
+  uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true);   // lane ^ 1
+  v = v > o ? v : o;
+  o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true);            // lane ^ 2
+  return v > o ? v : o;
+}
+FP4_D uint32_t other_quad(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true); }   // mirrored in eight lanes
+
+// A 16-byte piece of a row: eight bf16 or four fp32 from column c on; zeros behind the row's end and in rows that are not there.
+template <class T>
+FP4_D u32x4 load_piece(const void* x, int64_t row, int64_t rows, int64_t cols, int64_t ld, int64_t c) {
+  constexpr int E = sizeof(T);
+  constexpr int N = 16 / E;
+  u32x4 w = {0u, 0u, 0u, 0u};
+  if (row < rows) {
+    const T* p = reinterpret_cast<const T*>(x) + row * ld + c;
+    if (c + N <= cols) {
+      w = *reinterpret_cast<const u32x4*>(p);
+    } else {
+      union { T t[N]; u32x4 v; } u;
+      u.v = w;
+      for (int e = 0; e < N; ++e)
+        if (c + e < cols) u.t[e] = p[e];
+      w = u.v;
+    }
+  }
+  return w;
+}
+
+FP4_D u32x4 magnitudes_bf16(const u32x4& w) { return u32x4{w.x & 0x7fff7fffu, w.y & 0x7fff7fffu, w.z & 0x7fff7fffu, w.w & 0x7fff7fffu}; }
+FP4_D uint32_t amax_bf16(const u32x4& w) {   // bits of the largest magnitude of eight bf16, as fp32
+  const u32x4 m = magnitudes_bf16(w);
+  const uint32_t a = mx_pk_max_u16(mx_pk_max_u16(m.x, m.y), mx_pk_max_u16(m.z, m.w));
+  const uint32_t lo = a & 0xffffu, hi = a >> 16;
+  return (lo > hi ? lo : hi) << 16;
+}
+FP4_D uint32_t amax_f32(const u32x4& w) {
+  const uint32_t a = w.x & 0x7fffffffu, b = w.y & 0x7fffffffu, c = w.z & 0x7fffffffu, d = w.w & 0x7fffffffu;
+  const uint32_t ab = a > b ? a : b, cd = c > d ? c : d;
+  return ab > cd ? ab : cd;
+}
+
+// ---- rows --------------------------------------------------------------------------------------------------------------------
+// A wave takes 512 elements of a row at a time (a unit of the pitch), ROWS_U of them from consecutive units.
+constexpr int ROWS_U = 4;
+
+template <class T, int BITS>
+__global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units, int per_row) {
+  const int lane = threadIdx.x & 63;
+  const int64_t u0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * ROWS_U;
+  constexpr int P = sizeof(T) == 2 ? 1 : 2;   // pieces a lane
+  u32x4 w[ROWS_U][P];
+  int64_t row[ROWS_U];
+  int seg[ROWS_U];
+#pragma unroll
+  for (int i = 0; i < ROWS_U; ++i) {
+    row[i] = (u0 + i) / per_row;
+    seg[i] = (int)((u0 + i) - row[i] * per_row);
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      w[i][p] = load_piece<T>(a.x, u0 + i < units ? row[i] : a.rows, a.rows, a.cols, a.ld, (int64_t)seg[i] * MX_PITCH + lane * 8 + p * 4);
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS_U; ++i) {
+    if (u0 + i >= units) break;
+    uint32_t top;
+    if constexpr (P == 1) top = amax_bf16(w[i][0]);
+    else {
+      const uint32_t t0 = amax_f32(w[i][0]), t1 = amax_f32(w[i][P - 1]);
+      top = t0 > t1 ? t0 : t1;
+    }
+    const uint32_t byte = mx_scale_byte<BITS>(quad_max(top));
+    const float s = mx_scale_f32(byte);
+    const int64_t unit = u0 + i;   // lines are pitch / 512 units long, so units are numbered as they lie
+    uint32_t h, l;
+    if constexpr (P == 1) mx_encode8<BITS>(w[i][0], s, h, l);
+    else {
+      const float v[8] = {u2f(w[i][0].x), u2f(w[i][0].y), u2f(w[i][0].z), u2f(w[i][0].w), u2f(w[i][P - 1].x), u2f(w[i][P - 1].y), u2f(w[i][P - 1].z), u2f(w[i][P - 1].w)};
+      mx_encode8<BITS>(v, s, h, l);
+    }
+    reinterpret_cast<uint32_t*>(a.row_codes)[unit * 64 + lane] = h;
+    if constexpr (BITS == 8) reinterpret_cast<uint32_t*>(a.row_codes)[(units + unit) * 64 + lane] = l;
+    if ((lane & 3) == 0) a.row_scales[unit * 16 + (lane >> 2)] = (uint8_t)byte;
+  }
+}
+
+// ---- columns, and rows beside them ----------------------------------------------------------------------------------------------
+// A workgroup of four waves takes 128 rows x 256 bytes of columns, a wave 32 of the rows: one block of every column.
+template <class T, int ROW, int COL>
+__global__ __launch_bounds__(256) void mx_tile_kernel(QuantArgs a) {
+  constexpr int E = sizeof(T);
+  constexpr int CW = 256 / E;        // columns a tile
+  constexpr int EPP = 16 / E;        // elements of a 16-byte piece
+  __shared__ __attribute__((aligned(16))) uint32_t park[4][32 * 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t r0 = (int64_t)blockIdx.y * 128 + wave * 32;
+  const int64_t c0 = (int64_t)blockIdx.x * CW;
+  const int64_t row_pitch = mx_pitch_of(a.cols), col_pitch = mx_pitch_of(a.rows);
+  const int piece = lane & 15, sub = lane >> 4;
+  u32x4 w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = load_piece<T>(a.x, r0 + i * 4 + sub, a.rows, a.cols, a.ld, c0 + piece * EPP);
+  uint32_t* const mine = park[wave];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(mine + (i * 4 + sub) * 64 + piece * 4) = w[i];
+  if constexpr (ROW != NO_AXIS) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = r0 + i * 4 + sub;
+      uint32_t top = quad_max(E == 2 ? amax_bf16(w[i]) : amax_f32(w[i]));
+      if constexpr (E == 4) {
+        const uint32_t o = other_quad(top);
+        top = top > o ? top : o;
+      }
+      const uint32_t byte = mx_scale_byte<ROW>(top);
+      const float s = mx_scale_f32(byte);
+      const int64_t at = row * row_pitch + c0 + piece * EPP;
+      if (row < a.rows) {
+        uint32_t h, l;
+        uint8_t *const ph = a.row_codes + at / 2, *const pl = ph + a.rows * row_pitch / 2;
+        if constexpr (E == 2) {
+          mx_encode8<ROW>(w[i], s, h, l);
+          *reinterpret_cast<uint32_t*>(ph) = h;
+          if constexpr (ROW == 8) *reinterpret_cast<uint32_t*>(pl) = l;
+        } else {
+          h = l = 0;
+          mx_pair<ROW, 0>(u2f(w[i].x), u2f(w[i].y), s, h, l);
+          mx_pair<ROW, 1>(u2f(w[i].z), u2f(w[i].w), s, h, l);
+          *reinterpret_cast<uint16_t*>(ph) = (uint16_t)h;
+          if constexpr (ROW == 8) *reinterpret_cast<uint16_t*>(pl) = (uint16_t)l;
+        }
+        if (piece % (MX_BLOCK / EPP) == 0) a.row_scales[at / MX_BLOCK] = (uint8_t)byte;
+      }
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  uint32_t d[32];
+#pragma unroll
+  for (int r = 0; r < 32; ++r) d[r] = mine[r * 64 + lane];
+  constexpr int NC = 4 / E;   // columns a lane
+#pragma unroll
+  for (int h = 0; h < NC; ++h) {
+    const int64_t col = c0 + lane * NC + h;
+    uint32_t top = 0;
+    if constexpr (E == 2) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) {
+        const uint32_t m = (h == 0 ? d[r] << 16 : d[r] & 0xffff0000u) & 0x7fffffffu;
+        top = top > m ? top : m;
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) {
+        const uint32_t m = d[r] & 0x7fffffffu;
+        top = top > m ? top : m;
+      }
+    }
+    const uint32_t byte = mx_scale_byte<COL>(top);
+    const float s = mx_scale_f32(byte);
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {   // eight rows
+      if constexpr (E == 2) {
+        u32x4 pr;   // rows 2 i and 2 i + 1 of this column
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_perm(d[8 * q + 2 * i + 1], d[8 * q + 2 * i], h == 0 ? 0x05040100u : 0x07060302u);
+        mx_encode8<COL>(pr, s, hi[q], lo[q]);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = u2f(d[8 * q + i]);
+        mx_encode8<COL>(v, s, hi[q], lo[q]);
+      }
+    }
+    if (col < a.cols) {
+      const int64_t at = col * col_pitch + r0;
+      *reinterpret_cast<u32x4*>(a.col_codes + at / 2) = u32x4{hi[0], hi[1], hi[2], hi[3]};
+      if constexpr (COL == 8) *reinterpret_cast<u32x4*>(a.col_codes + (a.cols * col_pitch + at) / 2) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+      a.col_scales[at / MX_BLOCK] = (uint8_t)byte;
+    }
+  }
+}
+
+// ---- back ----------------------------------------------------------------------------------------------------------------------
+struct DequantArgs {
+  const uint8_t *codes, *scales;
+  void* x;
+  int64_t lines, length, ld;
+};
+
+FP4_D float decode_scale(uint32_t byte) { return u2f(byte ? byte << 23 : 0x00400000u); }   // 2^(byte - 127)
+
+// eight codes, of 8 bits two words of them, under one scale -> eight fp32; byte 255: NaN throughout
+template <int BITS>
+FP4_D void decode8(const uint32_t (&c)[BITS / 4], uint32_t byte, float (&o)[8]) {
+  const float s = decode_scale(byte), t = BITS == 4 ? s : 1.0f;   // of 8 bits the codes are joined before they are scaled: s h alone may overflow
+  mx_f32x2 v[4];
+  v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], t, 0);
+  v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], t, 1);
+  v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], t, 2);
+  v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], t, 3);
+  if constexpr (BITS == 8) {
+    mx_f32x2 l[4];
+    l[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[1], 0.125f, 0);
+    l[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[1], 0.125f, 1);
+    l[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[1], 0.125f, 2);
+    l[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[1], 0.125f, 3);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i].x = (v[i].x + l[i].x) * s;
+      v[i].y = (v[i].y + l[i].y) * s;
+    }
+  }
+  const float nan = u2f(0x7fffffffu);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = byte == 255u ? nan : v[i / 2][i & 1];
+}
+// ... -> four pairs of bf16, exactly: s (h + l / 8) has seven bits
+template <int BITS>
+FP4_D void decode8(const uint32_t (&c)[BITS / 4], uint32_t byte, uint32_t (&o)[4]) {
+  if constexpr (BITS == 4) {
+    const float s = decode_scale(byte);
+    o[0] = mx_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[0], s, 0));
+    o[1] = mx_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[0], s, 1));
+    o[2] = mx_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[0], s, 2));
+    o[3] = mx_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[0], s, 3));
+    if (byte == 255u) o[0] = o[1] = o[2] = o[3] = 0x7fff7fffu;
+  } else {
+    float v[8];
+    decode8<BITS>(c, byte, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = (f2u(v[2 * i]) >> 16) | (f2u(v[2 * i + 1]) & 0xffff0000u);
+  }
+}
+
+// Eight elements of a row from column c on; the row may end among them.
+FP4_D void store8(uint16_t* p, const uint32_t (&o)[4], int64_t left) {
+  if (left >= 8) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{o[0], o[1], o[2], o[3]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
+  }
+}
+FP4_D void store8(float* p, const float (&o)[8], int64_t left) {
+  if (left >= 8) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{o[0], o[1], o[2], o[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{o[4], o[5], o[6], o[7]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = o[e];
+  }
+}
+template <class T> struct Eight;
+template <> struct Eight<uint16_t> { typedef uint32_t type[4]; };
+template <> struct Eight<float> { typedef float type[8]; };
+
+// Lines as rows: a lane takes eight codes.
+template <class T, int BITS>
+__global__ __launch_bounds__(256) void mx_restore_rows_kernel(DequantArgs a, int64_t units, int per_line) {
+  const int lane = threadIdx.x & 63;
+  const int64_t u0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * ROWS_U;
+  uint32_t c[ROWS_U][BITS / 4], b[ROWS_U];
+#pragma unroll
+  for (int i = 0; i < ROWS_U; ++i) {
+    const int64_t u = u0 + i < units ? u0 + i : units - 1;
+#pragma unroll
+    for (int k = 0; k < BITS / 4; ++k) c[i][k] = reinterpret_cast<const uint32_t*>(a.codes)[(k * units + u) * 64 + lane];
+    b[i] = a.scales[u * 16 + (lane >> 2)];
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS_U; ++i) {
+    if (u0 + i >= units) break;
+    const int64_t line = (u0 + i) / per_line;
+    const int64_t at = ((u0 + i) - line * per_line) * MX_PITCH + lane * 8;
+    if (at >= a.length) continue;
+    typename Eight<T>::type o;
+    decode8<BITS>(c[i], b[i], o);
+    store8(reinterpret_cast<T*>(a.x) + line * a.ld + at, o, a.length - at);
+  }
+}
+
+// Lines as columns: a lane takes eight rows of eight columns, a wave 64 x 64.
+template <class T, int BITS>
+__global__ __launch_bounds__(256) void mx_restore_cols_kernel(DequantArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t r0 = (int64_t)blockIdx.x * 256 + wave * 64 + (lane >> 3) * 8;   // the element of a line = the row of x
+  const int64_t c0 = (int64_t)blockIdx.y * 64 + (lane & 7) * 8;                 // the line = the column of x
+  const int64_t pitch = mx_pitch_of(a.length);
+  if (r0 >= a.length || c0 >= a.lines) return;
+  uint32_t c[8][BITS / 4], b[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int64_t line = c0 + j < a.lines ? c0 + j : a.lines - 1;
+    const int64_t at = line * pitch + r0;
+#pragma unroll
+    for (int k = 0; k < BITS / 4; ++k) c[j][k] = reinterpret_cast<const uint32_t*>(a.codes)[(k * a.lines * pitch + at) / 8];
+    b[j] = a.scales[at / MX_BLOCK];
+  }
+  typename Eight<T>::type o[8];   // by column
+#pragma unroll
+  for (int j = 0; j < 8; ++j) decode8<BITS>(c[j], b[j], o[j]);
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    if (r0 + r >= a.length) break;
+    typename Eight<T>::type v;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_perm(o[2 * j + 1][r / 2], o[2 * j][r / 2], (r & 1) ? 0x07060302u : 0x05040100u);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = o[j][r];
+    }
+    store8(reinterpret_cast<T*>(a.x) + (r0 + r) * a.ld + c0, v, a.lines - c0);
+  }
+}
+
+template <class T, int ROW>
+void launch_tiles(const QuantArgs& a, int col_bits, hipStream_t s) {
+  const dim3 grid((unsigned)(mx_pitch_of(a.cols) * sizeof(T) / 256), (unsigned)(mx_pitch_of(a.rows) / 128));
+  if (col_bits == 4) hipLaunchKernelGGL((mx_tile_kernel<T, ROW, 4>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((mx_tile_kernel<T, ROW, 8>), grid, dim3(256), 0, s, a);
+}
+
+template <class T>
+int launch_quantize(const QuantArgs& a, int row_bits, int col_bits, hipStream_t s) {
+  if (col_bits == NO_AXIS) {
+    const int per_row = (int)(mx_pitch_of(a.cols) / MX_PITCH);
+    const int64_t units = a.rows * per_row;
+    const dim3 grid((unsigned)((units + 4 * ROWS_U - 1) / (4 * ROWS_U)));
+    if (row_bits == 4) hipLaunchKernelGGL((mx_rows_kernel<T, 4>), grid, dim3(256), 0, s, a, units, per_row);
+    else hipLaunchKernelGGL((mx_rows_kernel<T, 8>), grid, dim3(256), 0, s, a, units, per_row);
+  } else if (row_bits == NO_AXIS) launch_tiles<T, NO_AXIS>(a, col_bits, s);
+  else if (row_bits == 4) launch_tiles<T, 4>(a, col_bits, s);
+  else launch_tiles<T, 8>(a, col_bits, s);
+  FP4_CHECK_LAUNCH();
+  return FP4_OK;
+}
+
+template <class T, int BITS>
+int launch_dequantize(const DequantArgs& a, bool transposed, hipStream_t s) {
+  if (transposed) {
+    const dim3 grid((unsigned)((a.length + 255) / 256), (unsigned)((a.lines + 63) / 64));
+    hipLaunchKernelGGL((mx_restore_cols_kernel<T, BITS>), grid, dim3(256), 0, s, a);
+  } else {
+    const int per_line = (int)(mx_pitch_of(a.length) / MX_PITCH);
+    const int64_t units = a.lines * per_line;
+    hipLaunchKernelGGL((mx_restore_rows_kernel<T, BITS>), dim3((unsigned)((units + 4 * ROWS_U - 1) / (4 * ROWS_U))), dim3(256), 0, s, a, units, per_line);
+  }
+  FP4_CHECK_LAUNCH();
+  return FP4_OK;
+}
+
+}  // namespace
+
+// row_bits / col_bits: 4 or 8, or 0 where that axis is not wanted.  rows and cols are at least 1.
+int mx_launch_quantize(const void* x, int bf16, int64_t rows, int64_t cols, int64_t ld, int row_bits, uint8_t* row_codes, uint8_t* row_scales,
+                       int col_bits, uint8_t* col_codes, uint8_t* col_scales, hipStream_t s) {
+  const QuantArgs a = {x, rows, cols, ld, row_codes, row_scales, col_codes, col_scales};
+  return bf16 ? launch_quantize<uint16_t>(a, row_bits, col_bits, s) : launch_quantize<float>(a, row_bits, col_bits, s);
+}
+
+int mx_launch_dequantize(const uint8_t* codes, const uint8_t* scales, int bits, int64_t lines, int64_t length, bool transposed, void* x, int bf16,
+                         int64_t ld, hipStream_t s) {
+  const DequantArgs a = {codes, scales, x, lines, length, ld};
+  if (bf16) return bits == 4 ? launch_dequantize<uint16_t, 4>(a, transposed, s) : launch_dequantize<uint16_t, 8>(a, transposed, s);
+  return bits == 4 ? launch_dequantize<float, 4>(a, transposed, s) : launch_dequantize<float, 8>(a, transposed, s);
+}
