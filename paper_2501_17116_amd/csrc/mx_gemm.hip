@@ -13,9 +13,13 @@
 #include "mx_common.h"
 
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 typedef int mx_i32x8 __attribute__((ext_vector_type(8)));
 typedef float mx_f32x16 __attribute__((ext_vector_type(16)));
+
+int fp4_compute_units_of_current_device();
 
 namespace {
 
@@ -27,14 +31,29 @@ struct MxGemm {
   int64_t planeL, planeR;   // bytes of a plane of codes
   int64_t pitch;            // elements of a line
   int nl, nr;               // planes
+  int tiles_p, tiles_q;
+  int first, count;         // tiles of this launch, in the order of tile_at
 };
 
-// first operand: columns (Rt), second: rows (L); S: the byte of the scale registers, 0 or 2
+template <class F, int... I>
+FP4_D void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+FP4_D void static_for(F&& f) {
+  static_for_impl(f, std::make_integer_sequence<int, N>{});
+}
+
+// First operand: columns (Rt), second: rows (L).  S: the byte of the scale registers.  A step is 256 codes of a line, of which lane
+// half h takes 128 h .. 128 h + 127: its four words of codes a slice, its one word of scales the four slices in order, so that no scale
+// has to be moved to its place (the instruction does not mind which elements of a line meet, only that those of both operands do).
 template <int S>
 FP4_D mx_f32x16 mx_mfma(const u32x4& r, const u32x4& l, const mx_f32x16& c, uint32_t sr, uint32_t sl) {
   const mx_i32x8 a = {(int)r.x, (int)r.y, (int)r.z, (int)r.w, 0, 0, 0, 0}, b = {(int)l.x, (int)l.y, (int)l.z, (int)l.w, 0, 0, 0, 0};
   if constexpr (S == 0) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 0, (int)sr, 0, (int)sl);
-  else return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 2, (int)sr, 2, (int)sl);
+  else if constexpr (S == 1) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 1, (int)sr, 1, (int)sl);
+  else if constexpr (S == 2) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 2, (int)sr, 2, (int)sl);
+  else return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 3, (int)sr, 3, (int)sl);
 }
 
 FP4_D uint32_t mx_pack_bf16x2(float a, float b) {
@@ -78,16 +97,18 @@ __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
   for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
   for (int pass = 0; pass < g.nl * g.nr; ++pass) {
     const int pl = pass % g.nl, pr = pass / g.nl;
-    const uint8_t *l = g.L + pl * g.planeL + p * (g.pitch / 2) + h * 16, *r = g.R + pr * g.planeR + q * (g.pitch / 2) + h * 16;
+    const uint8_t *l = g.L + pl * g.planeL + p * (g.pitch / 2) + h * 64, *r = g.R + pr * g.planeR + q * (g.pitch / 2) + h * 64;
     const uint32_t lessl = pl ? MX_EIGHTH : 0u, lessr = pr ? MX_EIGHTH : 0u;
-    for (int64_t k = 0; k < g.pitch / 128; k += 4) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {   // 128 codes, one word of scales
-        const uint32_t bl = (sl[k + j] - lessl) >> (8 * h), br = (sr[k + j] - lessr) >> (8 * h);
-        const u32x4 *lv = reinterpret_cast<const u32x4*>(l + (k + j) * 64), *rv = reinterpret_cast<const u32x4*>(r + (k + j) * 64);
-        acc = mx_mfma<0>(rv[0], lv[0], acc, br, bl);
-        acc = mx_mfma<2>(rv[2], lv[2], acc, br, bl);
-      }
+    for (int64_t k = 0; k < g.pitch / 256; k += 2) {
+      static_for<2>([&](auto jc) {   // 256 codes, one word of scales
+        constexpr int j = decltype(jc)::value;
+        const uint32_t bl = sl[2 * (k + j) + h] - lessl, br = sr[2 * (k + j) + h] - lessr;
+        const u32x4 *lv = reinterpret_cast<const u32x4*>(l + (k + j) * 128), *rv = reinterpret_cast<const u32x4*>(r + (k + j) * 128);
+        static_for<4>([&](auto sc) {
+          constexpr int sl4 = decltype(sc)::value;
+          acc = mx_mfma<sl4>(rv[sl4], lv[sl4], acc, br, bl);
+        });
+      });
     }
   }
   if (P0 + l32 >= g.P) return;
@@ -99,10 +120,322 @@ __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
   }
 }
 
+// ---- 256 x 256 ------------------------------------------------------------------------------------------------------------------
+// For outputs that go round the chip in 256 x 256 tiles.  Eight waves (2 along rows x 4 along columns, 128 x 64 each), persistent
+// workgroups, K step 256 codes.  Operands come into two LDS stages by direct-to-LDS loads, the scales of two steps at a time (16 bytes of
+// every row, one load a thread) into a ring of two of their own; the two waves of a SIMD alternate between a compute phase (16 matrix
+// instructions) and a memory phase (the fragments of the next two slices, and once a step its share of the loads of the step after
+// next), half a period apart.  The next tile's first stage travels while a tile's epilogue runs.
+// An operand stage: row r takes bytes [128 r, 128 r + 128), its 16-byte chunk c sits in slot c ^ ((r >> 1) & 7), so that sixteen rows
+// reading one chunk touch sixteen different bank groups.  Bound: the matrix cores at the clock that random operands leave them.
+constexpr int BT = 256, BKB = 128;
+constexpr int BWAVES = 8;
+constexpr int BLD = BT * 8 / (BWAVES * 64);      // 16-byte chunks a thread, operand and step
+constexpr int QI = 2, PJ = 4;                    // 32 x 32 blocks of a wave
+constexpr int OP_BYTES = BT * BKB, STAGE_BYTES = 2 * OP_BYTES;
+constexpr int EPI_LD = QI * 32 + 4, EPI_BYTES = BWAVES * 32 * EPI_LD * 4;
+constexpr int SC_BASE = STAGE_BYTES + (EPI_BYTES > STAGE_BYTES ? EPI_BYTES : STAGE_BYTES), SC_BYTES = 2 * BT * 16;   // the epilogue's rows lie over stage 1
+constexpr int BIG_SMEM = SC_BASE + 2 * SC_BYTES;
+static_assert(BIG_SMEM <= 160 * 1024, "LDS budget");
+constexpr int GROUP_P = 8;   // tile rows side by side
+
+FP4_D void tile_at(const MxGemm& g, int id, int& tp, int& tq) {
+  const int in_group = GROUP_P * g.tiles_q, group = id / in_group, first_p = group * GROUP_P;
+  const int gsz = min(g.tiles_p - first_p, GROUP_P);
+  tp = first_p + (id % in_group) % gsz;
+  tq = (id % in_group) / gsz;
+}
+
+FP4_D const uint8_t* uniform_ptr(const uint8_t* p) {
+  const uint64_t v = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return (const uint8_t*)(((uint64_t)hi << 32) | lo);
+}
+FP4_D __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* p, int64_t rows, int64_t pitch) {   // over so many rows; they stay below 2^30 bytes
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(uniform_ptr(p)), 0, __builtin_amdgcn_readfirstlane((int)(rows * pitch)), 0x00020000);
+}
+#define MX_TO_LDS(rsrc, lds, width, voff, soff) \
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds), width, voff, soff, 0, 0)
+
+// Eight columns of a row from q on, y without the addend.
 template <bool OUT_BF16>
-int launch(const MxGemm& g, hipStream_t s) {
-  const dim3 grid((unsigned)((g.P + 63) / 64), (unsigned)((g.Q + 63) / 64));
-  hipLaunchKernelGGL((mx_gemm_small_kernel<OUT_BF16>), grid, dim3(256), 0, s, g);
+FP4_D void store8(const MxGemm& g, int64_t at, int64_t left, const float (&y)[8]) {
+  if (left >= 8) {
+    if constexpr (OUT_BF16) {
+      *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(g.out) + at) =
+          u32x4{mx_pack_bf16x2(y[0], y[1]), mx_pack_bf16x2(y[2], y[3]), mx_pack_bf16x2(y[4], y[5]), mx_pack_bf16x2(y[6], y[7])};
+    } else {
+      float* o = reinterpret_cast<float*>(g.out) + at;
+      *reinterpret_cast<f32x4*>(o) = f32x4{y[0], y[1], y[2], y[3]};
+      *reinterpret_cast<f32x4*>(o + 4) = f32x4{y[4], y[5], y[6], y[7]};
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) {
+        if constexpr (OUT_BF16) reinterpret_cast<uint16_t*>(g.out)[at + e] = (uint16_t)mx_pack_bf16x2(y[e], y[e]);
+        else reinterpret_cast<float*>(g.out)[at + e] = y[e];
+      }
+  }
+}
+FP4_D void load_addend8(const MxGemm& g, int64_t at, int64_t left, float (&a)[8]) {
+  if (left >= 8) {
+    const f32x4 u = *reinterpret_cast<const f32x4*>(g.addend + at), v = *reinterpret_cast<const f32x4*>(g.addend + at + 4);
+    a[0] = u.x; a[1] = u.y; a[2] = u.z; a[3] = u.w;
+    a[4] = v.x; a[5] = v.y; a[6] = v.z; a[7] = v.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = e < left ? g.addend[at + e] : 0.0f;
+  }
+}
+
+template <bool OUT_BF16>
+__global__ __launch_bounds__(BWAVES * 64) void mx_gemm_big_kernel(MxGemm g) {
+  __shared__ __attribute__((aligned(16))) uint8_t smem[BIG_SMEM];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave_p = wave & 1, wave_q = wave >> 1;
+  const int l32 = lane & 31, h = lane >> 5;
+  // each XCD a contiguous run of tiles, so that those that share rows meet in one L2
+  const int per_xcd = (g.count + 7) / 8;
+  const int xcd = (int)(blockIdx.x % 8), stride = (int)(gridDim.x / 8);
+  const int run_end = min(g.count, (xcd + 1) * per_xcd);
+  int lid = xcd * per_xcd + (int)(blockIdx.x / 8);
+  if (lid >= run_end) return;
+
+  const int64_t rowb = g.pitch / 2, rows_s = g.pitch / MX_BLOCK;
+  const int KT = (int)(g.pitch / 256), T = KT * g.nl * g.nr;   // steps of a pass (even), of all passes
+  int64_t P0 = 0, Q0 = 0;
+  __amdgpu_buffer_rsrc_t rsrcL, rsrcR, rsrcS;
+  uint32_t offL[BLD], offR[BLD], offS;
+  int ld_k = 0, ld_pass = 0, sc_k = 0;   // the step in its pass that is requested next, and the pair of steps whose scales are
+  auto planes = [&](int pass) {
+    rsrcL = rows_rsrc(g.L + (pass % g.nl) * g.planeL + P0 * rowb, min(g.P - P0, (int64_t)BT), rowb);
+    rsrcR = rows_rsrc(g.R + (pass / g.nl) * g.planeR + Q0 * rowb, min(g.Q - Q0, (int64_t)BT), rowb);
+  };
+  auto tile_scalars = [&](int id) {
+    int tp, tq;
+    tile_at(g, id, tp, tq);
+    P0 = (int64_t)tp * BT;
+    Q0 = (int64_t)tq * BT;
+    ld_k = ld_pass = sc_k = 0;
+    planes(0);
+    rsrcS = wave < 4 ? rows_rsrc(g.sL + P0 * rows_s, min(g.P - P0, (int64_t)BT), rows_s) : rows_rsrc(g.sR + Q0 * rows_s, min(g.Q - Q0, (int64_t)BT), rows_s);
+  };
+  // rebuilt where they are needed from a copy of the lane id that the optimizer cannot see through: kept across the epilogue they
+  // would cost registers there
+  auto tile_offsets = [&]() {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+#pragma unroll
+    for (int j = 0; j < BLD; ++j) {
+      const int row = 8 * (wave * BLD + j) + (ln >> 3);
+      const int chunk = (ln & 7) ^ ((row >> 1) & 7);
+      offL[j] = (uint32_t)((min(P0 + row, g.P - 1) - P0) * rowb + chunk * 16);   // rows past the edge re-read the last row
+      offR[j] = (uint32_t)((min(Q0 + row, g.Q - 1) - Q0) * rowb + chunk * 16);
+    }
+    const int row = (wave & 3) * 64 + ln;
+    offS = (uint32_t)(wave < 4 ? (min(P0 + row, g.P - 1) - P0) * rows_s : (min(Q0 + row, g.Q - 1) - Q0) * rows_s);
+  };
+  auto load_step = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < BLD; ++j) {
+      MX_TO_LDS(rsrcL, smem + buf * STAGE_BYTES + (wave * BLD + j) * 1024, 16, offL[j], ld_k * BKB);
+      MX_TO_LDS(rsrcR, smem + buf * STAGE_BYTES + OP_BYTES + (wave * BLD + j) * 1024, 16, offR[j], ld_k * BKB);
+    }
+    if (++ld_k == KT) {
+      ld_k = 0;
+      if (++ld_pass < g.nl * g.nr) planes(ld_pass);
+    }
+  };
+  auto load_scales = [&](int buf) {   // wave w: rows 64 w .. of L, then of Rt
+    MX_TO_LDS(rsrcS, smem + SC_BASE + buf * SC_BYTES + wave * 1024, 16, offS, sc_k * 16);
+    if (++sc_k == KT / 2) sc_k = 0;
+  };
+
+  // Fragments: lane (l32, h) takes chunk 4 h + slice of rows l32 + 32 j; the swizzle only depends on l32.
+  const int key = (l32 >> 1) & 7;
+  int frag_l[4], frag_r[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    frag_l[s] = (wave_p * 128 + l32) * BKB + ((4 * h + s) ^ key) * 16;
+    frag_r[s] = OP_BYTES + (wave_q * 64 + l32) * BKB + ((4 * h + s) ^ key) * 16;
+  }
+  const int scale_l = SC_BASE + (wave_p * 128 + l32) * 16 + h * 4, scale_r = SC_BASE + BT * 16 + (wave_q * 64 + l32) * 16 + h * 4;
+  u32x4 fl[2][PJ], fr[2][QI];
+  uint32_t sl[PJ], sr[QI], lessl = 0, lessr = 0;
+  auto read_frags = [&](int buf, int half) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int j = 0; j < QI; ++j) fr[s][j] = *reinterpret_cast<const u32x4*>(smem + buf * STAGE_BYTES + frag_r[2 * half + s] + j * 32 * BKB);
+#pragma unroll
+      for (int j = 0; j < PJ; ++j) fl[s][j] = *reinterpret_cast<const u32x4*>(smem + buf * STAGE_BYTES + frag_l[2 * half + s] + j * 32 * BKB);
+    }
+  };
+  auto read_scales = [&](int buf, int parity) {
+#pragma unroll
+    for (int j = 0; j < QI; ++j) sr[j] = *reinterpret_cast<const uint32_t*>(smem + buf * SC_BYTES + scale_r + parity * 8 + j * 512) - lessr;
+#pragma unroll
+    for (int j = 0; j < PJ; ++j) sl[j] = *reinterpret_cast<const uint32_t*>(smem + buf * SC_BYTES + scale_l + parity * 8 + j * 512) - lessl;
+  };
+  mx_f32x16 acc[QI][PJ];
+
+  tile_scalars(lid);
+  tile_offsets();
+  load_step(0);
+  load_scales(0);
+  while (true) {
+    const int64_t eP0 = P0, eQ0 = Q0;   // of this tile, for its epilogue
+    tile_offsets();
+#pragma unroll
+    for (int i = 0; i < QI; ++i)
+#pragma unroll
+      for (int j = 0; j < PJ; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    load_step(1);
+    load_scales(1);
+    {
+      constexpr int n = 2 * BLD + 1;   // all but what was just issued
+      __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | ((n >> 4) << 14));
+    }
+    __builtin_amdgcn_s_barrier();   // a bare one: the fence of __syncthreads() would wait for the second stage too
+    asm volatile("" ::: "memory");
+    lessl = lessr = 0;
+    read_scales(0, 0);
+    read_frags(0, 0);
+    int rd_k = 0, rd_pass = 0;   // of the step whose scales are held
+    const bool second_group = wave >= BWAVES / 2;
+    if (second_group) __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    for (int t = 0; t < T; t += 2) {
+      const int sbuf = (t >> 1) & 1;
+      static_for<2>([&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        static_for<2>([&](auto hc) {
+          constexpr int half = decltype(hc)::value;
+          __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+          for (int qi = 0; qi < QI; ++qi)
+#pragma unroll
+            for (int pj = 0; pj < PJ; ++pj) acc[qi][pj] = mx_mfma<2 * half>(fr[0][qi], fl[0][pj], acc[qi][pj], sr[qi], sl[pj]);
+#pragma unroll
+          for (int qi = 0; qi < QI; ++qi)
+#pragma unroll
+            for (int pj = 0; pj < PJ; ++pj) acc[qi][pj] = mx_mfma<2 * half + 1>(fr[1][qi], fl[1][pj], acc[qi][pj], sr[qi], sl[pj]);
+#pragma unroll
+          for (int qi = 0; qi < QI; ++qi) asm volatile("" : "+v"(acc[qi][0]), "+v"(acc[qi][1]), "+v"(acc[qi][2]), "+v"(acc[qi][3]));
+          __builtin_amdgcn_s_setprio(0);
+          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (half == 1) {   // the next step is first read in this memory phase: its loads have landed by the barrier before
+            if (!second_group) __builtin_amdgcn_s_waitcnt(0x0f70);
+          }
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (half == 0) {
+            read_frags(e, 1);
+            // its share of the next step has landed before the first group reads it, and these reads of a stage that the first group
+            // fills next are over
+            if (second_group) __builtin_amdgcn_s_waitcnt(0x0070);
+          } else {
+            if (++rd_k == KT) {
+              rd_k = 0;
+              ++rd_pass;
+              lessl = rd_pass % g.nl ? MX_EIGHTH : 0u;
+              lessr = rd_pass / g.nl ? MX_EIGHTH : 0u;
+            }
+            read_scales(e == 0 ? sbuf : sbuf ^ 1, e ^ 1);
+            read_frags(e ^ 1, 0);
+            if (t + e + 2 < T) load_step(e);
+            if constexpr (e == 1) {
+              if (t + 4 < T) load_scales(sbuf);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+        });
+      });
+    }
+    if (!second_group) __builtin_amdgcn_s_barrier();
+    __syncthreads();   // every wave is done with the stages
+
+    const int next = lid + stride;
+    const bool has_next = next < run_end;
+    if (has_next) {
+      tile_scalars(next);
+      tile_offsets();
+      load_step(0);
+      load_scales(0);
+    }
+
+    // Epilogue: 32 rows at a time through the wave's own LDS, so that they are written (and the addend is read) along rows.  Loads and
+    // stores count on one in-order counter, so the addend of all 32 rows is requested before the first of them is stored.
+    float* const park = reinterpret_cast<float*>(smem + STAGE_BYTES) + wave * 32 * EPI_LD;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int64_t q0 = eQ0 + wave_q * 64 + (ln & 7) * 8;
+    const int64_t left = g.Q - q0;
+    static_for<PJ>([&](auto pc) {
+      constexpr int pj = decltype(pc)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<4 * QI>([&](auto ic) {
+        constexpr int qi = decltype(ic)::value / 4, b = decltype(ic)::value % 4;
+        const mx_f32x16& c = acc[qi][pj];
+        *reinterpret_cast<f32x4*>(park + (ln & 31) * EPI_LD + qi * 32 + b * 8 + (ln >> 5) * 4) = f32x4{c[b * 4], c[b * 4 + 1], c[b * 4 + 2], c[b * 4 + 3]};
+      });
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const int64_t p0 = eP0 + wave_p * 128 + pj * 32 + (ln >> 3);
+      float a[4][8];
+      if (g.addend) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (p0 + i * 8 < g.P && left > 0) load_addend8(g, (p0 + i * 8) * g.ldo + q0, left, a[i]);
+          else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[i][e] = 0.0f;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a[i][e] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float* r = park + ((ln >> 3) + i * 8) * EPI_LD + (ln & 7) * 8;
+        const f32x4 u = *reinterpret_cast<const f32x4*>(r), v = *reinterpret_cast<const f32x4*>(r + 4);
+        const float y[8] = {u.x + a[i][0], u.y + a[i][1], u.z + a[i][2], u.w + a[i][3], v.x + a[i][4], v.y + a[i][5], v.z + a[i][6], v.w + a[i][7]};
+        if (p0 + i * 8 < g.P && left > 0) store8<OUT_BF16>(g, (p0 + i * 8) * g.ldo + q0, left, y);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    });
+    __syncthreads();   // the parked rows lie over stage 1, which the next tile fills first thing
+    if (!has_next) break;
+    lid = next;
+  }
+}
+
+template <bool OUT_BF16>
+int launch(MxGemm& g, hipStream_t s) {
+  const int64_t big = ((g.P + BT - 1) / BT) * ((g.Q + BT - 1) / BT);
+  if (g.pitch > 0 && big >= 64) {
+    const int n_cu = fp4_compute_units_of_current_device();
+    g.tiles_p = (int)((g.P + BT - 1) / BT);
+    g.tiles_q = (int)((g.Q + BT - 1) / BT);
+    g.first = 0;
+    g.count = (int)big;
+    const dim3 grid((unsigned)std::min((g.count + 7) / 8 * 8, n_cu / 8 * 8));
+    hipLaunchKernelGGL((mx_gemm_big_kernel<OUT_BF16>), grid, dim3(BWAVES * 64), 0, s, g);
+  } else {
+    const dim3 grid((unsigned)((g.P + 63) / 64), (unsigned)((g.Q + 63) / 64));
+    hipLaunchKernelGGL((mx_gemm_small_kernel<OUT_BF16>), grid, dim3(256), 0, s, g);
+  }
   FP4_CHECK_LAUNCH();
   return FP4_OK;
 }

@@ -49,6 +49,22 @@ def test_products(P, Q, Kc, bl, br):
 
 
 @pytest.mark.parametrize("bl,br", BITS)
+@pytest.mark.parametrize("P,Q,Kc", [(2050, 2056, 40), (1800, 3000, 520), (4100, 1032, 1100)])
+def test_outputs_of_many_tiles(P, Q, Kc, bl, br):
+    """Rows and columns past the last tile's edge, one step of the contraction and several, with an addend and without."""
+    l, vl = operand(P, Kc, bl, P + Kc)
+    r, vr = operand(Q, Kc, br, Q + Kc)
+    ref, tol = vl @ vr.T, bound(vl, vr, Kc)
+    close(b.mx_gemm(l, r, torch.bfloat16), ref, tol, bf16=True)
+    got = b.mx_gemm(l, r)
+    close(got, ref, tol)
+    add = torch.randn(P, Q, device="cuda") * float(np.abs(ref).mean())
+    host = add.double().cpu().numpy()
+    close(b.mx_gemm(l, r, addend=add, out=add), ref + host, tol + 2.0 ** -22 * np.abs(host))
+    assert torch.equal(b.mx_gemm(l, r), got)
+
+
+@pytest.mark.parametrize("bl,br", BITS)
 @pytest.mark.parametrize("P,Q,Kc", [(5, 24, 100), (200, 136, 700), (600, 520, 1100)])
 def test_addend_and_accumulation_and_rows_apart(P, Q, Kc, bl, br):
     l, vl = operand(P, Kc, bl, 11)
