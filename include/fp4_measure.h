@@ -30,6 +30,13 @@ int fp8_host_round_codes(const float* x_host, int64_t n, uint8_t* codes_host);
 int fp4_device_round_codes(const float* x, int64_t n, uint8_t* codes, void* stream);
 int fp4_device_round_sweep(unsigned long long* mismatches, void* stream);
 
+/* mx_gemm by one kind of tile: 16 (few tokens), 32 (waves share the contraction), 64, 128 or 256; 0: by the rule that mx_gemm follows.  A
+ * contraction of no length goes by the rule.
+ * mx_gemm_tile: what the rule says for [P x Q] over Kc on a device with that many compute units (host arithmetic, no GPU); with 256,
+ * *last_round (may be NULL) is the number of tiles of the last round that are cut into 128 x 128 ones. */
+int mx_gemm_by_tile(const fp4_mx* l, const fp4_mx* rt, const float* addend, void* out, fp4_dtype out_dt, int64_t ldo, int tile, void* stream);
+int mx_gemm_tile(int64_t P, int64_t Q, int64_t Kc, int bits_l, int bits_r, int compute_units, int* last_round);
+
 /* Output tiles the FP4 GEMM [P x Q], contraction Kc, is cut into on a device with that many compute units, by the rule its launches
  * follow (host arithmetic, no GPU): 32 (whose waves share a contraction), 64, 128 or 256 rows and columns.  With 256, *last_round is the number of tiles of the
  * last round that are cut into 128 x 128 ones and *stagger how much later than the one before each quarter of the workgroups

@@ -99,7 +99,9 @@ def lib() -> C.CDLL:
         L.mx_linear_bwd_dgrad.argtypes = [vp, i32, i64, i64, i64, i64, mx, vp, i64, vp, sz, vp]
         L.mx_linear_bwd_wgrad.argtypes = [vp, i32, i64, i64, i64, i64, mx, i32, i32, vp, i64, vp, sz, vp]
         L.mx_linear_bwd.argtypes = [vp, i32, i64, i64, i64, i64, mx, mx, i32, vp, i64, i32, vp, i64, vp, sz, vp]
-        for name in ("mx_quantize", "mx_dequantize", "mx_gemm", "mx_linear_fwd", "mx_linear_bwd_dgrad", "mx_linear_bwd_wgrad", "mx_linear_bwd"):
+        L.mx_gemm_by_tile.argtypes = [mx, mx, vp, vp, i32, i64, i32, vp]
+        L.mx_gemm_tile.argtypes = [i64, i64, i64, i32, i32, i32, vp]
+        for name in ("mx_gemm_by_tile", "mx_gemm_tile", "mx_quantize", "mx_dequantize", "mx_gemm", "mx_linear_fwd", "mx_linear_bwd_dgrad", "mx_linear_bwd_wgrad", "mx_linear_bwd"):
             getattr(L, name).restype = i32
         L.fp8_host_round_codes.argtypes = [vp, i64, vp]
         for name in ("fp8_quantize", "fp4_gemm_mixed", "fp4_linear_fwd_mixed", "fp8_host_round_codes"):
@@ -655,6 +657,22 @@ def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, a
             raise ValueError("addend and out must have the same leading dimension")
     _check(lib().mx_gemm(_mx_ref(l), _mx_ref(rt), _ptr(addend), _ptr(out), _dt(out), ldo, _stream()), "mx_gemm")
     return out
+
+
+def mx_gemm_by_tile(l: MxTensor, rt: MxTensor, tile: int, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """mx_gemm by one kind of tile (16, 32, 64, 128, 256), for tests and measuring; addend has the output's leading dimension."""
+    out = _out(None, (l.lines, rt.lines), out_dtype, l.codes, "out")
+    _check(lib().mx_gemm_by_tile(_mx_ref(l), _mx_ref(rt), _ptr(addend), _ptr(out), _dt(out), _ld(out, "out"), tile, _stream()), "mx_gemm_by_tile")
+    return out
+
+
+def mx_gemm_tile(P: int, Q: int, Kc: int, bits_l: int = 4, bits_r: int = 4, compute_units: int = 256) -> Tuple[int, int]:
+    """The tile that mx_gemm takes, and how many tiles of a last round are cut smaller (host arithmetic, no GPU)."""
+    last_round = C.c_int(0)
+    tile = lib().mx_gemm_tile(P, Q, Kc, bits_l, bits_r, compute_units, C.byref(last_round))
+    if tile < 0:
+        _check(tile, "mx_gemm_tile")
+    return tile, last_round.value
 
 
 def mx_checkpoint(M: int, K: int, bits: int = 8, device="cuda") -> MxTensor:

@@ -10,7 +10,10 @@ int mx_launch_quantize(const void* x, int bf16, int64_t rows, int64_t cols, int6
 int mx_launch_dequantize(const uint8_t* codes, const uint8_t* scales, int bits, int64_t lines, int64_t length, bool transposed, void* x, int bf16,
                          int64_t ld, hipStream_t s);
 int mx_launch_gemm(const uint8_t* L, const uint8_t* sL, int bits_l, const uint8_t* R, const uint8_t* sR, int bits_r, int64_t P, int64_t Q, int64_t Kc,
-                   const float* addend, void* out, int out_bf16, int64_t ldo, hipStream_t s);
+                   const float* addend, void* out, int out_bf16, int64_t ldo, int tile, hipStream_t s);
+int mx_launch_few(const uint8_t* L, const uint8_t* sL, const void* x, int x_bf16, int64_t ldx, int bits_l, const uint8_t* R, const uint8_t* sR, int bits_r,
+                  int64_t P, int64_t Q, int64_t Kc, const float* addend, void* out, int out_bf16, int64_t ldo, hipStream_t s);
+bool mx_few_fuses(int64_t M, int64_t K, int bits);
 
 namespace {
 
@@ -66,7 +69,7 @@ int quantize(const void* x, int dt, int64_t rows, int64_t cols, int64_t ld, cons
                             c ? c->codes : nullptr, c ? c->scales : nullptr, s);
 }
 int gemm(const fp4_mx& l, const fp4_mx& rt, const float* addend, void* out, int dt, int64_t ldo, hipStream_t s) {
-  return mx_launch_gemm(l.codes, l.scales, l.bits, rt.codes, rt.scales, rt.bits, l.lines, rt.lines, l.length, addend, out, dt == FP4_BF16, ldo, s);
+  return mx_launch_gemm(l.codes, l.scales, l.bits, rt.codes, rt.scales, rt.bits, l.lines, rt.lines, l.length, addend, out, dt == FP4_BF16, ldo, 0, s);
 }
 
 }  // namespace
@@ -102,7 +105,7 @@ extern "C" int mx_dequantize(const fp4_mx* t, int transposed, void* x, fp4_dtype
   return mx_launch_dequantize(t->codes, t->scales, t->bits, t->lines, t->length, transposed != 0, x, dt == FP4_BF16, ld, (hipStream_t)stream);
 }
 
-extern "C" int mx_gemm(const fp4_mx* l, const fp4_mx* rt, const float* addend, void* out, fp4_dtype out_dt, int64_t ldo, void* stream) {
+int mx_check_gemm(const fp4_mx* l, const fp4_mx* rt, const float* addend, const void* out, int out_dt, int64_t ldo) {
   if (!l || !rt) return FP4_ERR_NULL;
   if (l->length != rt->length || l->length < 0) return FP4_ERR_SHAPE;
   if (l->length > MAX_DIM) return FP4_ERR_LIMIT;
@@ -110,8 +113,12 @@ extern "C" int mx_gemm(const fp4_mx* l, const fp4_mx* rt, const float* addend, v
   if (!rc) rc = check_mx(l, l->lines, l->length);
   if (!rc) rc = check_mx(rt, rt->lines, rt->length);
   if (rc || l->lines == 0 || rt->lines == 0) return rc;
-  if (addend && !aligned16(addend)) return FP4_ERR_ARG;
-  return gemm(*l, *rt, addend, out, out_dt, ldo, (hipStream_t)stream);
+  return addend && !aligned16(addend) ? FP4_ERR_ARG : FP4_OK;
+}
+
+extern "C" int mx_gemm(const fp4_mx* l, const fp4_mx* rt, const float* addend, void* out, fp4_dtype out_dt, int64_t ldo, void* stream) {
+  const int rc = mx_check_gemm(l, rt, addend, out, out_dt, ldo);
+  return rc || l->lines == 0 || rt->lines == 0 ? rc : gemm(*l, *rt, addend, out, out_dt, ldo, (hipStream_t)stream);
 }
 
 extern "C" int mx_linear_fwd(const void* A, fp4_dtype dt, int64_t M, int64_t K, int64_t N, int64_t lda, int act_bits, const fp4_mx* W, void* Y,
@@ -125,6 +132,8 @@ extern "C" int mx_linear_fwd(const void* A, fp4_dtype dt, int64_t M, int64_t K, 
   if (M == 0) return FP4_OK;
   if (!workspace || workspace_bytes < mx_workspace_bytes(FP4_OP_MX_FWD, M, K, N)) return FP4_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
+  if (!saved && K > 0 && N > 0 && mx_few_fuses(M, K, act_bits))
+    return mx_launch_few(nullptr, nullptr, A, dt == FP4_BF16, lda, act_bits, W->codes, W->scales, W->bits, M, N, K, nullptr, Y, dt == FP4_BF16, ldy, s);
   Carve c(aligned_workspace(workspace));
   const fp4_mx a = c.take(M, K, act_bits);
   if (K > 0 && (rc = quantize(A, dt, M, K, lda, N > 0 ? &a : nullptr, saved, s))) return rc;

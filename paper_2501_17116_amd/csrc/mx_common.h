@@ -89,6 +89,76 @@ FP4_D void mx_encode8(const u32x4& w, float s, uint32_t& h, uint32_t& l) {   // 
   mx_pair<BITS, 2>(w.z, s, h, l);
   mx_pair<BITS, 3>(w.w, s, h, l);
 }
+template <int BITS>
+FP4_D void mx_encode8(const u32x4& a, const u32x4& b, float s, uint32_t& h, uint32_t& l) {   // eight fp32
+  const float v[8] = {u2f(a.x), u2f(a.y), u2f(a.z), u2f(a.w), u2f(b.x), u2f(b.y), u2f(b.z), u2f(b.w)};
+  mx_encode8<BITS>(v, s, h, l);
+}
 // The scale as the converts want it.  (For byte 255 the codes do not matter.)
 FP4_D float mx_scale_f32(uint32_t byte) { return u2f(byte << 23); }
+// max over a group of four lanes
+FP4_D uint32_t mx_quad_max(uint32_t v) {
+  uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true);   // lane ^ 1
+  v = v > o ? v : o;
+  o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true);            // lane ^ 2
+  return v > o ? v : o;
+}
+// A 16-byte piece of a row: eight bf16 or four fp32 from column c on; zeros behind the row's end and in rows that are not there.
+template <class T>
+FP4_D u32x4 mx_load_piece(const void* x, int64_t row, int64_t rows, int64_t cols, int64_t ld, int64_t c) {
+  constexpr int E = sizeof(T);
+  constexpr int N = 16 / E;
+  u32x4 w = {0u, 0u, 0u, 0u};
+  if (row < rows) {
+    const T* p = reinterpret_cast<const T*>(x) + row * ld + c;
+    if (c + N <= cols) {
+      w = *reinterpret_cast<const u32x4*>(p);
+    } else {
+      union { T t[N]; u32x4 v; } u;
+      u.v = w;
+      for (int e = 0; e < N; ++e)
+        if (c + e < cols) u.t[e] = p[e];
+      w = u.v;
+    }
+  }
+  return w;
+}
+
+FP4_D u32x4 mx_magnitudes_bf16(const u32x4& w) { return u32x4{w.x & 0x7fff7fffu, w.y & 0x7fff7fffu, w.z & 0x7fff7fffu, w.w & 0x7fff7fffu}; }
+FP4_D uint32_t mx_amax_bf16(const u32x4& w) {   // bits of the largest magnitude of eight bf16, as fp32
+  const u32x4 m = mx_magnitudes_bf16(w);
+  const uint32_t a = mx_pk_max_u16(mx_pk_max_u16(m.x, m.y), mx_pk_max_u16(m.z, m.w));
+  const uint32_t lo = a & 0xffffu, hi = a >> 16;
+  return (lo > hi ? lo : hi) << 16;
+}
+FP4_D uint32_t mx_amax_f32(const u32x4& w) {
+  const uint32_t a = w.x & 0x7fffffffu, b = w.y & 0x7fffffffu, c = w.z & 0x7fffffffu, d = w.w & 0x7fffffffu;
+  const uint32_t ab = a > b ? a : b, cd = c > d ? c : d;
+  return ab > cd ? ab : cd;
+}
+
+FP4_D uint32_t mx_pack_bf16x2(float a, float b) {
+  mx_f32x2 f = {a, b};
+  return mx_bits(__builtin_convertvector(f, mx_bf16x2));
+}
+// Four columns of a row, `left` of them there, with the addend where there is one.
+template <bool OUT_BF16>
+FP4_D void mx_store4(void* out, const float* addend, int64_t at, int64_t left, float (&y)[4]) {
+  if (left >= 4) {
+    if (addend) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(addend + at);
+      y[0] += a.x; y[1] += a.y; y[2] += a.z; y[3] += a.w;
+    }
+    if constexpr (OUT_BF16) *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + at) = u32x2{mx_pack_bf16x2(y[0], y[1]), mx_pack_bf16x2(y[2], y[3])};
+    else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + at) = f32x4{y[0], y[1], y[2], y[3]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) {
+        const float v = addend ? y[e] + addend[at + e] : y[e];
+        if constexpr (OUT_BF16) reinterpret_cast<uint16_t*>(out)[at + e] = (uint16_t)mx_pack_bf16x2(v, v);
+        else reinterpret_cast<float*>(out)[at + e] = v;
+      }
+  }
+}
 #endif  // __HIPCC__

@@ -11,6 +11,8 @@
 // l32, sixteen bytes, and brings their scale, in the byte of its scale register that the instruction names.  A scale byte of 255 makes
 // the row NaN, also over zero codes.
 #include "mx_common.h"
+#include "mx_tiling.h"
+#include "fp4_measure.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -20,6 +22,9 @@ typedef int mx_i32x8 __attribute__((ext_vector_type(8)));
 typedef float mx_f32x16 __attribute__((ext_vector_type(16)));
 
 int fp4_compute_units_of_current_device();
+int mx_check_gemm(const fp4_mx* l, const fp4_mx* rt, const float* addend, const void* out, int out_dt, int64_t ldo);
+int mx_launch_few(const uint8_t* L, const uint8_t* sL, const void* x, int x_bf16, int64_t ldx, int bits_l, const uint8_t* R, const uint8_t* sR, int bits_r,
+                  int64_t P, int64_t Q, int64_t Kc, const float* addend, void* out, int out_bf16, int64_t ldo, hipStream_t s);
 
 namespace {
 
@@ -56,33 +61,6 @@ FP4_D mx_f32x16 mx_mfma(const u32x4& r, const u32x4& l, const mx_f32x16& c, uint
   else return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 3, (int)sr, 3, (int)sl);
 }
 
-FP4_D uint32_t mx_pack_bf16x2(float a, float b) {
-  mx_f32x2 f = {a, b};
-  return mx_bits(__builtin_convertvector(f, mx_bf16x2));
-}
-
-// Four columns of a row; the row may end among them.
-template <bool OUT_BF16>
-FP4_D void mx_store4(const MxGemm& g, int64_t p, int64_t q, float (&y)[4]) {
-  const int64_t at = p * g.ldo + q;
-  if (q + 4 <= g.Q) {
-    if (g.addend) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(g.addend + at);
-      y[0] += a.x; y[1] += a.y; y[2] += a.z; y[3] += a.w;
-    }
-    if constexpr (OUT_BF16) *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(g.out) + at) = u32x2{mx_pack_bf16x2(y[0], y[1]), mx_pack_bf16x2(y[2], y[3])};
-    else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(g.out) + at) = f32x4{y[0], y[1], y[2], y[3]};
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (q + e < g.Q) {
-        const float v = g.addend ? y[e] + g.addend[at + e] : y[e];
-        if constexpr (OUT_BF16) reinterpret_cast<uint16_t*>(g.out)[at + e] = (uint16_t)mx_pack_bf16x2(v, v);
-        else reinterpret_cast<float*>(g.out)[at + e] = v;
-      }
-  }
-}
-
 // 64 x 64 outputs a workgroup, 32 x 32 a wave, operands straight from memory to the matrix core's registers, 512 codes of the contraction a
 // step.  Rows past the matrix's edge repeat its last one and are not stored.
 template <bool OUT_BF16>
@@ -116,7 +94,7 @@ __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
   for (int b = 0; b < 4; ++b) {
     const int64_t qc = Q0 + b * 8 + h * 4;
     float y[4] = {acc[b * 4], acc[b * 4 + 1], acc[b * 4 + 2], acc[b * 4 + 3]};
-    if (qc < g.Q) mx_store4<OUT_BF16>(g, P0 + l32, qc, y);
+    if (qc < g.Q) mx_store4<OUT_BF16>(g.out, g.addend, (P0 + l32) * g.ldo + qc, g.Q - qc, y);
   }
 }
 
@@ -421,17 +399,283 @@ __global__ __launch_bounds__(BWAVES * 64) void mx_gemm_big_kernel(MxGemm g) {
   }
 }
 
+// What is left of a T x T tile whose sums lie in LDS, rows T + 4 floats apart: the addend, the rounding, stores along rows.  A batch of rows'
+// addends is requested before the first of them is stored.
+template <int T, int THREADS, bool OUT_BF16>
+FP4_D void finish_tile(const MxGemm& g, const float* tile, int64_t P0, int64_t Q0) {
+  constexpr int UPR = T / 8, RPP = THREADS / UPR, NP = T / RPP, B = NP < 4 ? NP : 4;   // 8-column units a row, rows a pass, passes, passes a batch
+  const int tid = threadIdx.x, ql = (tid % UPR) * 8;
+  const int64_t q0 = Q0 + ql, left = g.Q - q0;
+  if (left <= 0) return;
+#pragma unroll 1
+  for (int b = 0; b < NP; b += B) {
+    float a[B][8];
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      const int64_t p = P0 + tid / UPR + (b + i) * RPP;
+      if (g.addend && p < g.P) load_addend8(g, p * g.ldo + q0, left, a[i]);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[i][e] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      const int pl = tid / UPR + (b + i) * RPP;
+      const f32x4 u = *reinterpret_cast<const f32x4*>(&tile[pl * (T + 4) + ql]), v = *reinterpret_cast<const f32x4*>(&tile[pl * (T + 4) + ql + 4]);
+      const float y[8] = {u.x + a[i][0], u.y + a[i][1], u.z + a[i][2], u.w + a[i][3], v.x + a[i][4], v.y + a[i][5], v.z + a[i][6], v.w + a[i][7]};
+      if (P0 + pl < g.P) store8<OUT_BF16>(g, (P0 + pl) * g.ldo + q0, left, y);
+    }
+  }
+}
+
+// ---- 128 x 128 ------------------------------------------------------------------------------------------------------------------
+// For outputs with too few 256 x 256 tiles: a workgroup of four waves, 64 x 64 each.  A step's products take a fifth of a microsecond, less
+// than a load, so steps go through a ring of four LDS stages with three on their way; a stage's scales lie behind its codes as the lanes
+// want them, one word each.
+constexpr int MT = 128, M_RING = 4;
+constexpr int M_OP = MT * BKB, M_STAGE = 2 * M_OP + 8 * 256, M_LD = MT * 8 / 256, M_LOADS = 2 * M_LD + 2;
+constexpr uint32_t PAST_THE_END = 0xf0000000u;   // behind any descriptor: arrives as zeros
+
 template <bool OUT_BF16>
-int launch(MxGemm& g, hipStream_t s) {
-  const int64_t big = ((g.P + BT - 1) / BT) * ((g.Q + BT - 1) / BT);
-  if (g.pitch > 0 && big >= 64) {
-    const int n_cu = fp4_compute_units_of_current_device();
-    g.tiles_p = (int)((g.P + BT - 1) / BT);
-    g.tiles_q = (int)((g.Q + BT - 1) / BT);
-    g.first = 0;
-    g.count = (int)big;
-    const dim3 grid((unsigned)std::min((g.count + 7) / 8 * 8, n_cu / 8 * 8));
-    hipLaunchKernelGGL((mx_gemm_big_kernel<OUT_BF16>), grid, dim3(BWAVES * 64), 0, s, g);
+__global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
+  static_assert(M_RING * M_STAGE >= MT * (MT + 4) * 4 && M_RING * M_STAGE <= 160 * 1024, "the sums lie over the ring");
+  __shared__ __attribute__((aligned(16))) uint8_t smem[M_RING * M_STAGE];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, h = lane >> 5;
+  const int wp = (wave & 1) * 64, wq = (wave >> 1) * 64;
+  // each XCD a contiguous run of tiles: of the whole output, or (first > 0) the quarters of the 256 x 256 tiles from `first` on
+  const int per_xcd = (g.count + 7) / 8, id = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
+  if ((int)(blockIdx.x / 8) >= per_xcd || id >= g.count) return;
+  int tp, tq;
+  if (g.first > 0) {
+    tile_at(g, g.first + (id >> 2), tp, tq);
+    tp = 2 * tp + (id & 1);
+    tq = 2 * tq + (id >> 1 & 1);
+  } else {
+    tile_at(g, id, tp, tq);
+  }
+  const int64_t P0 = (int64_t)tp * MT, Q0 = (int64_t)tq * MT;
+  if (P0 >= g.P || Q0 >= g.Q) return;   // a quarter behind the edge
+  const int64_t rowb = g.pitch / 2, rows_s = g.pitch / MX_BLOCK, np = min(g.P - P0, (int64_t)MT), nq = min(g.Q - Q0, (int64_t)MT);
+  const int KT = (int)(g.pitch / 256), T = KT * g.nl * g.nr;
+  __amdgpu_buffer_rsrc_t rsrcL, rsrcR;
+  auto planes = [&](int pass) {
+    rsrcL = rows_rsrc(g.L + (pass % g.nl) * g.planeL + P0 * rowb, np, rowb);
+    rsrcR = rows_rsrc(g.R + (pass / g.nl) * g.planeR + Q0 * rowb, nq, rowb);
+  };
+  planes(0);
+  const __amdgpu_buffer_rsrc_t rsrcS = wave < 2 ? rows_rsrc(g.sL + P0 * rows_s, np, rows_s) : rows_rsrc(g.sR + Q0 * rows_s, nq, rows_s);
+  uint32_t offL[M_LD], offR[M_LD], offS[2];
+#pragma unroll
+  for (int j = 0; j < M_LD; ++j) {
+    const int row = 8 * (wave * M_LD + j) + (lane >> 3), at = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    offL[j] = (uint32_t)(min((int64_t)row, np - 1) * rowb + at);   // rows past the edge re-read the last row
+    offR[j] = (uint32_t)(min((int64_t)row, nq - 1) * rowb + at);
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j)   // blocks of 32 rows 0 .. 3 of L, 4 .. 7 of Rt
+    offS[j] = (uint32_t)(min((int64_t)((2 * wave + j) % 4 * 32 + l32), (wave < 2 ? np : nq) - 1) * rows_s + h * 4);
+  int ld_t = 0, ld_k = 0, ld_pass = 0;
+  auto request = [&]() {   // the next step; behind the last one zeros
+    uint8_t* const st = smem + (ld_t & (M_RING - 1)) * M_STAGE;
+    const bool in = ld_t < T;
+#pragma unroll
+    for (int j = 0; j < M_LD; ++j) {
+      MX_TO_LDS(rsrcL, st + (wave * M_LD + j) * 1024, 16, in ? offL[j] : PAST_THE_END, ld_k * BKB);
+      MX_TO_LDS(rsrcR, st + M_OP + (wave * M_LD + j) * 1024, 16, in ? offR[j] : PAST_THE_END, ld_k * BKB);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) MX_TO_LDS(rsrcS, st + 2 * M_OP + (2 * wave + j) * 256, 4, in ? offS[j] : PAST_THE_END, ld_k * 8);
+    ++ld_t;
+    if (++ld_k == KT) {
+      ld_k = 0;
+      if (++ld_pass < g.nl * g.nr) planes(ld_pass);
+    }
+  };
+  const int key = (l32 >> 1) & 7;
+  mx_f32x16 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[i >> 1][i & 1][v] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < M_RING - 1; ++i) request();
+  uint32_t lessl = 0, lessr = 0;
+  int rd_k = 0, rd_pass = 0;
+  for (int t = 0; t < T; ++t) {
+    asm volatile("" ::: "memory");
+    // this wave's share of step t is there, and it is done reading step t - 1; behind the barrier that holds for all
+    constexpr int left = (M_RING - 2) * M_LOADS;
+    __builtin_amdgcn_s_waitcnt(0x0070 | (left & 15) | ((left >> 4) << 14));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    request();
+    const uint8_t* const st = smem + (t & (M_RING - 1)) * M_STAGE;
+    const uint8_t *const sL = st + (wp + l32) * BKB, *const sR = st + M_OP + (wq + l32) * BKB;
+    uint32_t sl[2], sr[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      sl[j] = *reinterpret_cast<const uint32_t*>(st + 2 * M_OP + (wp / 32 + j) * 256 + lane * 4) - lessl;
+      sr[j] = *reinterpret_cast<const uint32_t*>(st + 2 * M_OP + (4 + wq / 32 + j) * 256 + lane * 4) - lessr;
+    }
+    u32x4 fl[4][2], fr[4][2];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int slot = ((4 * h + s) ^ key) * 16;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        fr[s][j] = *reinterpret_cast<const u32x4*>(sR + slot + j * 32 * BKB);
+        fl[s][j] = *reinterpret_cast<const u32x4*>(sL + slot + j * 32 * BKB);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);   // all requested before the first product
+    static_for<4>([&](auto sc) {
+      constexpr int s = decltype(sc)::value;
+#pragma unroll
+      for (int qi = 0; qi < 2; ++qi)
+#pragma unroll
+        for (int pj = 0; pj < 2; ++pj) acc[qi][pj] = mx_mfma<s>(fr[s][qi], fl[s][pj], acc[qi][pj], sr[qi], sl[pj]);
+    });
+    if (++rd_k == KT) {
+      rd_k = 0;
+      ++rd_pass;
+      lessl = rd_pass % g.nl ? MX_EIGHTH : 0u;
+      lessr = rd_pass / g.nl ? MX_EIGHTH : 0u;
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);   // no load may land over the sums
+  __syncthreads();
+  float* const tile = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int pj = 0; pj < 2; ++pj)
+#pragma unroll
+    for (int qi = 0; qi < 2; ++qi)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const mx_f32x16& c = acc[qi][pj];
+        *reinterpret_cast<f32x4*>(&tile[(wp + pj * 32 + l32) * (MT + 4) + wq + qi * 32 + b * 8 + h * 4]) = f32x4{c[b * 4], c[b * 4 + 1], c[b * 4 + 2], c[b * 4 + 3]};
+      }
+  __syncthreads();
+  finish_tile<MT, 256, OUT_BF16>(g, tile, P0, Q0);
+}
+
+// ---- 32 x 32, the contraction shared ---------------------------------------------------------------------------------------------
+// For the smallest outputs: a workgroup of four waves takes 32 x 32, and each wave every fourth step of the contraction through a ring of its
+// own, without a barrier before the end.  Such a call is one round trip to memory after another, so there are as many workgroups as can be
+// and each wave has RING steps under way.  The waves' sums are added in their order.
+constexpr int ST = 32, S_OP = ST * BKB, S_STEP = 2 * S_OP + 512, S_LD = ST / 8;
+
+template <bool OUT_BF16, int RING>
+__global__ __launch_bounds__(256) void mx_gemm_split_kernel(MxGemm g) {
+  constexpr int LD = ST + 4, WAVES = 4;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[WAVES * RING * S_STEP];
+  static_assert(RING * S_STEP >= ST * LD * 4, "a wave's sums lie over its ring");
+  auto part = [&](int w) { return reinterpret_cast<float*>(smem + w * (RING * S_STEP)); };
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, h = lane >> 5;
+  // each XCD a contiguous run of tiles, column by column: the rows of Rt are read by one of them
+  const int per_xcd = (g.count + 7) / 8, id = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
+  if ((int)(blockIdx.x / 8) >= per_xcd || id >= g.count) return;
+  const int64_t P0 = (int64_t)(id % g.tiles_p) * ST, Q0 = (int64_t)(id / g.tiles_p) * ST;
+  const int64_t rowb = g.pitch / 2, rows_s = g.pitch / MX_BLOCK, np = min(g.P - P0, (int64_t)ST), nq = min(g.Q - Q0, (int64_t)ST);
+  const int KT = (int)(g.pitch / 256), T = KT * g.nl * g.nr, steps = (T - wave + WAVES - 1) / WAVES;   // of this wave
+  const __amdgpu_buffer_rsrc_t rsrcSL = rows_rsrc(g.sL + P0 * rows_s, np, rows_s), rsrcSR = rows_rsrc(g.sR + Q0 * rows_s, nq, rows_s);
+  uint32_t offL[S_LD], offR[S_LD];
+#pragma unroll
+  for (int j = 0; j < S_LD; ++j) {
+    const int row = 8 * j + (lane >> 3), at = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    offL[j] = (uint32_t)(min((int64_t)row, np - 1) * rowb + at);   // rows past the edge re-read the last row
+    offR[j] = (uint32_t)(min((int64_t)row, nq - 1) * rowb + at);
+  }
+  const uint32_t offSL = (uint32_t)(min((int64_t)l32, np - 1) * rows_s + h * 4), offSR = (uint32_t)(min((int64_t)l32, nq - 1) * rows_s + h * 4);
+  uint8_t* const mine = smem + wave * (RING * S_STEP);
+  auto request = [&](int i) {   // steps past the last arrive as zeros
+    uint8_t* const st = mine + (i % RING) * S_STEP;
+    const bool in = i < steps;
+    const int t = in ? wave + WAVES * i : 0, pass = t / KT, k = t - pass * KT;
+    const __amdgpu_buffer_rsrc_t rsrcL = rows_rsrc(g.L + (pass % g.nl) * g.planeL + P0 * rowb, np, rowb);
+    const __amdgpu_buffer_rsrc_t rsrcR = rows_rsrc(g.R + (pass / g.nl) * g.planeR + Q0 * rowb, nq, rowb);
+#pragma unroll
+    for (int j = 0; j < S_LD; ++j) {
+      MX_TO_LDS(rsrcL, st + j * 1024, 16, in ? offL[j] : PAST_THE_END, k * BKB);
+      MX_TO_LDS(rsrcR, st + S_OP + j * 1024, 16, in ? offR[j] : PAST_THE_END, k * BKB);
+    }
+    MX_TO_LDS(rsrcSL, st + 2 * S_OP, 4, in ? offSL : PAST_THE_END, k * 8);
+    MX_TO_LDS(rsrcSR, st + 2 * S_OP + 256, 4, in ? offSR : PAST_THE_END, k * 8);
+  };
+  const int key = (l32 >> 1) & 7;
+  mx_f32x16 acc;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < RING; ++i) request(i);
+  for (int i = 0; i < steps; ++i) {
+    asm volatile("" ::: "memory");
+    constexpr int left = (RING - 1) * (2 * S_LD + 2);   // the steps behind this one
+    __builtin_amdgcn_s_waitcnt(0x0070 | (left & 15) | ((left >> 4) << 14));
+    asm volatile("" ::: "memory");
+    const uint8_t* const st = mine + (i % RING) * S_STEP;
+    const int pass = (wave + WAVES * i) / KT;
+    const uint32_t sl = *reinterpret_cast<const uint32_t*>(st + 2 * S_OP + lane * 4) - (pass % g.nl ? MX_EIGHTH : 0u);
+    const uint32_t sr = *reinterpret_cast<const uint32_t*>(st + 2 * S_OP + 256 + lane * 4) - (pass / g.nl ? MX_EIGHTH : 0u);
+    u32x4 fl[4], fr[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int slot = l32 * BKB + ((4 * h + s) ^ key) * 16;
+      fr[s] = *reinterpret_cast<const u32x4*>(st + S_OP + slot);
+      fl[s] = *reinterpret_cast<const u32x4*>(st + slot);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read: the slot may be filled again
+    request(i + RING);
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<4>([&](auto sc) {
+      constexpr int s = decltype(sc)::value;
+      acc = mx_mfma<s>(fr[s], fl[s], acc, sr, sl);
+    });
+  }
+  __builtin_amdgcn_s_waitcnt(0);   // no load may land over the sums
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+    *reinterpret_cast<f32x4*>(&part(wave)[l32 * LD + b * 8 + h * 4]) = f32x4{acc[b * 4], acc[b * 4 + 1], acc[b * 4 + 2], acc[b * 4 + 3]};
+  __syncthreads();
+  const int row = tid >> 3, col = (tid & 7) * 4;   // four columns of a row a thread
+  f32x4 sum = *reinterpret_cast<const f32x4*>(&part(0)[row * LD + col]);
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) sum += *reinterpret_cast<const f32x4*>(&part(w)[row * LD + col]);
+  float y[4] = {sum.x, sum.y, sum.z, sum.w};
+  if (P0 + row < g.P && Q0 + col < g.Q) mx_store4<OUT_BF16>(g.out, g.addend, (P0 + row) * g.ldo + Q0 + col, g.Q - Q0 - col, y);
+}
+
+void set_tiles(MxGemm& g, int tile) {
+  g.tiles_p = (int)((g.P + tile - 1) / tile);
+  g.tiles_q = (int)((g.Q + tile - 1) / tile);
+  g.first = 0;
+  g.count = g.tiles_p * g.tiles_q;
+}
+
+template <bool OUT_BF16>
+int launch(MxGemm& g, MxTiling t, int n_cu, hipStream_t s) {
+  const auto dealt = [](int count) { return dim3((unsigned)((count + 7) / 8 * 8)); };   // a run of tiles for each XCD
+  if (t.tile == 256) {
+    set_tiles(g, 256);
+    MxGemm m = g;
+    g.count -= t.rest;
+    hipLaunchKernelGGL((mx_gemm_big_kernel<OUT_BF16>), dim3((unsigned)std::min((g.count + 7) / 8 * 8, n_cu / 8 * 8)), dim3(BWAVES * 64), 0, s, g);
+    if (t.rest) {
+      m.first = g.count;
+      m.count = 4 * t.rest;
+      hipLaunchKernelGGL((mx_gemm_mid_kernel<OUT_BF16>), dealt(m.count), dim3(256), 0, s, m);
+    }
+  } else if (t.tile == 128) {
+    set_tiles(g, 128);
+    hipLaunchKernelGGL((mx_gemm_mid_kernel<OUT_BF16>), dealt(g.count), dim3(256), 0, s, g);
+  } else if (t.tile == 32) {
+    set_tiles(g, 32);
+    if (g.count <= n_cu) hipLaunchKernelGGL((mx_gemm_split_kernel<OUT_BF16, 4>), dealt(g.count), dim3(256), 0, s, g);
+    else hipLaunchKernelGGL((mx_gemm_split_kernel<OUT_BF16, 2>), dealt(g.count), dim3(256), 0, s, g);
   } else {
     const dim3 grid((unsigned)((g.P + 63) / 64), (unsigned)((g.Q + 63) / 64));
     hipLaunchKernelGGL((mx_gemm_small_kernel<OUT_BF16>), grid, dim3(256), 0, s, g);
@@ -442,9 +686,13 @@ int launch(MxGemm& g, hipStream_t s) {
 
 }  // namespace
 
-// P and Q are at least 1; Kc may be 0.
+// P and Q are at least 1; Kc may be 0.  tile: one of MxTiling's, or 0 for the rule's.
 int mx_launch_gemm(const uint8_t* L, const uint8_t* sL, int bits_l, const uint8_t* R, const uint8_t* sR, int bits_r, int64_t P, int64_t Q, int64_t Kc,
-                   const float* addend, void* out, int out_bf16, int64_t ldo, hipStream_t s) {
+                   const float* addend, void* out, int out_bf16, int64_t ldo, int tile, hipStream_t s) {
+  const int n_cu = fp4_compute_units_of_current_device();
+  MxTiling t = mx_gemm_tiling(P, Q, Kc, bits_l, bits_r, n_cu);
+  if (tile) t = {tile, 0};
+  if (t.tile == 16) return mx_launch_few(L, sL, nullptr, 0, 0, bits_l, R, sR, bits_r, P, Q, Kc, addend, out, out_bf16, ldo, s);
   MxGemm g;
   g.L = L; g.R = R; g.sL = sL; g.sR = sR;
   g.addend = addend;
@@ -455,5 +703,21 @@ int mx_launch_gemm(const uint8_t* L, const uint8_t* sL, int bits_l, const uint8_
   g.planeR = Q * (g.pitch / 2);
   g.nl = bits_l / 4;
   g.nr = bits_r / 4;
-  return out_bf16 ? launch<true>(g, s) : launch<false>(g, s);
+  return out_bf16 ? launch<true>(g, t, n_cu, s) : launch<false>(g, t, n_cu, s);
+}
+
+// For measuring and for tests: the product by one kind of tile (16, 32, 64, 128 or 256), or by the rule's (0).
+extern "C" int mx_gemm_by_tile(const fp4_mx* l, const fp4_mx* rt, const float* addend, void* out, fp4_dtype out_dt, int64_t ldo, int tile, void* stream) {
+  if (tile != 0 && tile != 16 && tile != 32 && tile != 64 && tile != 128 && tile != 256) return FP4_ERR_ARG;
+  const int rc = mx_check_gemm(l, rt, addend, out, out_dt, ldo);
+  if (rc || l->lines == 0 || rt->lines == 0) return rc;
+  return mx_launch_gemm(l->codes, l->scales, l->bits, rt->codes, rt->scales, rt->bits, l->lines, rt->lines, l->length, addend, out, out_dt == FP4_BF16, ldo,
+                        l->length == 0 ? 0 : tile, (hipStream_t)stream);
+}
+
+extern "C" int mx_gemm_tile(int64_t P, int64_t Q, int64_t Kc, int bits_l, int bits_r, int compute_units, int* last_round) {
+  if (P <= 0 || Q <= 0 || Kc < 0 || compute_units < 8) return FP4_ERR_SHAPE;
+  const MxTiling t = mx_gemm_tiling(P, Q, Kc, bits_l, bits_r, compute_units);
+  if (last_round) *last_round = t.rest;
+  return t.tile;
 }

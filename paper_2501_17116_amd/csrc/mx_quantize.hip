@@ -21,48 +21,8 @@ struct QuantArgs {
   uint8_t *row_codes, *row_scales, *col_codes, *col_scales;
 };
 
-// max with a lane of the same group of four / eight
-FP4_D uint32_t quad_max(uint32_t v) {
-  uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true);   // lane ^ 1
-  v = v > o ? v : o;
-  o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true);            // lane ^ 2
-  return v > o ? v : o;
-}
+// of the other four lanes of eight
 FP4_D uint32_t other_quad(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true); }   // mirrored in eight lanes
-
-// A 16-byte piece of a row: eight bf16 or four fp32 from column c on; zeros behind the row's end and in rows that are not there.
-template <class T>
-FP4_D u32x4 load_piece(const void* x, int64_t row, int64_t rows, int64_t cols, int64_t ld, int64_t c) {
-  constexpr int E = sizeof(T);
-  constexpr int N = 16 / E;
-  u32x4 w = {0u, 0u, 0u, 0u};
-  if (row < rows) {
-    const T* p = reinterpret_cast<const T*>(x) + row * ld + c;
-    if (c + N <= cols) {
-      w = *reinterpret_cast<const u32x4*>(p);
-    } else {
-      union { T t[N]; u32x4 v; } u;
-      u.v = w;
-      for (int e = 0; e < N; ++e)
-        if (c + e < cols) u.t[e] = p[e];
-      w = u.v;
-    }
-  }
-  return w;
-}
-
-FP4_D u32x4 magnitudes_bf16(const u32x4& w) { return u32x4{w.x & 0x7fff7fffu, w.y & 0x7fff7fffu, w.z & 0x7fff7fffu, w.w & 0x7fff7fffu}; }
-FP4_D uint32_t amax_bf16(const u32x4& w) {   // bits of the largest magnitude of eight bf16, as fp32
-  const u32x4 m = magnitudes_bf16(w);
-  const uint32_t a = mx_pk_max_u16(mx_pk_max_u16(m.x, m.y), mx_pk_max_u16(m.z, m.w));
-  const uint32_t lo = a & 0xffffu, hi = a >> 16;
-  return (lo > hi ? lo : hi) << 16;
-}
-FP4_D uint32_t amax_f32(const u32x4& w) {
-  const uint32_t a = w.x & 0x7fffffffu, b = w.y & 0x7fffffffu, c = w.z & 0x7fffffffu, d = w.w & 0x7fffffffu;
-  const uint32_t ab = a > b ? a : b, cd = c > d ? c : d;
-  return ab > cd ? ab : cd;
-}
 
 // ---- rows --------------------------------------------------------------------------------------------------------------------
 // A wave takes 512 elements of a row at a time (a unit of the pitch), ROWS_U of them from consecutive units.
@@ -82,26 +42,23 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units
     seg[i] = (int)((u0 + i) - row[i] * per_row);
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      w[i][p] = load_piece<T>(a.x, u0 + i < units ? row[i] : a.rows, a.rows, a.cols, a.ld, (int64_t)seg[i] * MX_PITCH + lane * 8 + p * 4);
+      w[i][p] = mx_load_piece<T>(a.x, u0 + i < units ? row[i] : a.rows, a.rows, a.cols, a.ld, (int64_t)seg[i] * MX_PITCH + lane * 8 + p * 4);
   }
 #pragma unroll
   for (int i = 0; i < ROWS_U; ++i) {
     if (u0 + i >= units) break;
     uint32_t top;
-    if constexpr (P == 1) top = amax_bf16(w[i][0]);
+    if constexpr (P == 1) top = mx_amax_bf16(w[i][0]);
     else {
-      const uint32_t t0 = amax_f32(w[i][0]), t1 = amax_f32(w[i][P - 1]);
+      const uint32_t t0 = mx_amax_f32(w[i][0]), t1 = mx_amax_f32(w[i][P - 1]);
       top = t0 > t1 ? t0 : t1;
     }
-    const uint32_t byte = mx_scale_byte<BITS>(quad_max(top));
+    const uint32_t byte = mx_scale_byte<BITS>(mx_quad_max(top));
     const float s = mx_scale_f32(byte);
     const int64_t unit = u0 + i;   // lines are pitch / 512 units long, so units are numbered as they lie
     uint32_t h, l;
     if constexpr (P == 1) mx_encode8<BITS>(w[i][0], s, h, l);
-    else {
-      const float v[8] = {u2f(w[i][0].x), u2f(w[i][0].y), u2f(w[i][0].z), u2f(w[i][0].w), u2f(w[i][P - 1].x), u2f(w[i][P - 1].y), u2f(w[i][P - 1].z), u2f(w[i][P - 1].w)};
-      mx_encode8<BITS>(v, s, h, l);
-    }
+    else mx_encode8<BITS>(w[i][0], w[i][P - 1], s, h, l);
     reinterpret_cast<uint32_t*>(a.row_codes)[unit * 64 + lane] = h;
     if constexpr (BITS == 8) reinterpret_cast<uint32_t*>(a.row_codes)[(units + unit) * 64 + lane] = l;
     if ((lane & 3) == 0) a.row_scales[unit * 16 + (lane >> 2)] = (uint8_t)byte;
@@ -123,7 +80,7 @@ __global__ __launch_bounds__(256) void mx_tile_kernel(QuantArgs a) {
   const int piece = lane & 15, sub = lane >> 4;
   u32x4 w[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = load_piece<T>(a.x, r0 + i * 4 + sub, a.rows, a.cols, a.ld, c0 + piece * EPP);
+  for (int i = 0; i < 8; ++i) w[i] = mx_load_piece<T>(a.x, r0 + i * 4 + sub, a.rows, a.cols, a.ld, c0 + piece * EPP);
   uint32_t* const mine = park[wave];
 #pragma unroll
   for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(mine + (i * 4 + sub) * 64 + piece * 4) = w[i];
@@ -131,7 +88,7 @@ __global__ __launch_bounds__(256) void mx_tile_kernel(QuantArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = r0 + i * 4 + sub;
-      uint32_t top = quad_max(E == 2 ? amax_bf16(w[i]) : amax_f32(w[i]));
+      uint32_t top = mx_quad_max(E == 2 ? mx_amax_bf16(w[i]) : mx_amax_f32(w[i]));
       if constexpr (E == 4) {
         const uint32_t o = other_quad(top);
         top = top > o ? top : o;

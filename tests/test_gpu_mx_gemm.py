@@ -64,6 +64,20 @@ def test_outputs_of_many_tiles(P, Q, Kc, bl, br):
     assert torch.equal(b.mx_gemm(l, r), got)
 
 
+@pytest.mark.parametrize("tile", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("bl,br", BITS)
+@pytest.mark.parametrize("P,Q,Kc", [(1, 8, 8), (70, 40, 2000), (129, 264, 513), (513, 528, 1536)])
+def test_every_tile_gives_the_product(P, Q, Kc, bl, br, tile):
+    """One row, edges inside every tile, one to eight steps of the contraction, whatever the rule would take."""
+    l, vl = operand(P, Kc, bl, P + Kc)
+    r, vr = operand(Q, Kc, br, Q + Kc)
+    ref, tol = vl @ vr.T, bound(vl, vr, Kc)
+    close(b.mx_gemm_by_tile(l, r, tile), ref, tol)
+    close(b.mx_gemm_by_tile(l, r, tile, torch.bfloat16), ref, tol, bf16=True)
+    add = torch.randn(P, Q, device="cuda") * float(np.abs(ref).mean())
+    close(b.mx_gemm_by_tile(l, r, tile, addend=add), ref + add.double().cpu().numpy(), tol + 2.0 ** -22 * np.abs(add.double().cpu().numpy()))
+
+
 @pytest.mark.parametrize("bl,br", BITS)
 @pytest.mark.parametrize("P,Q,Kc", [(5, 24, 100), (200, 136, 700), (600, 520, 1100)])
 def test_addend_and_accumulation_and_rows_apart(P, Q, Kc, bl, br):
