@@ -52,27 +52,27 @@ FP4_HD int64_t few_scales(int64_t pitch) { return pitch / MX_BLOCK + 4; }
 
 // Quantizes the workgroup's tokens into LDS: [plane][token] codes, then [token] scales, those of 512 codes as four words, word g the bytes
 // of blocks g, 4 + g, 8 + g, 12 + g: what lane group g wants.  Four threads a block.
-constexpr int FQ = 4;   // pieces a thread requests before it looks at the first
-
 template <class T, int BITS>
 FP4_D void few_quantize(const FewArgs& a, int64_t p0, int rows, uint8_t* codes, uint8_t* scales) {
+  constexpr int P = sizeof(T) == 2 ? 1 : 2;   // 16-byte pieces of a thread's eight elements
+  constexpr int FQ = P == 1 ? 8 : 4;          // times eight elements that a thread requests before it looks at the first
   const int64_t row_bytes = few_row(a.pitch), scale_bytes = few_scales(a.pitch);
-  const int per_row = (int)(a.pitch / 8), total = rows * per_row;   // threads' eight elements
-  constexpr int P = sizeof(T) == 2 ? 1 : 2;                         // 16-byte pieces of them
-  for (int i0 = threadIdx.x; i0 < total; i0 += FQ * FW_WAVES * 64) {
+  const int per_row = (int)(a.pitch / MX_PITCH), total = rows * per_row;   // a wave takes 512 elements of a token at a time
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int i0 = wave; i0 < total; i0 += FQ * FW_WAVES) {
     u32x4 w[FQ][P];
     int row[FQ], c[FQ];
 #pragma unroll
     for (int n = 0; n < FQ; ++n) {
-      const int i = i0 + n * FW_WAVES * 64;
+      const int i = i0 + n * FW_WAVES;
       row[n] = i / per_row;
-      c[n] = i - row[n] * per_row;
+      c[n] = (i - row[n] * per_row) * 64 + lane;
 #pragma unroll
       for (int p = 0; p < P; ++p) w[n][p] = mx_load_piece<T>(a.x, p0 + row[n], p0 + rows, a.K, a.ldx, c[n] * 8 + p * 4);
     }
 #pragma unroll
     for (int n = 0; n < FQ; ++n) {
-      if (row[n] >= rows) break;   // the same for all four threads of a block
+      if (row[n] >= rows) break;
       uint32_t h, l, byte;
       if constexpr (P == 1) {
         byte = mx_scale_byte<BITS>(mx_quad_max(mx_amax_bf16(w[n][0])));
@@ -233,14 +233,17 @@ void few_launch(const FewArgs& a, bool out_bf16, hipStream_t s) {
   if (out_bf16) hipLaunchKernelGGL((mx_few_kernel<SRC, NT, NW, true>), grid, dim3(FW_WAVES * 64), lds, s, a);
   else hipLaunchKernelGGL((mx_few_kernel<SRC, NT, NW, false>), grid, dim3(FW_WAVES * 64), lds, s, a);
 }
+// Columns a workgroup: a workgroup a CU where there are enough of them, so that every CU has loads under way (one token, 4096 x 4096: 4.6 us
+// with 16 columns, 5.5 with 32), and no more of them than that, so that the tokens are not read more often than they have to be (11008
+// columns, 24 tokens of 4096: 10.2 us with 64 columns, 12.9 with 32; 5120 columns, 32 tokens of 13824: 19 us with 32, 26 with 16).
 template <int SRC, int NT>
 void few_columns(const FewArgs& a, bool out_bf16, int n_cu, hipStream_t s) {
   const int64_t cols = (a.Q + 15) / 16 * ((a.P + 16 * NT - 1) / (16 * NT));   // tiles of 16 columns
+  if (cols <= n_cu) return few_launch<SRC, NT, 1>(a, out_bf16, s);
   if constexpr (NT <= 2) {
-    if (cols >= 4 * (n_cu / 2)) return few_launch<SRC, NT, 4>(a, out_bf16, s);
+    if (cols > 2 * n_cu) return few_launch<SRC, NT, 4>(a, out_bf16, s);
   }
-  if (cols >= 2 * (n_cu / 2)) return few_launch<SRC, NT, 2>(a, out_bf16, s);
-  few_launch<SRC, NT, 1>(a, out_bf16, s);
+  few_launch<SRC, NT, 2>(a, out_bf16, s);
 }
 template <int SRC>
 void few_rows(const FewArgs& a, bool out_bf16, int n_cu, hipStream_t s) {

@@ -430,16 +430,16 @@ FP4_D void finish_tile(const MxGemm& g, const float* tile, int64_t P0, int64_t Q
 
 // ---- 128 x 128 ------------------------------------------------------------------------------------------------------------------
 // For outputs with too few 256 x 256 tiles: a workgroup of four waves, 64 x 64 each.  A step's products take a fifth of a microsecond, less
-// than a load, so steps go through a ring of four LDS stages with three on their way; a stage's scales lie behind its codes as the lanes
-// want them, one word each.
+// than a load, so steps go through a ring of four LDS stages with three on their way; scales come for two steps at a time, sixteen bytes of
+// every row, one load a thread, into a ring of their own.
 constexpr int MT = 128, M_RING = 4;
-constexpr int M_OP = MT * BKB, M_STAGE = 2 * M_OP + 8 * 256, M_LD = MT * 8 / 256, M_LOADS = 2 * M_LD + 2;
+constexpr int M_OP = MT * BKB, M_STAGE = 2 * M_OP, M_LD = MT * 8 / 256, M_SC = M_RING * M_STAGE, M_SC_BYTES = 2 * MT * 16, M_SMEM = M_SC + M_RING * M_SC_BYTES;
 constexpr uint32_t PAST_THE_END = 0xf0000000u;   // behind any descriptor: arrives as zeros
 
 template <bool OUT_BF16>
 __global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
-  static_assert(M_RING * M_STAGE >= MT * (MT + 4) * 4 && M_RING * M_STAGE <= 160 * 1024, "the sums lie over the ring");
-  __shared__ __attribute__((aligned(16))) uint8_t smem[M_RING * M_STAGE];
+  static_assert(M_RING * M_STAGE >= MT * (MT + 4) * 4 && M_SMEM <= 160 * 1024, "the sums lie over the ring");
+  __shared__ __attribute__((aligned(16))) uint8_t smem[M_SMEM];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
@@ -466,16 +466,14 @@ __global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
   };
   planes(0);
   const __amdgpu_buffer_rsrc_t rsrcS = wave < 2 ? rows_rsrc(g.sL + P0 * rows_s, np, rows_s) : rows_rsrc(g.sR + Q0 * rows_s, nq, rows_s);
-  uint32_t offL[M_LD], offR[M_LD], offS[2];
+  uint32_t offL[M_LD], offR[M_LD];
 #pragma unroll
   for (int j = 0; j < M_LD; ++j) {
     const int row = 8 * (wave * M_LD + j) + (lane >> 3), at = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     offL[j] = (uint32_t)(min((int64_t)row, np - 1) * rowb + at);   // rows past the edge re-read the last row
     offR[j] = (uint32_t)(min((int64_t)row, nq - 1) * rowb + at);
   }
-#pragma unroll
-  for (int j = 0; j < 2; ++j)   // blocks of 32 rows 0 .. 3 of L, 4 .. 7 of Rt
-    offS[j] = (uint32_t)(min((int64_t)((2 * wave + j) % 4 * 32 + l32), (wave < 2 ? np : nq) - 1) * rows_s + h * 4);
+  const uint32_t offS = (uint32_t)(min((int64_t)((wave & 1) * 64 + lane), (wave < 2 ? np : nq) - 1) * rows_s);   // wave w: rows 64 w .. of L, then of Rt
   int ld_t = 0, ld_k = 0, ld_pass = 0;
   auto request = [&]() {   // the next step; behind the last one zeros
     uint8_t* const st = smem + (ld_t & (M_RING - 1)) * M_STAGE;
@@ -485,8 +483,7 @@ __global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
       MX_TO_LDS(rsrcL, st + (wave * M_LD + j) * 1024, 16, in ? offL[j] : PAST_THE_END, ld_k * BKB);
       MX_TO_LDS(rsrcR, st + M_OP + (wave * M_LD + j) * 1024, 16, in ? offR[j] : PAST_THE_END, ld_k * BKB);
     }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) MX_TO_LDS(rsrcS, st + 2 * M_OP + (2 * wave + j) * 256, 4, in ? offS[j] : PAST_THE_END, ld_k * 8);
+    if ((ld_t & 1) == 0) MX_TO_LDS(rsrcS, smem + M_SC + ((ld_t >> 1) & (M_RING - 1)) * M_SC_BYTES + wave * 1024, 16, in ? offS : PAST_THE_END, ld_k * 8);
     ++ld_t;
     if (++ld_k == KT) {
       ld_k = 0;
@@ -506,18 +503,20 @@ __global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
   for (int t = 0; t < T; ++t) {
     asm volatile("" ::: "memory");
     // this wave's share of step t is there, and it is done reading step t - 1; behind the barrier that holds for all
-    constexpr int left = (M_RING - 2) * M_LOADS;
+    constexpr int left = (M_RING - 2) * 2 * M_LD + 1;   // of the two steps behind it one brings scales
+    static_assert(M_RING == 4, "so many steps");
     __builtin_amdgcn_s_waitcnt(0x0070 | (left & 15) | ((left >> 4) << 14));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     request();
     const uint8_t* const st = smem + (t & (M_RING - 1)) * M_STAGE;
     const uint8_t *const sL = st + (wp + l32) * BKB, *const sR = st + M_OP + (wq + l32) * BKB;
+    const uint8_t* const sc = smem + M_SC + ((t >> 1) & (M_RING - 1)) * M_SC_BYTES + (t & 1) * 8 + h * 4;
     uint32_t sl[2], sr[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      sl[j] = *reinterpret_cast<const uint32_t*>(st + 2 * M_OP + (wp / 32 + j) * 256 + lane * 4) - lessl;
-      sr[j] = *reinterpret_cast<const uint32_t*>(st + 2 * M_OP + (4 + wq / 32 + j) * 256 + lane * 4) - lessr;
+      sl[j] = *reinterpret_cast<const uint32_t*>(sc + (wp + j * 32 + l32) * 16) - lessl;
+      sr[j] = *reinterpret_cast<const uint32_t*>(sc + (MT + wq + j * 32 + l32) * 16) - lessr;
     }
     u32x4 fl[4][2], fr[4][2];
 #pragma unroll

@@ -31,18 +31,19 @@ constexpr int ROWS_U = 4;
 template <class T, int BITS>
 __global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units, int per_row) {
   const int lane = threadIdx.x & 63;
-  const int64_t u0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * ROWS_U;
+  const int64_t u0 = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * ROWS_U;
   constexpr int P = sizeof(T) == 2 ? 1 : 2;   // pieces a lane
   u32x4 w[ROWS_U][P];
-  int64_t row[ROWS_U];
-  int seg[ROWS_U];
+  int64_t row = u0 / per_row;
+  int seg = (int)(u0 - row * per_row);
 #pragma unroll
   for (int i = 0; i < ROWS_U; ++i) {
-    row[i] = (u0 + i) / per_row;
-    seg[i] = (int)((u0 + i) - row[i] * per_row);
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-      w[i][p] = mx_load_piece<T>(a.x, u0 + i < units ? row[i] : a.rows, a.rows, a.cols, a.ld, (int64_t)seg[i] * MX_PITCH + lane * 8 + p * 4);
+    for (int p = 0; p < P; ++p) w[i][p] = mx_load_piece<T>(a.x, row, a.rows, a.cols, a.ld, (int64_t)seg * MX_PITCH + lane * 8 + p * 4);
+    if (++seg == per_row) {
+      seg = 0;
+      ++row;
+    }
   }
 #pragma unroll
   for (int i = 0; i < ROWS_U; ++i) {
@@ -66,16 +67,23 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units
 }
 
 // ---- columns, and rows beside them ----------------------------------------------------------------------------------------------
-// A workgroup of four waves takes 128 rows x 256 bytes of columns, a wave 32 of the rows: one block of every column.
+// A workgroup of eight waves takes 256 rows x 256 bytes of columns, a wave 32 of the rows: one block of every column.  The columns' codes
+// pass through LDS once more, so that they leave as whole 128-byte lines (256 rows of 4-bit codes).
+constexpr int TW = 8;   // waves
+
 template <class T, int ROW, int COL>
-__global__ __launch_bounds__(256) void mx_tile_kernel(QuantArgs a) {
+__global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles_c, int64_t tiles) {
   constexpr int E = sizeof(T);
   constexpr int CW = 256 / E;        // columns a tile
   constexpr int EPP = 16 / E;        // elements of a 16-byte piece
-  __shared__ __attribute__((aligned(16))) uint32_t park[4][32 * 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t r0 = (int64_t)blockIdx.y * 128 + wave * 32;
-  const int64_t c0 = (int64_t)blockIdx.x * CW;
+  constexpr int NC = 4 / E;          // columns a lane
+  __shared__ __attribute__((aligned(16))) uint32_t park[TW][32 * 64];
+  // neighbours along a row on one XCD, whose L2 joins their parts of the rows' lines
+  const int64_t per_xcd = (tiles + 7) / 8, id = (int64_t)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if ((int64_t)(blockIdx.x / 8) >= per_xcd || id >= tiles) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t tr = id / tiles_c;
+  const int64_t r0 = tr * (TW * 32) + wave * 32, c0 = (id - tr * tiles_c) * CW;
   const int64_t row_pitch = mx_pitch_of(a.cols), col_pitch = mx_pitch_of(a.rows);
   const int piece = lane & 15, sub = lane >> 4;
   u32x4 w[8];
@@ -119,48 +127,62 @@ __global__ __launch_bounds__(256) void mx_tile_kernel(QuantArgs a) {
   uint32_t d[32];
 #pragma unroll
   for (int r = 0; r < 32; ++r) d[r] = mine[r * 64 + lane];
-  constexpr int NC = 4 / E;   // columns a lane
+  u32x4 hi[NC], lo[NC];
+  uint32_t bytes[NC];
 #pragma unroll
   for (int h = 0; h < NC; ++h) {
-    const int64_t col = c0 + lane * NC + h;
     uint32_t top = 0;
-    if constexpr (E == 2) {
 #pragma unroll
-      for (int r = 0; r < 32; ++r) {
-        const uint32_t m = (h == 0 ? d[r] << 16 : d[r] & 0xffff0000u) & 0x7fffffffu;
-        top = top > m ? top : m;
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < 32; ++r) {
-        const uint32_t m = d[r] & 0x7fffffffu;
-        top = top > m ? top : m;
-      }
+    for (int r = 0; r < 32; ++r) {
+      const uint32_t m = (E == 4 ? d[r] : h == 0 ? d[r] << 16 : d[r]) & (E == 4 ? 0x7fffffffu : 0x7fff0000u);
+      top = top > m ? top : m;
     }
-    const uint32_t byte = mx_scale_byte<COL>(top);
-    const float s = mx_scale_f32(byte);
-    uint32_t hi[4], lo[4];
+    bytes[h] = mx_scale_byte<COL>(top);
+    const float s = mx_scale_f32(bytes[h]);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {   // eight rows
+      uint32_t ch, cl;
       if constexpr (E == 2) {
         u32x4 pr;   // rows 2 i and 2 i + 1 of this column
 #pragma unroll
         for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_perm(d[8 * q + 2 * i + 1], d[8 * q + 2 * i], h == 0 ? 0x05040100u : 0x07060302u);
-        mx_encode8<COL>(pr, s, hi[q], lo[q]);
+        mx_encode8<COL>(pr, s, ch, cl);
       } else {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = u2f(d[8 * q + i]);
-        mx_encode8<COL>(v, s, hi[q], lo[q]);
+        mx_encode8<COL>(v, s, ch, cl);
       }
-    }
-    if (col < a.cols) {
-      const int64_t at = col * col_pitch + r0;
-      *reinterpret_cast<u32x4*>(a.col_codes + at / 2) = u32x4{hi[0], hi[1], hi[2], hi[3]};
-      if constexpr (COL == 8) *reinterpret_cast<u32x4*>(a.col_codes + (a.cols * col_pitch + at) / 2) = u32x4{lo[0], lo[1], lo[2], lo[3]};
-      a.col_scales[at / MX_BLOCK] = (uint8_t)byte;
+      hi[h][q] = ch;
+      lo[h][q] = cl;
     }
   }
+  // [plane][column][wave], sixteen bytes each, and the scales [column][wave], over the parked rows; a column's eight pieces are rotated by its
+  // number, so that eight lanes with one piece of eight columns meet eight bank groups
+  __syncthreads();
+  uint8_t* const out = reinterpret_cast<uint8_t*>(&park[0][0]);
+  uint8_t* const out_scales = out + COL / 4 * CW * 128;
+#pragma unroll
+  for (int h = 0; h < NC; ++h) {
+    const int c = lane * NC + h, at = c * 128 + ((wave + c) & 7) * 16;
+    *reinterpret_cast<u32x4*>(out + at) = hi[h];
+    if constexpr (COL == 8) *reinterpret_cast<u32x4*>(out + CW * 128 + at) = lo[h];
+    out_scales[c * 8 + wave] = (uint8_t)bytes[h];
+  }
+  __syncthreads();
+  const int64_t rr = tr * (TW * 32);
+#pragma unroll
+  for (int i = 0; i < CW * 8 / (TW * 64); ++i) {
+    const int n = i * TW * 64 + threadIdx.x, c = n >> 3, piece16 = n & 7;
+    if (c0 + c < a.cols) {
+      const int64_t at = ((c0 + c) * col_pitch + rr) / 2 + piece16 * 16;
+#pragma unroll
+      for (int p = 0; p < COL / 4; ++p)
+        *reinterpret_cast<u32x4*>(a.col_codes + p * (a.cols * col_pitch / 2) + at) = *reinterpret_cast<const u32x4*>(out + p * CW * 128 + c * 128 + ((piece16 + c) & 7) * 16);
+    }
+  }
+  if (threadIdx.x < CW && c0 + threadIdx.x < a.cols)
+    *reinterpret_cast<u32x2*>(a.col_scales + ((c0 + threadIdx.x) * col_pitch + rr) / MX_BLOCK) = *reinterpret_cast<const u32x2*>(out_scales + threadIdx.x * 8);
 }
 
 // ---- back ----------------------------------------------------------------------------------------------------------------------
@@ -243,7 +265,7 @@ template <> struct Eight<float> { typedef float type[8]; };
 template <class T, int BITS>
 __global__ __launch_bounds__(256) void mx_restore_rows_kernel(DequantArgs a, int64_t units, int per_line) {
   const int lane = threadIdx.x & 63;
-  const int64_t u0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * ROWS_U;
+  const int64_t u0 = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * ROWS_U;
   uint32_t c[ROWS_U][BITS / 4], b[ROWS_U];
 #pragma unroll
   for (int i = 0; i < ROWS_U; ++i) {
@@ -252,38 +274,62 @@ __global__ __launch_bounds__(256) void mx_restore_rows_kernel(DequantArgs a, int
     for (int k = 0; k < BITS / 4; ++k) c[i][k] = reinterpret_cast<const uint32_t*>(a.codes)[(k * units + u) * 64 + lane];
     b[i] = a.scales[u * 16 + (lane >> 2)];
   }
+  int64_t line = u0 / per_line;
+  int seg = (int)(u0 - line * per_line);
 #pragma unroll
   for (int i = 0; i < ROWS_U; ++i) {
     if (u0 + i >= units) break;
-    const int64_t line = (u0 + i) / per_line;
-    const int64_t at = ((u0 + i) - line * per_line) * MX_PITCH + lane * 8;
-    if (at >= a.length) continue;
-    typename Eight<T>::type o;
-    decode8<BITS>(c[i], b[i], o);
-    store8(reinterpret_cast<T*>(a.x) + line * a.ld + at, o, a.length - at);
+    const int64_t at = (int64_t)seg * MX_PITCH + lane * 8;
+    if (at < a.length) {
+      typename Eight<T>::type o;
+      decode8<BITS>(c[i], b[i], o);
+      store8(reinterpret_cast<T*>(a.x) + line * a.ld + at, o, a.length - at);
+    }
+    if (++seg == per_line) {
+      seg = 0;
+      ++line;
+    }
   }
 }
 
-// Lines as columns: a lane takes eight rows of eight columns, a wave 64 x 64.
+// Lines as columns: a workgroup takes 256 elements of 64 lines, whole 128-byte lines of codes, through LDS; then a lane eight rows of eight
+// columns.  A line's words in LDS are one apart from a multiple of the banks.
 template <class T, int BITS>
-__global__ __launch_bounds__(256) void mx_restore_cols_kernel(DequantArgs a) {
+__global__ __launch_bounds__(256) void mx_restore_cols_kernel(DequantArgs a, int tiles_l, int64_t tiles) {
+  constexpr int LW = 33;   // words a line
+  __shared__ uint32_t park[BITS / 4][64 * LW];
+  // neighbours along a row of x on one XCD
+  const int64_t per_xcd = (tiles + 7) / 8, id = (int64_t)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if ((int64_t)(blockIdx.x / 8) >= per_xcd || id >= tiles) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t r0 = (int64_t)blockIdx.x * 256 + wave * 64 + (lane >> 3) * 8;   // the element of a line = the row of x
-  const int64_t c0 = (int64_t)blockIdx.y * 64 + (lane & 7) * 8;                 // the line = the column of x
+  const int64_t te = id / tiles_l, e0 = te * 256, l0 = (id - te * tiles_l) * 64;
   const int64_t pitch = mx_pitch_of(a.length);
-  if (r0 >= a.length || c0 >= a.lines) return;
-  uint32_t c[8][BITS / 4], b[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int64_t line = c0 + j < a.lines ? c0 + j : a.lines - 1;
-    const int64_t at = line * pitch + r0;
+  for (int i = 0; i < 2; ++i) {
+    const int n = i * 256 + threadIdx.x, line = n >> 3, piece = n & 7;
+    const int64_t at = (min(l0 + line, a.lines - 1) * pitch + e0) / 2 + piece * 16;
 #pragma unroll
-    for (int k = 0; k < BITS / 4; ++k) c[j][k] = reinterpret_cast<const uint32_t*>(a.codes)[(k * a.lines * pitch + at) / 8];
-    b[j] = a.scales[at / MX_BLOCK];
+    for (int k = 0; k < BITS / 4; ++k) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(a.codes + k * (a.lines * pitch / 2) + at);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) park[k][line * LW + piece * 4 + q] = v[q];
+    }
   }
+  const int cl = (lane & 7) * 8, rg = wave * 8 + (lane >> 3);   // the lane's first column, and which eight rows
+  const int64_t r0 = e0 + rg * 8, c0 = l0 + cl;
+  uint32_t b[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) b[j] = a.scales[min(c0 + j, a.lines - 1) * (pitch / MX_BLOCK) + r0 / MX_BLOCK];
+  __syncthreads();
+  if (r0 >= a.length || c0 >= a.lines) return;
   typename Eight<T>::type o[8];   // by column
 #pragma unroll
-  for (int j = 0; j < 8; ++j) decode8<BITS>(c[j], b[j], o[j]);
+  for (int j = 0; j < 8; ++j) {
+    uint32_t c[BITS / 4];
+#pragma unroll
+    for (int k = 0; k < BITS / 4; ++k) c[k] = park[k][(cl + j) * LW + rg];
+    decode8<BITS>(c, b[j], o[j]);
+  }
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
     if (r0 + r >= a.length) break;
@@ -301,9 +347,11 @@ __global__ __launch_bounds__(256) void mx_restore_cols_kernel(DequantArgs a) {
 
 template <class T, int ROW>
 void launch_tiles(const QuantArgs& a, int col_bits, hipStream_t s) {
-  const dim3 grid((unsigned)(mx_pitch_of(a.cols) * sizeof(T) / 256), (unsigned)(mx_pitch_of(a.rows) / 128));
-  if (col_bits == 4) hipLaunchKernelGGL((mx_tile_kernel<T, ROW, 4>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((mx_tile_kernel<T, ROW, 8>), grid, dim3(256), 0, s, a);
+  const int tiles_c = (int)(mx_pitch_of(a.cols) * sizeof(T) / 256);   // up to the pitches: what lies behind the ends is written too
+  const int64_t tiles = tiles_c * (mx_pitch_of(a.rows) / (TW * 32));
+  const dim3 grid((unsigned)((tiles + 7) / 8 * 8)), block(TW * 64);
+  if (col_bits == 4) hipLaunchKernelGGL((mx_tile_kernel<T, ROW, 4>), grid, block, 0, s, a, tiles_c, tiles);
+  else hipLaunchKernelGGL((mx_tile_kernel<T, ROW, 8>), grid, block, 0, s, a, tiles_c, tiles);
 }
 
 template <class T>
@@ -324,8 +372,9 @@ int launch_quantize(const QuantArgs& a, int row_bits, int col_bits, hipStream_t 
 template <class T, int BITS>
 int launch_dequantize(const DequantArgs& a, bool transposed, hipStream_t s) {
   if (transposed) {
-    const dim3 grid((unsigned)((a.length + 255) / 256), (unsigned)((a.lines + 63) / 64));
-    hipLaunchKernelGGL((mx_restore_cols_kernel<T, BITS>), grid, dim3(256), 0, s, a);
+    const int tiles_l = (int)((a.lines + 63) / 64);
+    const int64_t tiles = tiles_l * ((a.length + 255) / 256);
+    hipLaunchKernelGGL((mx_restore_cols_kernel<T, BITS>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), 0, s, a, tiles_l, tiles);
   } else {
     const int per_line = (int)(mx_pitch_of(a.length) / MX_PITCH);
     const int64_t units = a.lines * per_line;

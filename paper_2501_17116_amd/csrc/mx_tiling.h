@@ -11,10 +11,11 @@ struct MxTiling {
 
 inline MxTiling mx_gemm_tiling(int64_t P, int64_t Q, int64_t Kc, int bits_l, int bits_r, int n_cu) {
   if (Kc == 0) return {64, 0};
-  if (P <= 64) return {16, 0};
+  const int64_t passes = (bits_l / 4) * (bits_r / 4);
+  if (P <= 32 || (P <= 64 && Kc * passes <= 2048)) return {16, 0};
   const int64_t t32 = ((P + 31) / 32) * ((Q + 31) / 32), t128 = ((P + 127) / 128) * ((Q + 127) / 128), t256 = ((P + 255) / 256) * ((Q + 255) / 256);
-  if (t32 <= 2 * n_cu) return {32, 0};
-  if (t128 <= 2 * n_cu) return {128, 0};
+  if (t32 <= 4 * (int64_t)n_cu) return {32, 0};
+  if (t128 <= n_cu) return {128, 0};
   const int64_t wgs = n_cu / 8 * 8;
   return {256, (int)(t256 > wgs && 4 * (t256 % wgs) <= wgs ? t256 % wgs : 0)};
 }
