@@ -549,20 +549,24 @@ class MxTensor:
     codes [lines, mx_pitch(length) / 2] (4 bits) or [2, lines, mx_pitch(length) / 2] (8 bits), scales [lines, mx_pitch(length) / 32],
     uint8.  transposed: the lines are the columns of the matrix that the tensor stands for."""
 
-    __slots__ = ("codes", "scales", "bits", "lines", "length", "transposed", "c")
+    __slots__ = ("codes", "scales", "bits", "lines", "length", "transposed", "c", "ref")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, length: int, transposed: bool = False):
-        _dev_check(codes, scales)
-        pitch = mx_pitch(length)
+        pitch, shape, lines = mx_pitch(length), tuple(codes.shape), scales.shape[0]
         if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
             raise TypeError("codes and scales must be uint8")
-        if scales.dim() != 2 or codes.shape[-1] != pitch // 2 or scales.shape[1] != pitch // MX_BLOCK or \
-                codes.shape[:-1] not in ((scales.shape[0],), (2, scales.shape[0])):
-            raise ValueError("codes %s and scales %s do not hold lines of %d elements" % (tuple(codes.shape), tuple(scales.shape), length))
-        if codes.device != scales.device:
-            raise ValueError("codes and scales must live on one device")
-        self.codes, self.scales, self.bits, self.lines, self.length, self.transposed = codes, scales, 4 * (codes.dim() - 1), scales.shape[0], length, transposed
-        self.c = fp4_mx(codes.data_ptr(), scales.data_ptr(), self.lines, length, self.bits)
+        if tuple(scales.shape) != (lines, pitch // MX_BLOCK) or shape not in ((lines, pitch // 2), (2, lines, pitch // 2)):
+            raise ValueError("codes %s and scales %s do not hold lines of %d elements" % (shape, tuple(scales.shape), length))
+        if not codes.is_cuda or codes.device != scales.device:
+            raise ValueError("codes and scales must live on one GPU")
+        if not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales must be contiguous")
+        self._set(codes, scales, 4 * (len(shape) - 1), lines, length, transposed)
+
+    def _set(self, codes, scales, bits, lines, length, transposed):
+        self.codes, self.scales, self.bits, self.lines, self.length, self.transposed = codes, scales, bits, lines, length, transposed
+        self.c = fp4_mx(codes.data_ptr(), scales.data_ptr(), lines, length, bits)
+        self.ref = C.byref(self.c)
 
     @property
     def shape(self) -> Tuple[int, int]:
@@ -574,8 +578,10 @@ def mx_empty(lines: int, length: int, bits: int = 4, transposed: bool = False, d
     if bits not in (4, 8):
         raise ValueError("an MX element has 4 or 8 bits")
     pitch = mx_pitch(length)
-    return MxTensor(torch.empty((lines, pitch // 2) if bits == 4 else (2, lines, pitch // 2), dtype=torch.uint8, device=device),
-                    torch.empty((lines, pitch // MX_BLOCK), dtype=torch.uint8, device=device), length, transposed)
+    t = MxTensor.__new__(MxTensor)
+    t._set(torch.empty((lines, pitch // 2) if bits == 4 else (2, lines, pitch // 2), dtype=torch.uint8, device=device),
+           torch.empty((lines, pitch // MX_BLOCK), dtype=torch.uint8, device=device), bits, lines, length, transposed)
+    return t
 
 
 def _ld(t: torch.Tensor, name: str) -> int:
@@ -584,10 +590,10 @@ def _ld(t: torch.Tensor, name: str) -> int:
         raise ValueError("tensors must live on the GPU")
     if t.dim() != 2:
         raise ValueError("%s must be a matrix" % name)
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("%s's rows must be contiguous" % name)
-    return t.stride(0) if rows > 1 and cols > 0 else max(8, -(-cols // 8) * 8)
+    return ld if rows > 1 and cols > 0 else max(8, -(-cols // 8) * 8)
 
 
 def _same_device(x: torch.Tensor, *mx: Optional[MxTensor]):
@@ -600,14 +606,35 @@ def _out(t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor, name: str)
     """The caller's output, checked, or a new one; its rows begin at multiples of 16 bytes."""
     if t is None:
         rows, cols = shape
+        if cols % 8 == 0:
+            return torch.empty(shape, dtype=dtype, device=like.device)
         return torch.empty((rows, -(-cols // 8) * 8), dtype=dtype, device=like.device)[:, :cols]
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != like.device:
+    if t.shape != shape or t.dtype != dtype or t.device != like.device:
         raise ValueError("%s must be %s %s on %s" % (name, tuple(shape), dtype, like.device))
     return t
 
 
-def _mx_ref(t: Optional[MxTensor]):
-    return None if t is None else C.byref(t.c)
+_mx_room = {}   # (op, M, K, N) -> bytes: the query's answer does not change
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    """Handle of the current stream of t's device.  (torch.cuda.current_stream() takes 4 us, as long as a small kernel.)"""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _mx_ws(op: int, M: int, K: int, N: int, ws: Optional[Workspace], like: torch.Tensor):
+    """(workspace pointer, its bytes, stream handle) of an MX layer call."""
+    need = _mx_room.get((op, M, K, N))
+    if need is None:
+        need = _mx_room[op, M, K, N] = workspace_bytes(op, M, K, N, FP4_BF16)
+    stream = _stream_of(like)
+    if ws is None:
+        key = (like.device.index, stream)
+        ws = _default_ws.get(key)
+        if ws is None:
+            ws = _default_ws[key] = Workspace(like.device)
+    buf = ws.get(need)
+    return buf.data_ptr(), buf.numel(), stream
 
 
 def mx_quantize(x: torch.Tensor, axis: int, bits: int = 4, out: Optional[MxTensor] = None) -> MxTensor:
@@ -620,9 +647,8 @@ def mx_quantize(x: torch.Tensor, axis: int, bits: int = 4, out: Optional[MxTenso
     if out is None:
         out = mx_empty(lines, length, bits, axis == FP4_AXIS_COL, x.device)
     _same_device(x, out)
-    ref = _mx_ref(out)
-    _check(lib().mx_quantize(_ptr(x), _dt(x), rows, cols, ld, ref if axis == FP4_AXIS_ROW else None, ref if axis == FP4_AXIS_COL else None, _stream()),
-           "mx_quantize")
+    _check(lib().mx_quantize(x.data_ptr(), _dt(x), rows, cols, ld, out.ref if axis == FP4_AXIS_ROW else None,
+                             out.ref if axis == FP4_AXIS_COL else None, _stream_of(x)), "mx_quantize")
     return out
 
 
@@ -631,14 +657,14 @@ def mx_quantize_both(x: torch.Tensor, row_bits: int = 4, col_bits: int = 4) -> T
     ld = _ld(x, "x")
     rows, cols = x.shape
     r, c = mx_empty(rows, cols, row_bits, False, x.device), mx_empty(cols, rows, col_bits, True, x.device)
-    _check(lib().mx_quantize(_ptr(x), _dt(x), rows, cols, ld, _mx_ref(r), _mx_ref(c), _stream()), "mx_quantize")
+    _check(lib().mx_quantize(x.data_ptr(), _dt(x), rows, cols, ld, r.ref, c.ref, _stream_of(x)), "mx_quantize")
     return r, c
 
 
 def mx_dequantize(t: MxTensor, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The matrix that t stands for, in the values of its codes."""
     x = _out(out, t.shape, dtype, t.codes, "out")
-    _check(lib().mx_dequantize(_mx_ref(t), int(t.transposed), _ptr(x), _dt(x), _ld(x, "out"), _stream()), "mx_dequantize")
+    _check(lib().mx_dequantize(t.ref, int(t.transposed), x.data_ptr(), _dt(x), _ld(x, "out"), _stream_of(x)), "mx_dequantize")
     return x
 
 
@@ -651,18 +677,18 @@ def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, a
     out = _out(out, (l.lines, rt.lines), out.dtype if out is not None else out_dtype, l.codes, "out")
     ldo = _ld(out, "out")
     if addend is not None:
-        if tuple(addend.shape) != tuple(out.shape) or addend.dtype != torch.float32 or addend.device != out.device:
+        if addend.shape != out.shape or addend.dtype != torch.float32 or addend.device != out.device:
             raise ValueError("addend must be %s float32 on %s" % (tuple(out.shape), out.device))
-        if addend.shape[0] > 1 and _ld(addend, "addend") != ldo:
+        if _ld(addend, "addend") != ldo:
             raise ValueError("addend and out must have the same leading dimension")
-    _check(lib().mx_gemm(_mx_ref(l), _mx_ref(rt), _ptr(addend), _ptr(out), _dt(out), ldo, _stream()), "mx_gemm")
+    _check(lib().mx_gemm(l.ref, rt.ref, None if addend is None else addend.data_ptr(), out.data_ptr(), _dt(out), ldo, _stream_of(out)), "mx_gemm")
     return out
 
 
 def mx_gemm_by_tile(l: MxTensor, rt: MxTensor, tile: int, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mx_gemm by one kind of tile (16, 32, 64, 128, 256), for tests and measuring; addend has the output's leading dimension."""
     out = _out(None, (l.lines, rt.lines), out_dtype, l.codes, "out")
-    _check(lib().mx_gemm_by_tile(_mx_ref(l), _mx_ref(rt), _ptr(addend), _ptr(out), _dt(out), _ld(out, "out"), tile, _stream()), "mx_gemm_by_tile")
+    _check(lib().mx_gemm_by_tile(l.ref, rt.ref, _ptr(addend), _ptr(out), _dt(out), _ld(out, "out"), tile, _stream()), "mx_gemm_by_tile")
     return out
 
 
@@ -710,9 +736,9 @@ def mx_linear_fwd(A: torch.Tensor, W: MxTensor, act_bits: int = 4, saved: Option
         raise ValueError("the checkpoint holds %d x %d activations, not %d x %d" % (saved.length, saved.lines, M, K))
     _same_device(A, W, saved)
     Y = _out(Y, (M, N), A.dtype, A, "Y")
-    w = _ws(workspace_bytes(FP4_OP_MX_FWD, M, K, N, _dt(A)), ws)
-    _check(lib().mx_linear_fwd(_ptr(A), _dt(A), M, K, N, lda, act_bits, _mx_ref(W), _ptr(Y), _ld(Y, "Y"), _mx_ref(saved), _ptr(w), w.numel(),
-                               _stream()), "mx_linear_fwd")
+    room, nbytes, stream = _mx_ws(FP4_OP_MX_FWD, M, K, N, ws, A)
+    _check(lib().mx_linear_fwd(A.data_ptr(), _dt(A), M, K, N, lda, act_bits, W.ref, Y.data_ptr(), _ld(Y, "Y"), None if saved is None else saved.ref,
+                               room, nbytes, stream), "mx_linear_fwd")
     return Y
 
 
@@ -725,8 +751,8 @@ def mx_linear_bwd_dgrad(dY: torch.Tensor, W: MxTensor, dA: Optional[torch.Tensor
         raise ValueError("dY [M,N] and W (lines K, length N) must agree in N")
     _same_device(dY, W)
     dA = _out(dA, (M, K), dY.dtype, dY, "dA")
-    w = _ws(workspace_bytes(FP4_OP_MX_DGRAD, M, K, N, _dt(dY)), ws)
-    _check(lib().mx_linear_bwd_dgrad(_ptr(dY), _dt(dY), M, K, N, ldy, _mx_ref(W), _ptr(dA), _ld(dA, "dA"), _ptr(w), w.numel(), _stream()),
+    room, nbytes, stream = _mx_ws(FP4_OP_MX_DGRAD, M, K, N, ws, dY)
+    _check(lib().mx_linear_bwd_dgrad(dY.data_ptr(), _dt(dY), M, K, N, ldy, W.ref, dA.data_ptr(), _ld(dA, "dA"), room, nbytes, stream),
            "mx_linear_bwd_dgrad")
     return dA
 
@@ -743,9 +769,9 @@ def mx_linear_bwd_wgrad(dY: torch.Tensor, saved: MxTensor, grad_bits: int = 4, d
         raise ValueError("accumulate needs the dW to add to")
     _same_device(dY, saved)
     dW = _out(dW, (K, N), torch.float32, dY, "dW")
-    w = _ws(workspace_bytes(FP4_OP_MX_WGRAD, M, K, N, _dt(dY)), ws)
-    _check(lib().mx_linear_bwd_wgrad(_ptr(dY), _dt(dY), M, K, N, ldy, _mx_ref(saved), grad_bits, int(accumulate), _ptr(dW), _ld(dW, "dW"), _ptr(w),
-                                     w.numel(), _stream()), "mx_linear_bwd_wgrad")
+    room, nbytes, stream = _mx_ws(FP4_OP_MX_WGRAD, M, K, N, ws, dY)
+    _check(lib().mx_linear_bwd_wgrad(dY.data_ptr(), _dt(dY), M, K, N, ldy, saved.ref, grad_bits, int(accumulate), dW.data_ptr(), _ld(dW, "dW"), room,
+                                     nbytes, stream), "mx_linear_bwd_wgrad")
     return dW
 
 
@@ -762,9 +788,9 @@ def mx_linear_bwd(dY: torch.Tensor, saved: MxTensor, W: MxTensor, grad_bits: int
     _same_device(dY, W, saved)
     dA = _out(dA, (M, K), dY.dtype, dY, "dA")
     dW = _out(dW, (K, N), torch.float32, dY, "dW")
-    w = _ws(workspace_bytes(FP4_OP_MX_BWD, M, K, N, _dt(dY)), ws)
-    _check(lib().mx_linear_bwd(_ptr(dY), _dt(dY), M, K, N, ldy, _mx_ref(W), _mx_ref(saved), grad_bits, _ptr(dA), _ld(dA, "dA"), int(accumulate),
-                               _ptr(dW), _ld(dW, "dW"), _ptr(w), w.numel(), _stream()), "mx_linear_bwd")
+    room, nbytes, stream = _mx_ws(FP4_OP_MX_BWD, M, K, N, ws, dY)
+    _check(lib().mx_linear_bwd(dY.data_ptr(), _dt(dY), M, K, N, ldy, W.ref, saved.ref, grad_bits, dA.data_ptr(), _ld(dA, "dA"), int(accumulate),
+                               dW.data_ptr(), _ld(dW, "dW"), room, nbytes, stream), "mx_linear_bwd")
     return dA, dW
 
 
