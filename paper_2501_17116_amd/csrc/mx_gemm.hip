@@ -35,6 +35,7 @@ struct MxGemm {
   int64_t P, Q, ldo;
   int64_t planeL, planeR;   // bytes of a plane of codes
   int64_t pitch;            // elements of a line
+  int steps;                // of 256 codes a pass
   int nl, nr;               // planes
   int tiles_p, tiles_q;
   int first, count;         // tiles of this launch, in the order of tile_at
@@ -61,8 +62,7 @@ FP4_D mx_f32x16 mx_mfma(const u32x4& r, const u32x4& l, const mx_f32x16& c, uint
   else return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 3, (int)sr, 3, (int)sl);
 }
 
-// 64 x 64 outputs a workgroup, 32 x 32 a wave, operands straight from memory to the matrix core's registers, 512 codes of the contraction a
-// step.  Rows past the matrix's edge repeat its last one and are not stored.
+// 64 x 64 outputs a workgroup, 32 x 32 a wave, operands straight from memory to the matrix core's registers.  Rows past the matrix's edge repeat its last one and are not stored.
 template <bool OUT_BF16>
 __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -77,15 +77,13 @@ __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
     const int pl = pass % g.nl, pr = pass / g.nl;
     const uint8_t *l = g.L + pl * g.planeL + p * (g.pitch / 2) + h * 64, *r = g.R + pr * g.planeR + q * (g.pitch / 2) + h * 64;
     const uint32_t lessl = pl ? MX_EIGHTH : 0u, lessr = pr ? MX_EIGHTH : 0u;
-    for (int64_t k = 0; k < g.pitch / 256; k += 2) {
-      static_for<2>([&](auto jc) {   // 256 codes, one word of scales
-        constexpr int j = decltype(jc)::value;
-        const uint32_t bl = sl[2 * (k + j) + h] - lessl, br = sr[2 * (k + j) + h] - lessr;
-        const u32x4 *lv = reinterpret_cast<const u32x4*>(l + (k + j) * 128), *rv = reinterpret_cast<const u32x4*>(r + (k + j) * 128);
-        static_for<4>([&](auto sc) {
-          constexpr int sl4 = decltype(sc)::value;
-          acc = mx_mfma<sl4>(rv[sl4], lv[sl4], acc, br, bl);
-        });
+#pragma unroll 2
+    for (int k = 0; k < g.steps; ++k) {   // 256 codes, one word of scales
+      const uint32_t bl = sl[2 * k + h] - lessl, br = sr[2 * k + h] - lessr;
+      const u32x4 *lv = reinterpret_cast<const u32x4*>(l + k * 128), *rv = reinterpret_cast<const u32x4*>(r + k * 128);
+      static_for<4>([&](auto sc) {
+        constexpr int s = decltype(sc)::value;
+        acc = mx_mfma<s>(rv[s], lv[s], acc, br, bl);
       });
     }
   }
@@ -429,21 +427,23 @@ FP4_D void finish_tile(const MxGemm& g, const float* tile, int64_t P0, int64_t Q
 }
 
 // ---- 128 x 128 ------------------------------------------------------------------------------------------------------------------
-// For outputs with too few 256 x 256 tiles: a workgroup of four waves, 64 x 64 each.  A step's products take a fifth of a microsecond, less
-// than a load, so steps go through a ring of four LDS stages with three on their way; scales come for two steps at a time, sixteen bytes of
-// every row, one load a thread, into a ring of their own.
-constexpr int MT = 128, M_RING = 4;
-constexpr int M_OP = MT * BKB, M_STAGE = 2 * M_OP, M_LD = MT * 8 / 256, M_SC = M_RING * M_STAGE, M_SC_BYTES = 2 * MT * 16, M_SMEM = M_SC + M_RING * M_SC_BYTES;
+// For outputs with too few 256 x 256 tiles.  Two groups of four waves, a wave 64 x 64 of the sums; the groups share each step, two of its
+// four slices each, so that a SIMD has one wave that reads fragments while another multiplies (with four waves a step took
+// the sum of both), and their sums are joined at the end, the first group's and the second's.  Steps go through a ring of four LDS stages
+// with three on their way; scales come for two steps at a time, sixteen bytes of every row, into a ring of their own.
+constexpr int MT = 128, M_RING = 4, M_WAVES = 8;
+constexpr int M_OP = MT * BKB, M_STAGE = 2 * M_OP, M_LD = MT * 8 / (M_WAVES * 64), M_SC = M_RING * M_STAGE, M_SC_BYTES = 2 * MT * 16;
+constexpr int M_SMEM = M_SC + M_RING * M_SC_BYTES;
 constexpr uint32_t PAST_THE_END = 0xf0000000u;   // behind any descriptor: arrives as zeros
 
 template <bool OUT_BF16>
-__global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
+__global__ __launch_bounds__(M_WAVES * 64) void mx_gemm_mid_kernel(MxGemm g) {
   static_assert(M_RING * M_STAGE >= MT * (MT + 4) * 4 && M_SMEM <= 160 * 1024, "the sums lie over the ring");
   __shared__ __attribute__((aligned(16))) uint8_t smem[M_SMEM];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, h = lane >> 5;
-  const int wp = (wave & 1) * 64, wq = (wave >> 1) * 64;
+  const int l32 = lane & 31, h = lane >> 5, group = wave >> 2;
+  const int wp = (wave & 1) * 64, wq = (wave >> 1 & 1) * 64;
   // each XCD a contiguous run of tiles: of the whole output, or (first > 0) the quarters of the 256 x 256 tiles from `first` on
   const int per_xcd = (g.count + 7) / 8, id = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
   if ((int)(blockIdx.x / 8) >= per_xcd || id >= g.count) return;
@@ -458,14 +458,17 @@ __global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
   const int64_t P0 = (int64_t)tp * MT, Q0 = (int64_t)tq * MT;
   if (P0 >= g.P || Q0 >= g.Q) return;   // a quarter behind the edge
   const int64_t rowb = g.pitch / 2, rows_s = g.pitch / MX_BLOCK, np = min(g.P - P0, (int64_t)MT), nq = min(g.Q - Q0, (int64_t)MT);
-  const int KT = (int)(g.pitch / 256), T = KT * g.nl * g.nr;
+  const int KT = g.steps, T = KT * g.nl * g.nr;
   __amdgpu_buffer_rsrc_t rsrcL, rsrcR;
   auto planes = [&](int pass) {
     rsrcL = rows_rsrc(g.L + (pass % g.nl) * g.planeL + P0 * rowb, np, rowb);
     rsrcR = rows_rsrc(g.R + (pass / g.nl) * g.planeR + Q0 * rowb, nq, rowb);
   };
   planes(0);
-  const __amdgpu_buffer_rsrc_t rsrcS = wave < 2 ? rows_rsrc(g.sL + P0 * rows_s, np, rows_s) : rows_rsrc(g.sR + Q0 * rows_s, nq, rows_s);
+  // waves 0, 1: L's scales, 2, 3: Rt's, 64 rows each; the second group has none to bring
+  const bool scales_l = (wave & 2) == 0;
+  const __amdgpu_buffer_rsrc_t rsrcS = scales_l ? rows_rsrc(g.sL + P0 * rows_s, np, rows_s) : rows_rsrc(g.sR + Q0 * rows_s, nq, rows_s);
+  const uint32_t offS = (uint32_t)(min((int64_t)((wave & 1) * 64 + lane), (scales_l ? np : nq) - 1) * rows_s);
   uint32_t offL[M_LD], offR[M_LD];
 #pragma unroll
   for (int j = 0; j < M_LD; ++j) {
@@ -473,17 +476,19 @@ __global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
     offL[j] = (uint32_t)(min((int64_t)row, np - 1) * rowb + at);   // rows past the edge re-read the last row
     offR[j] = (uint32_t)(min((int64_t)row, nq - 1) * rowb + at);
   }
-  const uint32_t offS = (uint32_t)(min((int64_t)((wave & 1) * 64 + lane), (wave < 2 ? np : nq) - 1) * rows_s);   // wave w: rows 64 w .. of L, then of Rt
-  int ld_t = 0, ld_k = 0, ld_pass = 0;
+  int ld_t = 0, ld_k = 0, ld_pass = 0, ld_pair = 0;
   auto request = [&]() {   // the next step; behind the last one zeros
     uint8_t* const st = smem + (ld_t & (M_RING - 1)) * M_STAGE;
     const bool in = ld_t < T;
+    if ((ld_k & 1) == 0) {
+      if (group == 0) MX_TO_LDS(rsrcS, smem + M_SC + (ld_pair & (M_RING - 1)) * M_SC_BYTES + wave * 1024, 16, in ? offS : PAST_THE_END, ld_k * 8);
+      ++ld_pair;
+    }
 #pragma unroll
     for (int j = 0; j < M_LD; ++j) {
       MX_TO_LDS(rsrcL, st + (wave * M_LD + j) * 1024, 16, in ? offL[j] : PAST_THE_END, ld_k * BKB);
       MX_TO_LDS(rsrcR, st + M_OP + (wave * M_LD + j) * 1024, 16, in ? offR[j] : PAST_THE_END, ld_k * BKB);
     }
-    if ((ld_t & 1) == 0) MX_TO_LDS(rsrcS, smem + M_SC + ((ld_t >> 1) & (M_RING - 1)) * M_SC_BYTES + wave * 1024, 16, in ? offS : PAST_THE_END, ld_k * 8);
     ++ld_t;
     if (++ld_k == KT) {
       ld_k = 0;
@@ -499,64 +504,77 @@ __global__ __launch_bounds__(256) void mx_gemm_mid_kernel(MxGemm g) {
 #pragma unroll
   for (int i = 0; i < M_RING - 1; ++i) request();
   uint32_t lessl = 0, lessr = 0;
-  int rd_k = 0, rd_pass = 0;
-  for (int t = 0; t < T; ++t) {
-    asm volatile("" ::: "memory");
-    // this wave's share of step t is there, and it is done reading step t - 1; behind the barrier that holds for all
-    constexpr int left = (M_RING - 2) * 2 * M_LD + 1;   // of the two steps behind it one brings scales
-    static_assert(M_RING == 4, "so many steps");
-    __builtin_amdgcn_s_waitcnt(0x0070 | (left & 15) | ((left >> 4) << 14));
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    request();
-    const uint8_t* const st = smem + (t & (M_RING - 1)) * M_STAGE;
-    const uint8_t *const sL = st + (wp + l32) * BKB, *const sR = st + M_OP + (wq + l32) * BKB;
-    const uint8_t* const sc = smem + M_SC + ((t >> 1) & (M_RING - 1)) * M_SC_BYTES + (t & 1) * 8 + h * 4;
-    uint32_t sl[2], sr[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      sl[j] = *reinterpret_cast<const uint32_t*>(sc + (wp + j * 32 + l32) * 16) - lessl;
-      sr[j] = *reinterpret_cast<const uint32_t*>(sc + (MT + wq + j * 32 + l32) * 16) - lessr;
-    }
-    u32x4 fl[4][2], fr[4][2];
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int slot = ((4 * h + s) ^ key) * 16;
+  int rd_k = 0, rd_pass = 0, rd_pair = 0;
+  const int slot0 = ((4 * h + 2 * group) ^ key) * 16, slot1 = ((4 * h + 2 * group + 1) ^ key) * 16;   // this group's two slices
+  auto slices = [&](auto gc) {   // S: the first of the two
+    constexpr int S = 2 * decltype(gc)::value;
+    for (int t = 0; t < T; ++t) {
+      asm volatile("" ::: "memory");
+      // this wave's share of step t is there (at most the two steps behind it are not), and it is done reading step t - 1; behind the
+      // barrier that holds for all
+      constexpr int left = (M_RING - 2) * 2 * M_LD;
+      __builtin_amdgcn_s_waitcnt(0x0070 | (left & 15) | ((left >> 4) << 14));
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      request();
+      const uint8_t* const st = smem + (t & (M_RING - 1)) * M_STAGE;
+      const uint8_t *const sL = st + (wp + l32) * BKB, *const sR = st + M_OP + (wq + l32) * BKB;
+      const uint8_t* const sc = smem + M_SC + (rd_pair & (M_RING - 1)) * M_SC_BYTES + (rd_k & 1) * 8 + h * 4;
+      uint32_t sl[2], sr[2];
+      u32x4 fl[2][2], fr[2][2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        fr[s][j] = *reinterpret_cast<const u32x4*>(sR + slot + j * 32 * BKB);
-        fl[s][j] = *reinterpret_cast<const u32x4*>(sL + slot + j * 32 * BKB);
+        sl[j] = *reinterpret_cast<const uint32_t*>(sc + (wp + j * 32 + l32) * 16) - lessl;
+        sr[j] = *reinterpret_cast<const uint32_t*>(sc + (MT + wq + j * 32 + l32) * 16) - lessr;
+        fr[0][j] = *reinterpret_cast<const u32x4*>(sR + slot0 + j * 32 * BKB);
+        fl[0][j] = *reinterpret_cast<const u32x4*>(sL + slot0 + j * 32 * BKB);
       }
-    }
-    __builtin_amdgcn_sched_barrier(0);   // all requested before the first product
-    static_for<4>([&](auto sc) {
-      constexpr int s = decltype(sc)::value;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        fr[1][j] = *reinterpret_cast<const u32x4*>(sR + slot1 + j * 32 * BKB);
+        fl[1][j] = *reinterpret_cast<const u32x4*>(sL + slot1 + j * 32 * BKB);
+      }
+      __builtin_amdgcn_sched_barrier(0);   // all requested before the first product
 #pragma unroll
       for (int qi = 0; qi < 2; ++qi)
 #pragma unroll
-        for (int pj = 0; pj < 2; ++pj) acc[qi][pj] = mx_mfma<s>(fr[s][qi], fl[s][pj], acc[qi][pj], sr[qi], sl[pj]);
-    });
-    if (++rd_k == KT) {
-      rd_k = 0;
-      ++rd_pass;
-      lessl = rd_pass % g.nl ? MX_EIGHTH : 0u;
-      lessr = rd_pass / g.nl ? MX_EIGHTH : 0u;
+        for (int pj = 0; pj < 2; ++pj) acc[qi][pj] = mx_mfma<S>(fr[0][qi], fl[0][pj], acc[qi][pj], sr[qi], sl[pj]);
+#pragma unroll
+      for (int qi = 0; qi < 2; ++qi)
+#pragma unroll
+        for (int pj = 0; pj < 2; ++pj) acc[qi][pj] = mx_mfma<S + 1>(fr[1][qi], fl[1][pj], acc[qi][pj], sr[qi], sl[pj]);
+      rd_pair += rd_k & 1;
+      if (++rd_k == KT) {
+        rd_pair += rd_k & 1;
+        rd_k = 0;
+        ++rd_pass;
+        lessl = rd_pass % g.nl ? MX_EIGHTH : 0u;
+        lessr = rd_pass / g.nl ? MX_EIGHTH : 0u;
+      }
     }
-  }
+  };
+  if (group == 0) slices(std::integral_constant<int, 0>{});
+  else slices(std::integral_constant<int, 1>{});
   __builtin_amdgcn_s_waitcnt(0);   // no load may land over the sums
   __syncthreads();
   float* const tile = reinterpret_cast<float*>(smem);
+  auto each = [&](auto&& f) {
 #pragma unroll
-  for (int pj = 0; pj < 2; ++pj)
+    for (int pj = 0; pj < 2; ++pj)
 #pragma unroll
-    for (int qi = 0; qi < 2; ++qi)
+      for (int qi = 0; qi < 2; ++qi)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const mx_f32x16& c = acc[qi][pj];
-        *reinterpret_cast<f32x4*>(&tile[(wp + pj * 32 + l32) * (MT + 4) + wq + qi * 32 + b * 8 + h * 4]) = f32x4{c[b * 4], c[b * 4 + 1], c[b * 4 + 2], c[b * 4 + 3]};
-      }
+        for (int b = 0; b < 4; ++b) {
+          const mx_f32x16& c = acc[qi][pj];
+          f(f32x4{c[b * 4], c[b * 4 + 1], c[b * 4 + 2], c[b * 4 + 3]},
+            *reinterpret_cast<f32x4*>(&tile[(wp + pj * 32 + l32) * (MT + 4) + wq + qi * 32 + b * 8 + h * 4]));
+        }
+  };
+  if (group == 1) each([](const f32x4& v, f32x4& at) { at = v; });
   __syncthreads();
-  finish_tile<MT, 256, OUT_BF16>(g, tile, P0, Q0);
+  if (group == 0) each([](const f32x4& v, f32x4& at) { at = v + at; });
+  __syncthreads();
+  finish_tile<MT, M_WAVES * 64, OUT_BF16>(g, tile, P0, Q0);
 }
 
 // ---- 32 x 32, the contraction shared ---------------------------------------------------------------------------------------------
@@ -579,7 +597,7 @@ __global__ __launch_bounds__(256) void mx_gemm_split_kernel(MxGemm g) {
   if ((int)(blockIdx.x / 8) >= per_xcd || id >= g.count) return;
   const int64_t P0 = (int64_t)(id % g.tiles_p) * ST, Q0 = (int64_t)(id / g.tiles_p) * ST;
   const int64_t rowb = g.pitch / 2, rows_s = g.pitch / MX_BLOCK, np = min(g.P - P0, (int64_t)ST), nq = min(g.Q - Q0, (int64_t)ST);
-  const int KT = (int)(g.pitch / 256), T = KT * g.nl * g.nr, steps = (T - wave + WAVES - 1) / WAVES;   // of this wave
+  const int KT = g.steps, T = KT * g.nl * g.nr, steps = (T - wave + WAVES - 1) / WAVES;   // of this wave
   const __amdgpu_buffer_rsrc_t rsrcSL = rows_rsrc(g.sL + P0 * rows_s, np, rows_s), rsrcSR = rows_rsrc(g.sR + Q0 * rows_s, nq, rows_s);
   uint32_t offL[S_LD], offR[S_LD];
 #pragma unroll
@@ -666,11 +684,11 @@ int launch(MxGemm& g, MxTiling t, int n_cu, hipStream_t s) {
     if (t.rest) {
       m.first = g.count;
       m.count = 4 * t.rest;
-      hipLaunchKernelGGL((mx_gemm_mid_kernel<OUT_BF16>), dealt(m.count), dim3(256), 0, s, m);
+      hipLaunchKernelGGL((mx_gemm_mid_kernel<OUT_BF16>), dealt(m.count), dim3(M_WAVES * 64), 0, s, m);
     }
   } else if (t.tile == 128) {
     set_tiles(g, 128);
-    hipLaunchKernelGGL((mx_gemm_mid_kernel<OUT_BF16>), dealt(g.count), dim3(256), 0, s, g);
+    hipLaunchKernelGGL((mx_gemm_mid_kernel<OUT_BF16>), dealt(g.count), dim3(M_WAVES * 64), 0, s, g);
   } else if (t.tile == 32) {
     set_tiles(g, 32);
     if (g.count <= n_cu) hipLaunchKernelGGL((mx_gemm_split_kernel<OUT_BF16, 4>), dealt(g.count), dim3(256), 0, s, g);
@@ -698,6 +716,7 @@ int mx_launch_gemm(const uint8_t* L, const uint8_t* sL, int bits_l, const uint8_
   g.out = out;
   g.P = P; g.Q = Q; g.ldo = ldo;
   g.pitch = mx_pitch_of(Kc);
+  g.steps = (int)((Kc + 255) / 256);
   g.planeL = P * (g.pitch / 2);
   g.planeR = Q * (g.pitch / 2);
   g.nl = bits_l / 4;
