@@ -30,7 +30,7 @@ int fp8_host_round_codes(const float* x_host, int64_t n, uint8_t* codes_host);
 int fp4_device_round_codes(const float* x, int64_t n, uint8_t* codes, void* stream);
 int fp4_device_round_sweep(unsigned long long* mismatches, void* stream);
 
-/* mx_gemm by one kind of tile: 16 (few tokens), 32 (waves share the contraction), 64, 128 or 256; 0: by the rule that mx_gemm follows.  A
+/* mx_gemm by one kind of tile: 16 (few tokens), 32 (waves share the contraction), 64, 128, 192 (256 rows) or 256; 0: by the rule that mx_gemm follows.  A
  * contraction of no length goes by the rule.
  * mx_gemm_tile: what the rule says for [P x Q] over Kc on a device with that many compute units (host arithmetic, no GPU); with 256,
  * *last_round (may be NULL) is the number of tiles of the last round that are cut into 128 x 128 ones. */

@@ -686,7 +686,7 @@ def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, a
 
 
 def mx_gemm_by_tile(l: MxTensor, rt: MxTensor, tile: int, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """mx_gemm by one kind of tile (16, 32, 64, 128, 256), for tests and measuring; addend has the output's leading dimension."""
+    """mx_gemm by one kind of tile (16, 32, 64, 128, 192, 256), for tests and measuring; addend has the output's leading dimension."""
     out = _out(None, (l.lines, rt.lines), out_dtype, l.codes, "out")
     _check(lib().mx_gemm_by_tile(l.ref, rt.ref, _ptr(addend), _ptr(out), _dt(out), _ld(out, "out"), tile, _stream()), "mx_gemm_by_tile")
     return out

@@ -77,7 +77,6 @@ __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
     const int pl = pass % g.nl, pr = pass / g.nl;
     const uint8_t *l = g.L + pl * g.planeL + p * (g.pitch / 2) + h * 64, *r = g.R + pr * g.planeR + q * (g.pitch / 2) + h * 64;
     const uint32_t lessl = pl ? MX_EIGHTH : 0u, lessr = pr ? MX_EIGHTH : 0u;
-#pragma unroll 2
     for (int k = 0; k < g.steps; ++k) {   // 256 codes, one word of scales
       const uint32_t bl = sl[2 * k + h] - lessl, br = sr[2 * k + h] - lessr;
       const u32x4 *lv = reinterpret_cast<const u32x4*>(l + k * 128), *rv = reinterpret_cast<const u32x4*>(r + k * 128);
@@ -96,23 +95,28 @@ __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
   }
 }
 
-// ---- 256 x 256 ------------------------------------------------------------------------------------------------------------------
-// For outputs that go round the chip in 256 x 256 tiles.  Eight waves (2 along rows x 4 along columns, 128 x 64 each), persistent
-// workgroups, K step 256 codes.  Operands come into two LDS stages by direct-to-LDS loads, the scales of two steps at a time (16 bytes of
-// every row, one load a thread) into a ring of two of their own; the two waves of a SIMD alternate between a compute phase (16 matrix
-// instructions) and a memory phase (the fragments of the next two slices, and once a step its share of the loads of the step after
-// next), half a period apart.  The next tile's first stage travels while a tile's epilogue runs.
+// ---- 256 x 256, 256 x 192 -------------------------------------------------------------------------------------------------------
+// For outputs that go round the chip in such tiles.  Eight waves, PJ x QI blocks of 32 x 32 each (256 columns: 2 along rows x 4 along columns,
+// 128 x 64 each; 192: 4 x 2, 64 x 96 each), persistent workgroups, K step 256 codes.  Operands come into two LDS stages by direct-to-LDS
+// loads, the scales of two steps at a time (16 bytes of every row, one load a thread) into a ring of two of their own; the two waves of a
+// SIMD alternate between a compute phase (the matrix instructions of two slices) and a memory phase (the fragments of the next two
+// slices, and once a step its share of the loads of the step after next), half a period apart.  The next tile's first stage travels while
+// a tile's epilogue runs.
 // An operand stage: row r takes bytes [128 r, 128 r + 128), its 16-byte chunk c sits in slot c ^ ((r >> 1) & 7), so that sixteen rows
-// reading one chunk touch sixteen different bank groups.  Bound: the matrix cores at the clock that random operands leave them.
-constexpr int BT = 256, BKB = 128;
+// reading one chunk touch sixteen different bank groups.  Bound: the matrix cores at the clock that random operands leave them, and LDS,
+// which a step of 256 x 256 keeps busy as long as the matrix cores (192 KiB of fragments and 64 KiB of arrivals at 128 bytes a cycle).
+constexpr int BP = 256, BKB = 128;
 constexpr int BWAVES = 8;
-constexpr int BLD = BT * 8 / (BWAVES * 64);      // 16-byte chunks a thread, operand and step
-constexpr int QI = 2, PJ = 4;                    // 32 x 32 blocks of a wave
-constexpr int OP_BYTES = BT * BKB, STAGE_BYTES = 2 * OP_BYTES;
-constexpr int EPI_LD = QI * 32 + 4, EPI_BYTES = BWAVES * 32 * EPI_LD * 4;
-constexpr int SC_BASE = STAGE_BYTES + (EPI_BYTES > STAGE_BYTES ? EPI_BYTES : STAGE_BYTES), SC_BYTES = 2 * BT * 16;   // the epilogue's rows lie over stage 1
-constexpr int BIG_SMEM = SC_BASE + 2 * SC_BYTES;
-static_assert(BIG_SMEM <= 160 * 1024, "LDS budget");
+template <int BQ> struct BigShape {
+  static constexpr int WP = BQ == 256 ? 2 : 4;                   // waves along rows
+  static constexpr int PJ = BP / 32 / WP, QI = BQ / 32 / (BWAVES / WP);
+  static constexpr int LDL = BP * 8 / (BWAVES * 64), LDR = BQ * 8 / (BWAVES * 64);   // 16-byte chunks a thread and step
+  static constexpr int OP_L = BP * BKB, STAGE = (BP + BQ) * BKB;
+  static constexpr int EROWS = QI == 2 ? 32 : 16, ELD = QI * 32 + 4, EPI = BWAVES * EROWS * ELD * 4;   // rows parked at a time, floats a row
+  static constexpr int SC_BASE = STAGE + (EPI > STAGE ? EPI : STAGE), SC = 2 * 256 * 16;   // the epilogue's rows lie over stage 1
+  static constexpr int SMEM = SC_BASE + 2 * SC;
+  static_assert(SMEM <= 160 * 1024, "LDS budget");
+};
 constexpr int GROUP_P = 8;   // tile rows side by side
 
 FP4_D void tile_at(const MxGemm& g, int id, int& tp, int& tq) {
@@ -130,8 +134,14 @@ FP4_D const uint8_t* uniform_ptr(const uint8_t* p) {
 FP4_D __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* p, int64_t rows, int64_t pitch) {   // over so many rows; they stay below 2^30 bytes
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(uniform_ptr(p)), 0, __builtin_amdgcn_readfirstlane((int)(rows * pitch)), 0x00020000);
 }
-#define MX_TO_LDS(rsrc, lds, width, voff, soff) \
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds), width, voff, soff, 0, 0)
+// global -> LDS without passing through registers, a wave's lanes one behind another from `lds` on.  (Functions of their own and no templates:
+// with arguments that depend on a template parameter the builtin makes the compiler drop the kernel's host stub.)
+FP4_D void to_lds16(__amdgpu_buffer_rsrc_t rsrc, uint8_t* lds, uint32_t voff, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, voff, soff, 0, 0);
+}
+FP4_D void to_lds4(__amdgpu_buffer_rsrc_t rsrc, uint8_t* lds, uint32_t voff, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 4, voff, soff, 0, 0);
+}
 
 // Eight columns of a row from q on, y without the addend.
 template <bool OUT_BF16>
@@ -165,12 +175,14 @@ FP4_D void load_addend8(const MxGemm& g, int64_t at, int64_t left, float (&a)[8]
   }
 }
 
-template <bool OUT_BF16>
+template <int BQ, bool OUT_BF16>
 __global__ __launch_bounds__(BWAVES * 64) void mx_gemm_big_kernel(MxGemm g) {
-  __shared__ __attribute__((aligned(16))) uint8_t smem[BIG_SMEM];
+  using S = BigShape<BQ>;
+  constexpr int PJ = S::PJ, QI = S::QI;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[S::SMEM];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wave_p = wave & 1, wave_q = wave >> 1;
+  const int wave_p = wave % S::WP, wave_q = wave / S::WP;
   const int l32 = lane & 31, h = lane >> 5;
   // each XCD a contiguous run of tiles, so that those that share rows meet in one L2
   const int per_xcd = (g.count + 7) / 8;
@@ -183,49 +195,49 @@ __global__ __launch_bounds__(BWAVES * 64) void mx_gemm_big_kernel(MxGemm g) {
   const int KT = (int)(g.pitch / 256), T = KT * g.nl * g.nr;   // steps of a pass (even), of all passes
   int64_t P0 = 0, Q0 = 0;
   __amdgpu_buffer_rsrc_t rsrcL, rsrcR, rsrcS;
-  uint32_t offL[BLD], offR[BLD], offS;
+  uint32_t offL[S::LDL], offR[S::LDR], offS;
   int ld_k = 0, ld_pass = 0, sc_k = 0;   // the step in its pass that is requested next, and the pair of steps whose scales are
   auto planes = [&](int pass) {
-    rsrcL = rows_rsrc(g.L + (pass % g.nl) * g.planeL + P0 * rowb, min(g.P - P0, (int64_t)BT), rowb);
-    rsrcR = rows_rsrc(g.R + (pass / g.nl) * g.planeR + Q0 * rowb, min(g.Q - Q0, (int64_t)BT), rowb);
+    rsrcL = rows_rsrc(g.L + (pass % g.nl) * g.planeL + P0 * rowb, min(g.P - P0, (int64_t)BP), rowb);
+    rsrcR = rows_rsrc(g.R + (pass / g.nl) * g.planeR + Q0 * rowb, min(g.Q - Q0, (int64_t)BQ), rowb);
   };
   auto tile_scalars = [&](int id) {
     int tp, tq;
     tile_at(g, id, tp, tq);
-    P0 = (int64_t)tp * BT;
-    Q0 = (int64_t)tq * BT;
+    P0 = (int64_t)tp * BP;
+    Q0 = (int64_t)tq * BQ;
     ld_k = ld_pass = sc_k = 0;
     planes(0);
-    rsrcS = wave < 4 ? rows_rsrc(g.sL + P0 * rows_s, min(g.P - P0, (int64_t)BT), rows_s) : rows_rsrc(g.sR + Q0 * rows_s, min(g.Q - Q0, (int64_t)BT), rows_s);
+    rsrcS = wave < 4 ? rows_rsrc(g.sL + P0 * rows_s, min(g.P - P0, (int64_t)BP), rows_s) : rows_rsrc(g.sR + Q0 * rows_s, min(g.Q - Q0, (int64_t)BQ), rows_s);
   };
   // rebuilt where they are needed from a copy of the lane id that the optimizer cannot see through: kept across the epilogue they
   // would cost registers there
   auto tile_offsets = [&]() {
     int ln = lane;
     asm volatile("" : "+v"(ln));
+    auto offset = [&](int row, int64_t first, int64_t rows) {   // of a lane's chunk; rows past the edge re-read the last row
+      return (uint32_t)((min(first + row, rows - 1) - first) * rowb + ((ln & 7) ^ ((row >> 1) & 7)) * 16);
+    };
 #pragma unroll
-    for (int j = 0; j < BLD; ++j) {
-      const int row = 8 * (wave * BLD + j) + (ln >> 3);
-      const int chunk = (ln & 7) ^ ((row >> 1) & 7);
-      offL[j] = (uint32_t)((min(P0 + row, g.P - 1) - P0) * rowb + chunk * 16);   // rows past the edge re-read the last row
-      offR[j] = (uint32_t)((min(Q0 + row, g.Q - 1) - Q0) * rowb + chunk * 16);
-    }
+    for (int j = 0; j < S::LDL; ++j) offL[j] = offset(8 * (wave * S::LDL + j) + (ln >> 3), P0, g.P);
+#pragma unroll
+    for (int j = 0; j < S::LDR; ++j) offR[j] = offset(8 * (wave * S::LDR + j) + (ln >> 3), Q0, g.Q);
     const int row = (wave & 3) * 64 + ln;
     offS = (uint32_t)(wave < 4 ? (min(P0 + row, g.P - 1) - P0) * rows_s : (min(Q0 + row, g.Q - 1) - Q0) * rows_s);
   };
   auto load_step = [&](int buf) {
 #pragma unroll
-    for (int j = 0; j < BLD; ++j) {
-      MX_TO_LDS(rsrcL, smem + buf * STAGE_BYTES + (wave * BLD + j) * 1024, 16, offL[j], ld_k * BKB);
-      MX_TO_LDS(rsrcR, smem + buf * STAGE_BYTES + OP_BYTES + (wave * BLD + j) * 1024, 16, offR[j], ld_k * BKB);
+    for (int j = 0; j < S::LDL; ++j) {
+      to_lds16(rsrcL, smem + buf * S::STAGE + (wave * S::LDL + j) * 1024, offL[j], ld_k * BKB);
+      if (j < S::LDR) to_lds16(rsrcR, smem + buf * S::STAGE + S::OP_L + (wave * S::LDR + j) * 1024, offR[j < S::LDR ? j : 0], ld_k * BKB);
     }
     if (++ld_k == KT) {
       ld_k = 0;
       if (++ld_pass < g.nl * g.nr) planes(ld_pass);
     }
   };
-  auto load_scales = [&](int buf) {   // wave w: rows 64 w .. of L, then of Rt
-    MX_TO_LDS(rsrcS, smem + SC_BASE + buf * SC_BYTES + wave * 1024, 16, offS, sc_k * 16);
+  auto load_scales = [&](int buf) {   // wave w: rows 64 w .. of L, then of Rt (those behind a tile's 192 arrive as zeros)
+    to_lds16(rsrcS, smem + S::SC_BASE + buf * S::SC + wave * 1024, offS, sc_k * 16);
     if (++sc_k == KT / 2) sc_k = 0;
   };
 
@@ -234,26 +246,26 @@ __global__ __launch_bounds__(BWAVES * 64) void mx_gemm_big_kernel(MxGemm g) {
   int frag_l[4], frag_r[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
-    frag_l[s] = (wave_p * 128 + l32) * BKB + ((4 * h + s) ^ key) * 16;
-    frag_r[s] = OP_BYTES + (wave_q * 64 + l32) * BKB + ((4 * h + s) ^ key) * 16;
+    frag_l[s] = (wave_p * (PJ * 32) + l32) * BKB + ((4 * h + s) ^ key) * 16;
+    frag_r[s] = S::OP_L + (wave_q * (QI * 32) + l32) * BKB + ((4 * h + s) ^ key) * 16;
   }
-  const int scale_l = SC_BASE + (wave_p * 128 + l32) * 16 + h * 4, scale_r = SC_BASE + BT * 16 + (wave_q * 64 + l32) * 16 + h * 4;
+  const int scale_l = S::SC_BASE + (wave_p * (PJ * 32) + l32) * 16 + h * 4, scale_r = S::SC_BASE + BP * 16 + (wave_q * (QI * 32) + l32) * 16 + h * 4;
   u32x4 fl[2][PJ], fr[2][QI];
   uint32_t sl[PJ], sr[QI], lessl = 0, lessr = 0;
   auto read_frags = [&](int buf, int half) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
 #pragma unroll
-      for (int j = 0; j < QI; ++j) fr[s][j] = *reinterpret_cast<const u32x4*>(smem + buf * STAGE_BYTES + frag_r[2 * half + s] + j * 32 * BKB);
+      for (int j = 0; j < QI; ++j) fr[s][j] = *reinterpret_cast<const u32x4*>(smem + buf * S::STAGE + frag_r[2 * half + s] + j * 32 * BKB);
 #pragma unroll
-      for (int j = 0; j < PJ; ++j) fl[s][j] = *reinterpret_cast<const u32x4*>(smem + buf * STAGE_BYTES + frag_l[2 * half + s] + j * 32 * BKB);
+      for (int j = 0; j < PJ; ++j) fl[s][j] = *reinterpret_cast<const u32x4*>(smem + buf * S::STAGE + frag_l[2 * half + s] + j * 32 * BKB);
     }
   };
   auto read_scales = [&](int buf, int parity) {
 #pragma unroll
-    for (int j = 0; j < QI; ++j) sr[j] = *reinterpret_cast<const uint32_t*>(smem + buf * SC_BYTES + scale_r + parity * 8 + j * 512) - lessr;
+    for (int j = 0; j < QI; ++j) sr[j] = *reinterpret_cast<const uint32_t*>(smem + buf * S::SC + scale_r + parity * 8 + j * 512) - lessr;
 #pragma unroll
-    for (int j = 0; j < PJ; ++j) sl[j] = *reinterpret_cast<const uint32_t*>(smem + buf * SC_BYTES + scale_l + parity * 8 + j * 512) - lessl;
+    for (int j = 0; j < PJ; ++j) sl[j] = *reinterpret_cast<const uint32_t*>(smem + buf * S::SC + scale_l + parity * 8 + j * 512) - lessl;
   };
   mx_f32x16 acc[QI][PJ];
 
@@ -273,7 +285,7 @@ __global__ __launch_bounds__(BWAVES * 64) void mx_gemm_big_kernel(MxGemm g) {
     load_step(1);
     load_scales(1);
     {
-      constexpr int n = 2 * BLD + 1;   // all but what was just issued
+      constexpr int n = S::LDL + S::LDR + 1;   // all but what was just issued
       __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | ((n >> 4) << 14));
     }
     __builtin_amdgcn_s_barrier();   // a bare one: the fence of __syncthreads() would wait for the second stage too
@@ -302,7 +314,9 @@ __global__ __launch_bounds__(BWAVES * 64) void mx_gemm_big_kernel(MxGemm g) {
 #pragma unroll
             for (int pj = 0; pj < PJ; ++pj) acc[qi][pj] = mx_mfma<2 * half + 1>(fr[1][qi], fl[1][pj], acc[qi][pj], sr[qi], sl[pj]);
 #pragma unroll
-          for (int qi = 0; qi < QI; ++qi) asm volatile("" : "+v"(acc[qi][0]), "+v"(acc[qi][1]), "+v"(acc[qi][2]), "+v"(acc[qi][3]));
+          for (int qi = 0; qi < QI; ++qi)
+#pragma unroll
+            for (int pj = 0; pj < PJ; pj += 2) asm volatile("" : "+v"(acc[qi][pj]), "+v"(acc[qi][pj + 1]));
           __builtin_amdgcn_s_setprio(0);
           __builtin_amdgcn_sched_barrier(0);
           if constexpr (half == 1) {   // the next step is first read in this memory phase: its loads have landed by the barrier before
@@ -348,45 +362,41 @@ __global__ __launch_bounds__(BWAVES * 64) void mx_gemm_big_kernel(MxGemm g) {
       load_scales(0);
     }
 
-    // Epilogue: 32 rows at a time through the wave's own LDS, so that they are written (and the addend is read) along rows.  Loads and
-    // stores count on one in-order counter, so the addend of all 32 rows is requested before the first of them is stored.
-    float* const park = reinterpret_cast<float*>(smem + STAGE_BYTES) + wave * 32 * EPI_LD;
+    // Epilogue: EROWS rows at a time through the wave's own LDS, so that they are written (and the addend is read) along rows.  Loads and
+    // stores count on one in-order counter, so the addend of all these rows is requested before the first of them is stored.
+    float* const park = reinterpret_cast<float*>(smem + S::STAGE) + wave * S::EROWS * S::ELD;
     int ln = lane;
     asm volatile("" : "+v"(ln));
-    const int64_t q0 = eQ0 + wave_q * 64 + (ln & 7) * 8;
-    const int64_t left = g.Q - q0;
-    static_for<PJ>([&](auto pc) {
-      constexpr int pj = decltype(pc)::value;
+    constexpr int UPR = QI * 4, NP = S::EROWS * UPR / 64, PARTS = 32 / S::EROWS;   // 8-column units a row, units a lane
+    static_for<PJ * PARTS>([&](auto pc) {
+      constexpr int pj = decltype(pc)::value / PARTS, part = decltype(pc)::value % PARTS;
       __builtin_amdgcn_sched_barrier(0);
-      static_for<4 * QI>([&](auto ic) {
-        constexpr int qi = decltype(ic)::value / 4, b = decltype(ic)::value % 4;
-        const mx_f32x16& c = acc[qi][pj];
-        *reinterpret_cast<f32x4*>(park + (ln & 31) * EPI_LD + qi * 32 + b * 8 + (ln >> 5) * 4) = f32x4{c[b * 4], c[b * 4 + 1], c[b * 4 + 2], c[b * 4 + 3]};
-      });
+      if (PARTS == 1 || ((ln & 31) / S::EROWS) == part) {
+        static_for<4 * QI>([&](auto ic) {
+          constexpr int qi = decltype(ic)::value / 4, b = decltype(ic)::value % 4;
+          const mx_f32x16& c = acc[qi][pj];
+          *reinterpret_cast<f32x4*>(park + (ln & (S::EROWS - 1)) * S::ELD + qi * 32 + b * 8 + (ln >> 5) * 4) = f32x4{c[b * 4], c[b * 4 + 1], c[b * 4 + 2], c[b * 4 + 3]};
+        });
+      }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      const int64_t p0 = eP0 + wave_p * 128 + pj * 32 + (ln >> 3);
-      float a[4][8];
-      if (g.addend) {
+      const int64_t p0 = eP0 + (wave_p * PJ + pj) * 32 + part * S::EROWS, q0 = eQ0 + wave_q * (QI * 32);
+      float a[NP][8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (p0 + i * 8 < g.P && left > 0) load_addend8(g, (p0 + i * 8) * g.ldo + q0, left, a[i]);
-          else
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a[i][e] = 0.0f;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < NP; ++i) {
+        const int u = i * 64 + ln, row = u / UPR, col = u % UPR * 8;
+        if (g.addend && p0 + row < g.P && q0 + col < g.Q) load_addend8(g, (p0 + row) * g.ldo + q0 + col, g.Q - q0 - col, a[i]);
+        else
 #pragma unroll
           for (int e = 0; e < 8; ++e) a[i][e] = 0.0f;
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float* r = park + ((ln >> 3) + i * 8) * EPI_LD + (ln & 7) * 8;
-        const f32x4 u = *reinterpret_cast<const f32x4*>(r), v = *reinterpret_cast<const f32x4*>(r + 4);
-        const float y[8] = {u.x + a[i][0], u.y + a[i][1], u.z + a[i][2], u.w + a[i][3], v.x + a[i][4], v.y + a[i][5], v.z + a[i][6], v.w + a[i][7]};
-        if (p0 + i * 8 < g.P && left > 0) store8<OUT_BF16>(g, (p0 + i * 8) * g.ldo + q0, left, y);
+      for (int i = 0; i < NP; ++i) {
+        const int u = i * 64 + ln, row = u / UPR, col = u % UPR * 8;
+        const float* r = park + row * S::ELD + col;
+        const f32x4 x = *reinterpret_cast<const f32x4*>(r), v = *reinterpret_cast<const f32x4*>(r + 4);
+        const float y[8] = {x.x + a[i][0], x.y + a[i][1], x.z + a[i][2], x.w + a[i][3], v.x + a[i][4], v.y + a[i][5], v.z + a[i][6], v.w + a[i][7]};
+        if (p0 + row < g.P && q0 + col < g.Q) store8<OUT_BF16>(g, (p0 + row) * g.ldo + q0 + col, g.Q - q0 - col, y);
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -481,13 +491,13 @@ __global__ __launch_bounds__(M_WAVES * 64) void mx_gemm_mid_kernel(MxGemm g) {
     uint8_t* const st = smem + (ld_t & (M_RING - 1)) * M_STAGE;
     const bool in = ld_t < T;
     if ((ld_k & 1) == 0) {
-      if (group == 0) MX_TO_LDS(rsrcS, smem + M_SC + (ld_pair & (M_RING - 1)) * M_SC_BYTES + wave * 1024, 16, in ? offS : PAST_THE_END, ld_k * 8);
+      if (group == 0) to_lds16(rsrcS, smem + M_SC + (ld_pair & (M_RING - 1)) * M_SC_BYTES + wave * 1024, in ? offS : PAST_THE_END, ld_k * 8);
       ++ld_pair;
     }
 #pragma unroll
     for (int j = 0; j < M_LD; ++j) {
-      MX_TO_LDS(rsrcL, st + (wave * M_LD + j) * 1024, 16, in ? offL[j] : PAST_THE_END, ld_k * BKB);
-      MX_TO_LDS(rsrcR, st + M_OP + (wave * M_LD + j) * 1024, 16, in ? offR[j] : PAST_THE_END, ld_k * BKB);
+      to_lds16(rsrcL, st + (wave * M_LD + j) * 1024, in ? offL[j] : PAST_THE_END, ld_k * BKB);
+      to_lds16(rsrcR, st + M_OP + (wave * M_LD + j) * 1024, in ? offR[j] : PAST_THE_END, ld_k * BKB);
     }
     ++ld_t;
     if (++ld_k == KT) {
@@ -616,11 +626,11 @@ __global__ __launch_bounds__(256) void mx_gemm_split_kernel(MxGemm g) {
     const __amdgpu_buffer_rsrc_t rsrcR = rows_rsrc(g.R + (pass / g.nl) * g.planeR + Q0 * rowb, nq, rowb);
 #pragma unroll
     for (int j = 0; j < S_LD; ++j) {
-      MX_TO_LDS(rsrcL, st + j * 1024, 16, in ? offL[j] : PAST_THE_END, k * BKB);
-      MX_TO_LDS(rsrcR, st + S_OP + j * 1024, 16, in ? offR[j] : PAST_THE_END, k * BKB);
+      to_lds16(rsrcL, st + j * 1024, in ? offL[j] : PAST_THE_END, k * BKB);
+      to_lds16(rsrcR, st + S_OP + j * 1024, in ? offR[j] : PAST_THE_END, k * BKB);
     }
-    MX_TO_LDS(rsrcSL, st + 2 * S_OP, 4, in ? offSL : PAST_THE_END, k * 8);
-    MX_TO_LDS(rsrcSR, st + 2 * S_OP + 256, 4, in ? offSR : PAST_THE_END, k * 8);
+    to_lds4(rsrcSL, st + 2 * S_OP, in ? offSL : PAST_THE_END, k * 8);
+    to_lds4(rsrcSR, st + 2 * S_OP + 256, in ? offSR : PAST_THE_END, k * 8);
   };
   const int key = (l32 >> 1) & 7;
   mx_f32x16 acc;
@@ -666,31 +676,35 @@ __global__ __launch_bounds__(256) void mx_gemm_split_kernel(MxGemm g) {
   if (P0 + row < g.P && Q0 + col < g.Q) mx_store4<OUT_BF16>(g.out, g.addend, (P0 + row) * g.ldo + Q0 + col, g.Q - Q0 - col, y);
 }
 
-void set_tiles(MxGemm& g, int tile) {
-  g.tiles_p = (int)((g.P + tile - 1) / tile);
-  g.tiles_q = (int)((g.Q + tile - 1) / tile);
+void set_tiles(MxGemm& g, int rows, int cols) {
+  g.tiles_p = (int)((g.P + rows - 1) / rows);
+  g.tiles_q = (int)((g.Q + cols - 1) / cols);
   g.first = 0;
   g.count = g.tiles_p * g.tiles_q;
 }
 
 template <bool OUT_BF16>
 int launch(MxGemm& g, MxTiling t, int n_cu, hipStream_t s) {
+  const auto resident = [&](int count) { return dim3((unsigned)std::min((count + 7) / 8 * 8, n_cu / 8 * 8)); };   // a workgroup a CU
   const auto dealt = [](int count) { return dim3((unsigned)((count + 7) / 8 * 8)); };   // a run of tiles for each XCD
   if (t.tile == 256) {
-    set_tiles(g, 256);
+    set_tiles(g, 256, 256);
     MxGemm m = g;
     g.count -= t.rest;
-    hipLaunchKernelGGL((mx_gemm_big_kernel<OUT_BF16>), dim3((unsigned)std::min((g.count + 7) / 8 * 8, n_cu / 8 * 8)), dim3(BWAVES * 64), 0, s, g);
+    hipLaunchKernelGGL((mx_gemm_big_kernel<256, OUT_BF16>), resident(g.count), dim3(BWAVES * 64), 0, s, g);
     if (t.rest) {
       m.first = g.count;
       m.count = 4 * t.rest;
       hipLaunchKernelGGL((mx_gemm_mid_kernel<OUT_BF16>), dealt(m.count), dim3(M_WAVES * 64), 0, s, m);
     }
+  } else if (t.tile == 192) {
+    set_tiles(g, 256, 192);
+    hipLaunchKernelGGL((mx_gemm_big_kernel<192, OUT_BF16>), resident(g.count), dim3(BWAVES * 64), 0, s, g);
   } else if (t.tile == 128) {
-    set_tiles(g, 128);
+    set_tiles(g, 128, 128);
     hipLaunchKernelGGL((mx_gemm_mid_kernel<OUT_BF16>), dealt(g.count), dim3(M_WAVES * 64), 0, s, g);
   } else if (t.tile == 32) {
-    set_tiles(g, 32);
+    set_tiles(g, 32, 32);
     if (g.count <= n_cu) hipLaunchKernelGGL((mx_gemm_split_kernel<OUT_BF16, 4>), dealt(g.count), dim3(256), 0, s, g);
     else hipLaunchKernelGGL((mx_gemm_split_kernel<OUT_BF16, 2>), dealt(g.count), dim3(256), 0, s, g);
   } else {
@@ -724,9 +738,9 @@ int mx_launch_gemm(const uint8_t* L, const uint8_t* sL, int bits_l, const uint8_
   return out_bf16 ? launch<true>(g, t, n_cu, s) : launch<false>(g, t, n_cu, s);
 }
 
-// For measuring and for tests: the product by one kind of tile (16, 32, 64, 128 or 256), or by the rule's (0).
+// For measuring and for tests: the product by one kind of tile (16, 32, 64, 128, 192 or 256), or by the rule's (0).
 extern "C" int mx_gemm_by_tile(const fp4_mx* l, const fp4_mx* rt, const float* addend, void* out, fp4_dtype out_dt, int64_t ldo, int tile, void* stream) {
-  if (tile != 0 && tile != 16 && tile != 32 && tile != 64 && tile != 128 && tile != 256) return FP4_ERR_ARG;
+  if (tile != 0 && tile != 16 && tile != 32 && tile != 64 && tile != 128 && tile != 192 && tile != 256) return FP4_ERR_ARG;
   const int rc = mx_check_gemm(l, rt, addend, out, out_dt, ldo);
   if (rc || l->lines == 0 || rt->lines == 0) return rc;
   return mx_launch_gemm(l->codes, l->scales, l->bits, rt->codes, rt->scales, rt->bits, l->lines, rt->lines, l->length, addend, out, out_dt == FP4_BF16, ldo,

@@ -64,7 +64,7 @@ def test_outputs_of_many_tiles(P, Q, Kc, bl, br):
     assert torch.equal(b.mx_gemm(l, r), got)
 
 
-@pytest.mark.parametrize("tile", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("tile", [16, 32, 64, 128, 192, 256])
 @pytest.mark.parametrize("bl,br", BITS)
 @pytest.mark.parametrize("P,Q,Kc", [(1, 8, 8), (70, 40, 2000), (129, 264, 513), (513, 528, 1536)])
 def test_every_tile_gives_the_product(P, Q, Kc, bl, br, tile):
