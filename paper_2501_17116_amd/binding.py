@@ -549,7 +549,7 @@ class MxTensor:
     codes [lines, mx_pitch(length) / 2] (4 bits) or [2, lines, mx_pitch(length) / 2] (8 bits), scales [lines, mx_pitch(length) / 32],
     uint8.  transposed: the lines are the columns of the matrix that the tensor stands for."""
 
-    __slots__ = ("codes", "scales", "bits", "lines", "length", "transposed", "c", "ref")
+    __slots__ = ("_codes", "_scales", "_room", "bits", "lines", "length", "transposed", "device", "c", "ref")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, length: int, transposed: bool = False):
         pitch, shape, lines = mx_pitch(length), tuple(codes.shape), scales.shape[0]
@@ -561,12 +561,27 @@ class MxTensor:
             raise ValueError("codes and scales must live on one GPU")
         if not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError("codes and scales must be contiguous")
-        self._set(codes, scales, 4 * (len(shape) - 1), lines, length, transposed)
+        self._codes, self._scales, self._room = codes, scales, None
+        self._set(codes.data_ptr(), scales.data_ptr(), 4 * (len(shape) - 1), lines, length, transposed, codes.device)
 
-    def _set(self, codes, scales, bits, lines, length, transposed):
-        self.codes, self.scales, self.bits, self.lines, self.length, self.transposed = codes, scales, bits, lines, length, transposed
-        self.c = fp4_mx(codes.data_ptr(), scales.data_ptr(), lines, length, bits)
+    def _set(self, codes, scales, bits, lines, length, transposed, device):
+        self.bits, self.lines, self.length, self.transposed, self.device = bits, lines, length, transposed, device
+        self.c = fp4_mx(codes, scales, lines, length, bits)
         self.ref = C.byref(self.c)
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            half = mx_pitch(self.length) // 2
+            self._codes = self._room[:self.bits // 4 * self.lines * half].view((self.lines, half) if self.bits == 4 else (2, self.lines, half))
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            per_line = mx_pitch(self.length) // MX_BLOCK
+            self._scales = self._room[16 * self.bits // 4 * self.lines * per_line:].view(self.lines, per_line)
+        return self._scales
 
     @property
     def shape(self) -> Tuple[int, int]:
@@ -575,12 +590,15 @@ class MxTensor:
 
 
 def mx_empty(lines: int, length: int, bits: int = 4, transposed: bool = False, device="cuda") -> MxTensor:
+    """Room for an MX tensor: one allocation, the scales behind the codes."""
     if bits not in (4, 8):
         raise ValueError("an MX element has 4 or 8 bits")
-    pitch = mx_pitch(length)
+    codes = lines * mx_pitch(length) // 8 * bits
     t = MxTensor.__new__(MxTensor)
-    t._set(torch.empty((lines, pitch // 2) if bits == 4 else (2, lines, pitch // 2), dtype=torch.uint8, device=device),
-           torch.empty((lines, pitch // MX_BLOCK), dtype=torch.uint8, device=device), bits, lines, length, transposed)
+    t._codes = t._scales = None
+    t._room = room = torch.empty(codes + lines * mx_pitch(length) // MX_BLOCK, dtype=torch.uint8, device=device)
+    at = room.data_ptr()
+    t._set(at, at + codes, bits, lines, length, transposed, room.device)
     return t
 
 
@@ -596,21 +614,21 @@ def _ld(t: torch.Tensor, name: str) -> int:
     return ld if rows > 1 and cols > 0 else max(8, -(-cols // 8) * 8)
 
 
-def _same_device(x: torch.Tensor, *mx: Optional[MxTensor]):
+def _same_device(x, *mx: Optional[MxTensor]):
     for t in mx:
-        if t is not None and t.codes.device != x.device:
+        if t is not None and t.device != x.device:
             raise ValueError("all tensors must live on one device")
 
 
-def _out(t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor, name: str) -> torch.Tensor:
+def _out(t: Optional[torch.Tensor], shape, dtype, device: torch.device, name: str) -> torch.Tensor:
     """The caller's output, checked, or a new one; its rows begin at multiples of 16 bytes."""
     if t is None:
         rows, cols = shape
         if cols % 8 == 0:
-            return torch.empty(shape, dtype=dtype, device=like.device)
-        return torch.empty((rows, -(-cols // 8) * 8), dtype=dtype, device=like.device)[:, :cols]
-    if t.shape != shape or t.dtype != dtype or t.device != like.device:
-        raise ValueError("%s must be %s %s on %s" % (name, tuple(shape), dtype, like.device))
+            return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty((rows, -(-cols // 8) * 8), dtype=dtype, device=device)[:, :cols]
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be %s %s on %s" % (name, tuple(shape), dtype, device))
     return t
 
 
@@ -663,7 +681,7 @@ def mx_quantize_both(x: torch.Tensor, row_bits: int = 4, col_bits: int = 4) -> T
 
 def mx_dequantize(t: MxTensor, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The matrix that t stands for, in the values of its codes."""
-    x = _out(out, t.shape, dtype, t.codes, "out")
+    x = _out(out, t.shape, dtype, t.device, "out")
     _check(lib().mx_dequantize(t.ref, int(t.transposed), x.data_ptr(), _dt(x), _ld(x, "out"), _stream_of(x)), "mx_dequantize")
     return x
 
@@ -673,8 +691,8 @@ def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, a
     """l . rt^T over their lines' common length (+ addend)."""
     if l.length != rt.length:
         raise ValueError("operands disagree in the contraction's length")
-    _same_device(l.codes, rt)
-    out = _out(out, (l.lines, rt.lines), out.dtype if out is not None else out_dtype, l.codes, "out")
+    _same_device(l, rt)
+    out = _out(out, (l.lines, rt.lines), out.dtype if out is not None else out_dtype, l.device, "out")
     ldo = _ld(out, "out")
     if addend is not None:
         if addend.shape != out.shape or addend.dtype != torch.float32 or addend.device != out.device:
@@ -687,7 +705,7 @@ def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, a
 
 def mx_gemm_by_tile(l: MxTensor, rt: MxTensor, tile: int, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mx_gemm by one kind of tile (16, 32, 64, 128, 192, 256), for tests and measuring; addend has the output's leading dimension."""
-    out = _out(None, (l.lines, rt.lines), out_dtype, l.codes, "out")
+    out = _out(None, (l.lines, rt.lines), out_dtype, l.device, "out")
     _check(lib().mx_gemm_by_tile(l.ref, rt.ref, _ptr(addend), _ptr(out), _dt(out), _ld(out, "out"), tile, _stream()), "mx_gemm_by_tile")
     return out
 
@@ -735,7 +753,7 @@ def mx_linear_fwd(A: torch.Tensor, W: MxTensor, act_bits: int = 4, saved: Option
     if saved is not None and (saved.lines, saved.length) != (K, M):
         raise ValueError("the checkpoint holds %d x %d activations, not %d x %d" % (saved.length, saved.lines, M, K))
     _same_device(A, W, saved)
-    Y = _out(Y, (M, N), A.dtype, A, "Y")
+    Y = _out(Y, (M, N), A.dtype, A.device, "Y")
     room, nbytes, stream = _mx_ws(FP4_OP_MX_FWD, M, K, N, ws, A)
     _check(lib().mx_linear_fwd(A.data_ptr(), _dt(A), M, K, N, lda, act_bits, W.ref, Y.data_ptr(), _ld(Y, "Y"), None if saved is None else saved.ref,
                                room, nbytes, stream), "mx_linear_fwd")
@@ -750,7 +768,7 @@ def mx_linear_bwd_dgrad(dY: torch.Tensor, W: MxTensor, dA: Optional[torch.Tensor
     if W.length != N:
         raise ValueError("dY [M,N] and W (lines K, length N) must agree in N")
     _same_device(dY, W)
-    dA = _out(dA, (M, K), dY.dtype, dY, "dA")
+    dA = _out(dA, (M, K), dY.dtype, dY.device, "dA")
     room, nbytes, stream = _mx_ws(FP4_OP_MX_DGRAD, M, K, N, ws, dY)
     _check(lib().mx_linear_bwd_dgrad(dY.data_ptr(), _dt(dY), M, K, N, ldy, W.ref, dA.data_ptr(), _ld(dA, "dA"), room, nbytes, stream),
            "mx_linear_bwd_dgrad")
@@ -768,7 +786,7 @@ def mx_linear_bwd_wgrad(dY: torch.Tensor, saved: MxTensor, grad_bits: int = 4, d
     if accumulate and dW is None:
         raise ValueError("accumulate needs the dW to add to")
     _same_device(dY, saved)
-    dW = _out(dW, (K, N), torch.float32, dY, "dW")
+    dW = _out(dW, (K, N), torch.float32, dY.device, "dW")
     room, nbytes, stream = _mx_ws(FP4_OP_MX_WGRAD, M, K, N, ws, dY)
     _check(lib().mx_linear_bwd_wgrad(dY.data_ptr(), _dt(dY), M, K, N, ldy, saved.ref, grad_bits, int(accumulate), dW.data_ptr(), _ld(dW, "dW"), room,
                                      nbytes, stream), "mx_linear_bwd_wgrad")
@@ -786,8 +804,8 @@ def mx_linear_bwd(dY: torch.Tensor, saved: MxTensor, W: MxTensor, grad_bits: int
     if accumulate and dW is None:
         raise ValueError("accumulate needs the dW to add to")
     _same_device(dY, W, saved)
-    dA = _out(dA, (M, K), dY.dtype, dY, "dA")
-    dW = _out(dW, (K, N), torch.float32, dY, "dW")
+    dA = _out(dA, (M, K), dY.dtype, dY.device, "dA")
+    dW = _out(dW, (K, N), torch.float32, dY.device, "dW")
     room, nbytes, stream = _mx_ws(FP4_OP_MX_BWD, M, K, N, ws, dY)
     _check(lib().mx_linear_bwd(dY.data_ptr(), _dt(dY), M, K, N, ldy, W.ref, saved.ref, grad_bits, dA.data_ptr(), _ld(dA, "dA"), int(accumulate),
                                dW.data_ptr(), _ld(dW, "dW"), room, nbytes, stream), "mx_linear_bwd")

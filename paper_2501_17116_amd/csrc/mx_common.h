@@ -103,23 +103,30 @@ FP4_D uint32_t mx_quad_max(uint32_t v) {
   o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true);            // lane ^ 2
   return v > o ? v : o;
 }
-// A 16-byte piece of a row: eight bf16 or four fp32 from column c on; zeros behind the row's end and in rows that are not there.
+// A 16-byte piece of a row: eight bf16 or four fp32 from column c on; zeros behind the row's end and in rows that are not there.  Without a
+// branch, which would have each request waited for before the next: what is not there is read from where something is, and cleared.  ragged:
+// whether rows end inside a piece (then element by element); the matrix has a row and a column.
 template <class T>
-FP4_D u32x4 mx_load_piece(const void* x, int64_t row, int64_t rows, int64_t cols, int64_t ld, int64_t c) {
-  constexpr int E = sizeof(T);
-  constexpr int N = 16 / E;
-  u32x4 w = {0u, 0u, 0u, 0u};
-  if (row < rows) {
-    const T* p = reinterpret_cast<const T*>(x) + row * ld + c;
-    if (c + N <= cols) {
-      w = *reinterpret_cast<const u32x4*>(p);
-    } else {
-      union { T t[N]; u32x4 v; } u;
-      u.v = w;
-      for (int e = 0; e < N; ++e)
-        if (c + e < cols) u.t[e] = p[e];
-      w = u.v;
+FP4_D u32x4 mx_load_piece(const void* x, int64_t row, int64_t rows, int64_t cols, int64_t ld, int64_t c, bool ragged) {
+  constexpr int N = 16 / sizeof(T);
+  const T* const p = reinterpret_cast<const T*>(x) + min(row, rows - 1) * ld;
+  u32x4 w;
+  if (ragged) {
+    uint32_t e[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const T v = p[min(c + i, cols - 1)];
+      uint32_t bits;
+      if constexpr (sizeof(T) == 2) bits = v;
+      else bits = f2u(v);
+      e[i] = row < rows && c + i < cols ? bits : 0u;
     }
+    if constexpr (sizeof(T) == 2) w = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[N - 4] | e[N - 3] << 16, e[N - 2] | e[N - 1] << 16};
+    else w = u32x4{e[0], e[1], e[2], e[3]};
+  } else {
+    w = *reinterpret_cast<const u32x4*>(p + min(c, cols - N));
+    const uint32_t in = row < rows && c < cols ? 0xffffffffu : 0u;
+    w = u32x4{w.x & in, w.y & in, w.z & in, w.w & in};
   }
   return w;
 }

@@ -62,14 +62,18 @@ FP4_D void few_quantize(const FewArgs& a, int64_t p0, int rows, uint8_t* codes, 
   for (int i0 = wave; i0 < total; i0 += FQ * FW_WAVES) {
     u32x4 w[FQ][P];
     int row[FQ], c[FQ];
+    auto each = [&](bool ragged) {
 #pragma unroll
-    for (int n = 0; n < FQ; ++n) {
-      const int i = i0 + n * FW_WAVES;
-      row[n] = i / per_row;
-      c[n] = (i - row[n] * per_row) * 64 + lane;
+      for (int n = 0; n < FQ; ++n) {
+        const int i = i0 + n * FW_WAVES;
+        row[n] = i / per_row;
+        c[n] = (i - row[n] * per_row) * 64 + lane;
 #pragma unroll
-      for (int p = 0; p < P; ++p) w[n][p] = mx_load_piece<T>(a.x, p0 + row[n], p0 + rows, a.K, a.ldx, c[n] * 8 + p * 4);
-    }
+        for (int p = 0; p < P; ++p) w[n][p] = mx_load_piece<T>(a.x, p0 + row[n], p0 + rows, a.K, a.ldx, c[n] * 8 + p * 4, ragged);
+      }
+    };
+    if (a.K % (16 / (int)sizeof(T))) each(true);
+    else each(false);
 #pragma unroll
     for (int n = 0; n < FQ; ++n) {
       if (row[n] >= rows) break;

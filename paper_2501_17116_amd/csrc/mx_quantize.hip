@@ -10,6 +10,9 @@
 #include "mx_common.h"
 
 #include <algorithm>
+#include <type_traits>
+
+int fp4_compute_units_of_current_device();
 
 namespace {
 
@@ -34,17 +37,21 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units
   const int64_t u0 = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * ROWS_U;
   constexpr int P = sizeof(T) == 2 ? 1 : 2;   // pieces a lane
   u32x4 w[ROWS_U][P];
-  int64_t row = u0 / per_row;
-  int seg = (int)(u0 - row * per_row);
+  auto each = [&](bool ragged) {
+    int64_t row = u0 / per_row;
+    int seg = (int)(u0 - row * per_row);
 #pragma unroll
-  for (int i = 0; i < ROWS_U; ++i) {
+    for (int i = 0; i < ROWS_U; ++i) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) w[i][p] = mx_load_piece<T>(a.x, row, a.rows, a.cols, a.ld, (int64_t)seg * MX_PITCH + lane * 8 + p * 4);
-    if (++seg == per_row) {
-      seg = 0;
-      ++row;
+      for (int p = 0; p < P; ++p) w[i][p] = mx_load_piece<T>(a.x, row, a.rows, a.cols, a.ld, (int64_t)seg * MX_PITCH + lane * 8 + p * 4, ragged);
+      if (++seg == per_row) {
+        seg = 0;
+        ++row;
+      }
     }
-  }
+  };
+  if (a.cols % (16 / (int)sizeof(T))) each(true);
+  else each(false);
 #pragma unroll
   for (int i = 0; i < ROWS_U; ++i) {
     if (u0 + i >= units) break;
@@ -67,11 +74,17 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units
 }
 
 // ---- columns, and rows beside them ----------------------------------------------------------------------------------------------
-// A workgroup of eight waves takes 256 rows x 256 bytes of columns, a wave 32 of the rows: one block of every column.  The columns' codes
-// pass through LDS once more, so that they leave as whole 128-byte lines (256 rows of 4-bit codes).
-constexpr int TW = 8;   // waves
+// A wave takes 32 rows x 256 bytes of columns, one block of every column, a workgroup eight waves' rows.  The columns' codes pass through LDS
+// once more, so that they leave as whole 128-byte lines (256 rows of 4-bit codes): with four waves, half lines, 16384 x 4096 bf16 takes 46 us
+// instead of 40 (columns in 4 bits) and 59 instead of 48 (8 bits).  What remains above the rows' rate are some 700 vector instructions a wave, which
+// four waves a SIMD do not hide altogether.  Tensors that do not give every CU such a workgroup are one wave's chain of requests and
+// instructions long; there a workgroup has two waves (1055 x 1384: rows and columns in 4 bits 5.8 us).
+// What the order of the tiles costs (GROUP_C side by side before the next rows): whole rows of tiles write one line of the output every so many
+// KiB at a time, columns of tiles read rows that far apart, and either may fall on a few of the memory's channels.  16384 x 4096 bf16, columns in
+// 4 bits 40.1 us with whole rows, 36.2 / 38.3 / 37.7 with 4 / 8 / 16; 8192 x 11008 51.0, 54.7 / 50.3 / 51.2; 4096 x 11008 fp32 46.4, 48.9 / 48.2 / 46.8.
+constexpr int GROUP_C = 16;
 
-template <class T, int ROW, int COL>
+template <class T, int ROW, int COL, int TW>   // TW: waves
 __global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles_c, int64_t tiles) {
   constexpr int E = sizeof(T);
   constexpr int CW = 256 / E;        // columns a tile
@@ -82,20 +95,37 @@ __global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles
   const int64_t per_xcd = (tiles + 7) / 8, id = (int64_t)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
   if ((int64_t)(blockIdx.x / 8) >= per_xcd || id >= tiles) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t tr = id / tiles_c;
-  const int64_t r0 = tr * (TW * 32) + wave * 32, c0 = (id - tr * tiles_c) * CW;
+  // GROUP_C tiles side by side, then the next rows of the same columns
+  const int64_t tiles_r = tiles / tiles_c, in_group = tiles_r * GROUP_C, group = id / in_group, at_c = group * GROUP_C;
+  const int64_t wide = min((int64_t)GROUP_C, tiles_c - at_c), tr = (id - group * in_group) / wide;
+  const int64_t r0 = tr * (TW * 32) + wave * 32, c0 = (at_c + (id - group * in_group) - tr * wide) * CW;
   const int64_t row_pitch = mx_pitch_of(a.cols), col_pitch = mx_pitch_of(a.rows);
   const int piece = lane & 15, sub = lane >> 4;
   u32x4 w[8];
+  if (r0 + 32 <= a.rows && c0 + CW <= a.cols) {   // eight requests and nothing between them
+    const uint8_t* const first = reinterpret_cast<const uint8_t*>(a.x) + (r0 * a.ld + c0) * E;
+    const uint32_t step = (uint32_t)a.ld * E;     // 32 rows are below 2^32 bytes
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = mx_load_piece<T>(a.x, r0 + i * 4 + sub, a.rows, a.cols, a.ld, c0 + piece * EPP);
+    for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const u32x4*>(first + (i * 4 + sub) * step + piece * 16);
+  } else {
+    auto each = [&](bool ragged) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = mx_load_piece<T>(a.x, r0 + i * 4 + sub, a.rows, a.cols, a.ld, c0 + piece * EPP, ragged);
+    };
+    if (r0 >= a.rows || c0 >= a.cols) {   // behind the edge: zeros up to the pitch
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
+    } else if (a.cols % EPP) each(true);
+    else each(false);
+  }
   uint32_t* const mine = park[wave];
 #pragma unroll
   for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(mine + (i * 4 + sub) * 64 + piece * 4) = w[i];
   if constexpr (ROW != NO_AXIS) {
+    uint8_t *const row_h = a.row_codes + (r0 * row_pitch + c0) / 2, *const row_s = a.row_scales + (r0 * row_pitch + c0) / MX_BLOCK;
+    const uint32_t rows_here = (uint32_t)max(min(a.rows - r0, (int64_t)32), (int64_t)0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int64_t row = r0 + i * 4 + sub;
       uint32_t top = mx_quad_max(E == 2 ? mx_amax_bf16(w[i]) : mx_amax_f32(w[i]));
       if constexpr (E == 4) {
         const uint32_t o = other_quad(top);
@@ -103,10 +133,10 @@ __global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles
       }
       const uint32_t byte = mx_scale_byte<ROW>(top);
       const float s = mx_scale_f32(byte);
-      const int64_t at = row * row_pitch + c0 + piece * EPP;
-      if (row < a.rows) {
+      const uint32_t row = (uint32_t)(i * 4 + sub);
+      if (row < rows_here) {
         uint32_t h, l;
-        uint8_t *const ph = a.row_codes + at / 2, *const pl = ph + a.rows * row_pitch / 2;
+        uint8_t *const ph = row_h + row * (uint32_t)(row_pitch / 2) + piece * (EPP / 2), *const pl = ph + a.rows * row_pitch / 2;
         if constexpr (E == 2) {
           mx_encode8<ROW>(w[i], s, h, l);
           *reinterpret_cast<uint32_t*>(ph) = h;
@@ -118,7 +148,7 @@ __global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles
           *reinterpret_cast<uint16_t*>(ph) = (uint16_t)h;
           if constexpr (ROW == 8) *reinterpret_cast<uint16_t*>(pl) = (uint16_t)l;
         }
-        if (piece % (MX_BLOCK / EPP) == 0) a.row_scales[at / MX_BLOCK] = (uint8_t)byte;
+        if (piece % (MX_BLOCK / EPP) == 0) row_s[row * (uint32_t)(row_pitch / MX_BLOCK) + piece / (MX_BLOCK / EPP)] = (uint8_t)byte;
       }
     }
   }
@@ -129,14 +159,15 @@ __global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles
   for (int r = 0; r < 32; ++r) d[r] = mine[r * 64 + lane];
   u32x4 hi[NC], lo[NC];
   uint32_t bytes[NC];
+  uint32_t tops = 0;   // of both columns at once where a word holds two
+#pragma unroll
+  for (int r = 0; r < 32; ++r) {
+    if constexpr (E == 2) tops = mx_pk_max_u16(tops, d[r] & 0x7fff7fffu);
+    else tops = max(tops, d[r] & 0x7fffffffu);
+  }
 #pragma unroll
   for (int h = 0; h < NC; ++h) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int r = 0; r < 32; ++r) {
-      const uint32_t m = (E == 4 ? d[r] : h == 0 ? d[r] << 16 : d[r]) & (E == 4 ? 0x7fffffffu : 0x7fff0000u);
-      top = top > m ? top : m;
-    }
+    const uint32_t top = E == 4 ? tops : h == 0 ? tops << 16 : tops & 0xffff0000u;
     bytes[h] = mx_scale_byte<COL>(top);
     const float s = mx_scale_f32(bytes[h]);
 #pragma unroll
@@ -157,32 +188,35 @@ __global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles
       lo[h][q] = cl;
     }
   }
-  // [plane][column][wave], sixteen bytes each, and the scales [column][wave], over the parked rows; a column's eight pieces are rotated by its
-  // number, so that eight lanes with one piece of eight columns meet eight bank groups
+  // [plane][column][wave], sixteen bytes each, and the scales [column][wave], over the parked rows; a column's pieces are rotated by half
+  // its number, so that lanes with one piece of neighbouring columns meet all bank groups
   __syncthreads();
   uint8_t* const out = reinterpret_cast<uint8_t*>(&park[0][0]);
-  uint8_t* const out_scales = out + COL / 4 * CW * 128;
+  uint8_t* const out_scales = out + COL / 4 * CW * (TW * 16);
 #pragma unroll
   for (int h = 0; h < NC; ++h) {
-    const int c = lane * NC + h, at = c * 128 + ((wave + c) & 7) * 16;
+    const int c = lane * NC + h, at = c * (TW * 16) + ((wave + (c >> 1)) & (TW - 1)) * 16;
     *reinterpret_cast<u32x4*>(out + at) = hi[h];
-    if constexpr (COL == 8) *reinterpret_cast<u32x4*>(out + CW * 128 + at) = lo[h];
-    out_scales[c * 8 + wave] = (uint8_t)bytes[h];
+    if constexpr (COL == 8) *reinterpret_cast<u32x4*>(out + CW * (TW * 16) + at) = lo[h];
+    out_scales[c * TW + wave] = (uint8_t)bytes[h];
   }
   __syncthreads();
-  const int64_t rr = tr * (TW * 32);
+  const int64_t first = (c0 * col_pitch + tr * (TW * 32));
+  const uint32_t cols_here = (uint32_t)min(a.cols - c0, (int64_t)CW);   // negative behind the last column: none
 #pragma unroll
-  for (int i = 0; i < CW * 8 / (TW * 64); ++i) {
-    const int n = i * TW * 64 + threadIdx.x, c = n >> 3, piece16 = n & 7;
-    if (c0 + c < a.cols) {
-      const int64_t at = ((c0 + c) * col_pitch + rr) / 2 + piece16 * 16;
+  for (int i = 0; i < CW / 64; ++i) {
+    const uint32_t n = i * TW * 64 + threadIdx.x, c = n / TW, piece16 = n % TW;
+    if (a.cols > c0 && c < cols_here) {
+      uint8_t* const o = a.col_codes + first / 2 + (c * (uint64_t)(col_pitch / 2) + piece16 * 16);
 #pragma unroll
       for (int p = 0; p < COL / 4; ++p)
-        *reinterpret_cast<u32x4*>(a.col_codes + p * (a.cols * col_pitch / 2) + at) = *reinterpret_cast<const u32x4*>(out + p * CW * 128 + c * 128 + ((piece16 + c) & 7) * 16);
+        *reinterpret_cast<u32x4*>(o + p * (a.cols * col_pitch / 2)) = *reinterpret_cast<const u32x4*>(out + (p * CW + c) * (TW * 16) + ((piece16 + (c >> 1)) & (TW - 1)) * 16);
     }
   }
+  typedef typename std::conditional<TW == 8, u32x2, uint16_t>::type Scales;   // a column's
+  static_assert(TW == 8 || TW == 2, "a byte a wave");
   if (threadIdx.x < CW && c0 + threadIdx.x < a.cols)
-    *reinterpret_cast<u32x2*>(a.col_scales + ((c0 + threadIdx.x) * col_pitch + rr) / MX_BLOCK) = *reinterpret_cast<const u32x2*>(out_scales + threadIdx.x * 8);
+    *reinterpret_cast<Scales*>(a.col_scales + first / MX_BLOCK + threadIdx.x * (col_pitch / MX_BLOCK)) = *reinterpret_cast<const Scales*>(out_scales + threadIdx.x * TW);
 }
 
 // ---- back ----------------------------------------------------------------------------------------------------------------------
@@ -194,16 +228,16 @@ struct DequantArgs {
 
 FP4_D float decode_scale(uint32_t byte) { return u2f(byte ? byte << 23 : 0x00400000u); }   // 2^(byte - 127)
 
-// eight codes, of 8 bits two words of them, under one scale -> eight fp32; byte 255: NaN throughout
+// eight codes, of 8 bits two words of them, under one scale -> eight fp32; byte 255: NaN throughout, which the scale brings
 template <int BITS>
 FP4_D void decode8(const uint32_t (&c)[BITS / 4], uint32_t byte, float (&o)[8]) {
-  const float s = decode_scale(byte), t = BITS == 4 ? s : 1.0f;   // of 8 bits the codes are joined before they are scaled: s h alone may overflow
+  const float s = byte == 255u ? u2f(0x7fffffffu) : decode_scale(byte);
   mx_f32x2 v[4];
-  v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], t, 0);
-  v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], t, 1);
-  v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], t, 2);
-  v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], t, 3);
-  if constexpr (BITS == 8) {
+  v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], 1.0f, 0);
+  v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], 1.0f, 1);
+  v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], 1.0f, 2);
+  v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], 1.0f, 3);
+  if constexpr (BITS == 8) {   // joined before they are scaled: s h alone may overflow
     mx_f32x2 l[4];
     l[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[1], 0.125f, 0);
     l[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[1], 0.125f, 1);
@@ -211,13 +245,12 @@ FP4_D void decode8(const uint32_t (&c)[BITS / 4], uint32_t byte, float (&o)[8]) 
     l[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[1], 0.125f, 3);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      v[i].x = (v[i].x + l[i].x) * s;
-      v[i].y = (v[i].y + l[i].y) * s;
+      v[i].x += l[i].x;
+      v[i].y += l[i].y;
     }
   }
-  const float nan = u2f(0x7fffffffu);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o[i] = byte == 255u ? nan : v[i / 2][i & 1];
+  for (int i = 0; i < 8; ++i) o[i] = v[i / 2][i & 1] * s;
 }
 // ... -> four pairs of bf16, exactly: s (h + l / 8) has seven bits
 template <int BITS>
@@ -233,7 +266,7 @@ FP4_D void decode8(const uint32_t (&c)[BITS / 4], uint32_t byte, uint32_t (&o)[4
     float v[8];
     decode8<BITS>(c, byte, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = (f2u(v[2 * i]) >> 16) | (f2u(v[2 * i + 1]) & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_perm(f2u(v[2 * i + 1]), f2u(v[2 * i]), 0x07060302u);
   }
 }
 
@@ -345,13 +378,19 @@ __global__ __launch_bounds__(256) void mx_restore_cols_kernel(DequantArgs a, int
   }
 }
 
+template <class T, int ROW, int COL>
+void launch_tiles(const QuantArgs& a, hipStream_t s) {
+  const int tiles_c = (int)(mx_pitch_of(a.cols) * sizeof(T) / 256);   // up to the pitches: what lies behind the ends is written too
+  const int64_t tiles = tiles_c * (mx_pitch_of(a.rows) / 256);
+  if (tiles >= fp4_compute_units_of_current_device())
+    hipLaunchKernelGGL((mx_tile_kernel<T, ROW, COL, 8>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(8 * 64), 0, s, a, tiles_c, tiles);
+  else
+    hipLaunchKernelGGL((mx_tile_kernel<T, ROW, COL, 2>), dim3((unsigned)((4 * tiles + 7) / 8 * 8)), dim3(2 * 64), 0, s, a, tiles_c, 4 * tiles);
+}
 template <class T, int ROW>
 void launch_tiles(const QuantArgs& a, int col_bits, hipStream_t s) {
-  const int tiles_c = (int)(mx_pitch_of(a.cols) * sizeof(T) / 256);   // up to the pitches: what lies behind the ends is written too
-  const int64_t tiles = tiles_c * (mx_pitch_of(a.rows) / (TW * 32));
-  const dim3 grid((unsigned)((tiles + 7) / 8 * 8)), block(TW * 64);
-  if (col_bits == 4) hipLaunchKernelGGL((mx_tile_kernel<T, ROW, 4>), grid, block, 0, s, a, tiles_c, tiles);
-  else hipLaunchKernelGGL((mx_tile_kernel<T, ROW, 8>), grid, block, 0, s, a, tiles_c, tiles);
+  if (col_bits == 4) launch_tiles<T, ROW, 4>(a, s);
+  else launch_tiles<T, ROW, 8>(a, s);
 }
 
 template <class T>
