@@ -43,6 +43,11 @@ def test_passes(M, K, N, dtype):
             alone = b.mx_checkpoint_save(A.cuda(), bits)
             assert torch.equal(saved.codes, alone.codes) and torch.equal(saved.scales, alone.scales)
             assert np.array_equal(host(b.mx_dequantize(saved, torch.float32)), mx.through(a.T, bits).T)
+    w8 = b.mx_quantize(W.cuda(), b.FP4_AXIS_COL, 8)      # weights in 8 bits
+    w8_fwd = mx.through(w.T, 8)
+    for act in (4, 8):
+        aq = mx.through(a, act)
+        close(b.mx_linear_fwd(A.cuda(), w8, act_bits=act), aq @ w8_fwd.T, bound(aq, w8_fwd, K), bf16)
     saved = b.mx_checkpoint_save(A.cuda())
     kept = mx.through(a.T, 8)
     gq = mx.through(g, 4)
