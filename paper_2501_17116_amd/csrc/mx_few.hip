@@ -2,9 +2,13 @@
 //
 // Bound by reading the weights once: K N (1/2 + 1/32) bytes.  A workgroup of eight waves takes 16 NT rows of L x 16 NW rows of R; its waves
 // share the contraction, 512 codes at a time (whole 128-byte lines of every row of R), and meet once, in LDS, where their sums are added in
-// the waves' order.  Each row of R is read by one workgroup for every 16 NT tokens.  The fewer columns a workgroup has, the more
-// often the tokens are read; half as many workgroups as CUs still draw nine tenths of the memory's rate, so they are given as many
-// columns as leaves that.
+// the waves' order.  Each row of R is read by one workgroup for every 16 NT tokens; the fewer columns a workgroup has, the more
+// often the tokens are read.
+//
+// Measured (other weights each call): a launch that has next to nothing to do takes 3.4 us in a graph; one token, 4096 x 4096 5.3, 4096 x 11008 9.5 - 10,
+// 13824 x 5120 13.5 - 15, so beyond the launch the weights come at 3.5 - 4 TB/s.  24 tokens in 8 bits, 4096 x 11008 11.7 and 3.4 for their codes.  Tried:
+// tokens and weights of two units on their way in registers, 128 bytes of a row a unit where those run short: within 2 % at 4096 x 4096 and
+// 13824 x 5120, 5 - 10 % slower at 4096 x 11008; the smaller pieces cost what the waits gave.
 //
 // Where the tokens' codes fit a workgroup's LDS they are made there, while its first weights are on their way: one launch, and nothing but
 // the weights, the tokens and the result moves.
@@ -260,8 +264,9 @@ void few_rows(const FewArgs& a, bool out_bf16, int n_cu, hipStream_t s) {
 
 int fp4_compute_units_of_current_device();
 
-// Whether the tokens of a forward pass are quantized inside the product's own launch: while a workgroup makes their codes in no more time
-// than its first weights take to arrive, and they fit 64 KiB of LDS.
+// Whether the tokens of a forward pass are quantized inside the product's own launch: while making their codes in every workgroup costs no
+// more than the launch that it saves (about 3 us), and they fit 64 KiB of LDS.  In the product / in a launch before, 4 bits: 8 x 4096 6.7 / 8.1 us, 16 x
+// 4096 8.7 / 8.4, 32 x 2048 7.9 / 7.5; the host saves a launch (about 3.5 us) besides.
 bool mx_few_fuses(int64_t M, int64_t K, int bits) {
   const int64_t pitch = mx_pitch_of(K);
   return M <= 32 && M * pitch <= 65536 && M * ((bits / 4) * few_row(pitch) + few_scales(pitch)) <= 65536;

@@ -63,7 +63,9 @@ FP4_D mx_f32x16 mx_mfma(const u32x4& r, const u32x4& l, const mx_f32x16& c, uint
   else return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 3, (int)sr, 3, (int)sl);
 }
 
-// 64 x 64 outputs a workgroup, 32 x 32 a wave, operands straight from memory to the matrix core's registers.  Rows past the matrix's edge repeat its last one and are not stored.
+// 64 x 64 outputs a workgroup, 32 x 32 a wave, operands straight from memory to the matrix core's registers.  Rows past the matrix's edge
+// repeat its last one and are not stored.  For short contractions, where a start through LDS costs more than it saves: one round trip to
+// memory a step is what bounds it (249 x 2400 over 264 5.3 us, a launch by itself 3.4).
 template <bool OUT_BF16>
 __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -107,9 +109,11 @@ __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
 // reading one chunk touch sixteen different bank groups.
 // Measured (4 x 4 bits, bf16 out, repeated calls): 8192 x 2048 x 5504 48 us, 8192 x 11008 x 4096 210 us, 16384 x 12288 x 4096 434 us (3.5 - 3.8e15
 // operations/s); 8 x 4 bits, 4096 x 4096 x 8192 129 us (4.3e15 of codes).  The issue loop alone over random operands reaches 6.4e15.  Bound:
-// without its loads the same loop reaches 5.5e15, with loads that hit L2 4.6e15, so the arrivals' place in LDS (64 KiB a step beside 192 KiB
-// of fragments) takes a fifth, and misses and the stores' share of memory the rest.  Tried: half steps of 64 bytes of a row with
-// three on their way (1.5 steps ahead instead of one): 5 % faster at the largest outputs, 5 % slower elsewhere, as twice the rows a
+// the matrix cores and power: over 16384 x 12288 x 4096 the clock falls to 1.8 - 1.9 GHz, and of its cycles the matrix cores are busy in
+// 49 %, LDS in 29 % (a quarter of that in conflicts).  Without its loads the same loop reaches 5.5e15, with loads that hit L2 4.6e15; misses and
+// the stores' share of memory are the rest.
+// Tried: half steps of 64 bytes of a row with three on their way (1.5 steps ahead instead of one): 5 % faster at the largest outputs, 5 %
+// slower elsewhere, as twice the rows a
 // load cost more than the distance gave.  Parking the sums in LDS for stores of 128 bytes instead of the swaps' 64: 50.0 against 48.4,
 // 220 against 210 us.
 constexpr int BP = 256, BKB = 128;
@@ -527,7 +531,10 @@ FP4_D void finish_tile(const MxGemm& g, const float* tile, int64_t P0, int64_t Q
 // For outputs with too few 256 x 256 tiles.  Two groups of four waves, a wave 64 x 64 of the sums; the groups share each step, two of its
 // four slices each, so that a SIMD has one wave that reads fragments while another multiplies (with four waves a step took
 // the sum of both), and their sums are joined at the end, the first group's and the second's.  Steps go through a ring of four LDS stages
-// with three on their way; scales come for two steps at a time, sixteen bytes of every row, into a ring of their own.
+// with three on their way; scales come for two steps at a time, sixteen bytes of every row, into a ring of their own.  Bound by the loads'
+// latency at the 96 KiB that a CU can have on their way: a step takes 0.68 - 0.72 us, 0.48 with the loads alone, 0.54 without them
+// (2048 x 2048 over 2048 12.8 us, over 8192 in 8 x 4 bits 49; 498 x 11936 over 2024 in 8 x 4 bits 30.5).  Tried: the groups half a step apart,
+// 55.3 against 53.2 us.
 constexpr int MT = 128, M_RING = 4, M_WAVES = 8;
 constexpr int M_OP = MT * BKB, M_STAGE = 2 * M_OP, M_LD = MT * 8 / (M_WAVES * 64), M_SC = M_RING * M_STAGE, M_SC_BYTES = 2 * MT * 16;
 constexpr int M_SMEM = M_SC + M_RING * M_SC_BYTES;
@@ -676,7 +683,8 @@ __global__ __launch_bounds__(M_WAVES * 64) void mx_gemm_mid_kernel(MxGemm g) {
 // ---- 32 x 32, the contraction shared ---------------------------------------------------------------------------------------------
 // For the smallest outputs: a workgroup of four waves takes 32 x 32, and each wave every fourth step of the contraction through a ring of its
 // own, without a barrier before the end.  Such a call is one round trip to memory after another, so there are as many workgroups as can be
-// and each wave has RING steps under way.  The waves' sums are added in their order.
+// and each wave has RING steps under way.  The waves' sums are added in their order.  512 x 512 over 256 in 8 x 4 bits 5.1 us, a launch by itself
+// 3.4; 1024 x 1024 over 4096 15.5, where what bounds it are the operands' reads from L2 (32 rows and 32 columns a tile).
 constexpr int ST = 32, S_OP = ST * BKB, S_STEP = 2 * S_OP + 512, S_LD = ST / 8;
 
 template <bool OUT_BF16, int RING>

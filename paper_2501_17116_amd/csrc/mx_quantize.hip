@@ -28,7 +28,8 @@ struct QuantArgs {
 FP4_D uint32_t other_quad(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true); }   // mirrored in eight lanes
 
 // ---- rows --------------------------------------------------------------------------------------------------------------------
-// A wave takes 512 elements of a row at a time (a unit of the pitch), ROWS_U of them from consecutive units.
+// A wave takes 512 elements of a row at a time (a unit of the pitch), ROWS_U of them from consecutive units.  Bound by memory: 16384 x 4096 bf16 to 4
+// bits 29.9 us, to 8 bits 35.2 (5.7 TB/s of what has to move); 4096 x 11008 fp32 38.0 and 40.2 (5.4, 5.7).
 constexpr int ROWS_U = 4;
 
 template <class T, int BITS>
@@ -75,10 +76,11 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units
 
 // ---- columns, and rows beside them ----------------------------------------------------------------------------------------------
 // A wave takes 32 rows x 256 bytes of columns, one block of every column, a workgroup eight waves' rows.  The columns' codes pass through LDS
-// once more, so that they leave as whole 128-byte lines (256 rows of 4-bit codes): with four waves, half lines, 16384 x 4096 bf16 takes 46 us
-// instead of 40 (columns in 4 bits) and 59 instead of 48 (8 bits).  What remains above the rows' rate are some 700 vector instructions a wave, which
-// four waves a SIMD do not hide altogether.  Tensors that do not give every CU such a workgroup are one wave's chain of requests and
-// instructions long; there a workgroup has two waves (1055 x 1384: rows and columns in 4 bits 5.8 us).
+// once more, so that they leave as whole 128-byte lines (256 rows of 4-bit codes); four waves, half lines, were slower by a seventh (4 bits)
+// and a fifth (8 bits).  16384 x 4096 bf16: columns in 4 bits 35.8 us, in 8 bits 40.0, rows and columns in 4 bits 44.9, rows in 4 and columns in 8
+// 49.3 (4.6 - 5.1 TB/s); 4096 x 11008 fp32, both in 4 bits 53.4 (4.3).  Bound by memory; what remains above the rows' rate are some 700 vector
+// instructions a wave, which four waves a SIMD do not hide altogether.  Tensors that do not give every CU such a workgroup are one wave's chain of requests and
+// instructions long; there a workgroup has two waves (1055 x 1384: rows and columns in 4 bits 5.7 us in the kernel).
 // What the order of the tiles costs (GROUP_C side by side before the next rows): whole rows of tiles write one line of the output every so many
 // KiB at a time, columns of tiles read rows that far apart, and either may fall on a few of the memory's channels.  16384 x 4096 bf16, columns in
 // 4 bits 40.1 us with whole rows, 36.2 / 38.3 / 37.7 with 4 / 8 / 16; 8192 x 11008 51.0, 54.7 / 50.3 / 51.2; 4096 x 11008 fp32 46.4, 48.9 / 48.2 / 46.8.
@@ -294,7 +296,7 @@ template <class T> struct Eight;
 template <> struct Eight<uint16_t> { typedef uint32_t type[4]; };
 template <> struct Eight<float> { typedef float type[8]; };
 
-// Lines as rows: a lane takes eight codes.
+// Lines as rows: a lane takes eight codes.  Bound by memory: 16384 x 4096 to bf16 from 4 bits 27.6 us, from 8 bits 33.8 (6.1 TB/s).
 template <class T, int BITS>
 __global__ __launch_bounds__(256) void mx_restore_rows_kernel(DequantArgs a, int64_t units, int per_line) {
   const int lane = threadIdx.x & 63;
@@ -326,7 +328,8 @@ __global__ __launch_bounds__(256) void mx_restore_rows_kernel(DequantArgs a, int
 }
 
 // Lines as columns: a workgroup takes 256 elements of 64 lines, whole 128-byte lines of codes, through LDS; then a lane eight rows of eight
-// columns.  A line's words in LDS are one apart from a multiple of the banks.
+// columns.  A line's words in LDS are one apart from a multiple of the banks.  Bound by memory: 16384 x 4096 to bf16 from 4 bits 28.4 us (6.0 TB/s),
+// from 8 bits 44.1 (4.6), 32 where the codes were just written.
 template <class T, int BITS>
 __global__ __launch_bounds__(256) void mx_restore_cols_kernel(DequantArgs a, int tiles_l, int64_t tiles) {
   constexpr int LW = 33;   // words a line
