@@ -107,8 +107,8 @@ __global__ __launch_bounds__(256) void mx_gemm_small_kernel(MxGemm g) {
 // next tile's first two steps travel during the stores.
 // An operand stage: row r takes bytes [128 r, 128 r + 128), its 16-byte chunk c sits in slot c ^ ((r >> 1) & 7), so that sixteen rows
 // reading one chunk touch sixteen different bank groups.
-// Measured (4 x 4 bits, bf16 out, repeated calls): 8192 x 2048 x 5504 48 us, 8192 x 11008 x 4096 210 us, 16384 x 12288 x 4096 434 us (3.5 - 3.8e15
-// operations/s); 8 x 4 bits, 4096 x 4096 x 8192 129 us (4.3e15 of codes).  The issue loop alone over random operands reaches 6.4e15.  Bound:
+// Measured (4 x 4 bits, bf16 out, repeated calls): 8192 x 2048 x 5504 48 us, 8192 x 11008 x 4096 203 us, 16384 x 12288 x 4096 419 us (3.7 - 3.9e15
+// operations/s); 8 x 4 bits, 4096 x 4096 x 8192 127 us (4.3e15 of codes).  The issue loop alone over random operands reaches 6.4e15.  Bound:
 // the matrix cores and power: over 16384 x 12288 x 4096 the clock falls to 1.8 - 1.9 GHz, and of its cycles the matrix cores are busy in
 // 49 %, LDS in 29 % (a quarter of that in conflicts).  Without its loads the same loop reaches 5.5e15, with loads that hit L2 4.6e15; misses and
 // the stores' share of memory are the rest.
@@ -127,7 +127,9 @@ template <int BQ> struct BigShape {
   static constexpr int SMEM = SC_BASE + 2 * SC;
   static_assert(SMEM <= 160 * 1024, "LDS budget");
 };
-constexpr int GROUP_P = 8;   // tile rows side by side
+// Tile rows side by side: the 32 CUs of an XCD work on 4 x 8 tiles, whose rows' operand stays in its L2 while the columns' passes (16384 x 12288
+// x 4096 with 4 / 6 / 8 / 16 of them 419 / 422 / 430 / 435 us, 4096 x 11008 x 8192 in 8 x 4 bits 387 / 385 / 391 / 405).
+constexpr int GROUP_P = 4;
 constexpr uint32_t PAST_THE_END = 0xf0000000u;   // behind any descriptor: arrives as zeros, is not stored
 constexpr int64_t WIDE_LDO = 1 << 24;            // 32 rows of so many floats stay below PAST_THE_END
 
