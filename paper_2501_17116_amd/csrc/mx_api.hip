@@ -129,7 +129,7 @@ extern "C" int mx_linear_fwd(const void* A, fp4_dtype dt, int64_t M, int64_t K, 
   if (!bits_ok(act_bits)) return FP4_ERR_DTYPE;
   if ((rc = check_mx(W, N, K))) return rc;
   if (saved && (rc = check_mx(saved, K, M))) return rc;
-  if (M == 0) return FP4_OK;
+  if (M == 0 || (N == 0 && !saved)) return FP4_OK;   // neither an output nor a checkpoint to fill
   if (!workspace || workspace_bytes < mx_workspace_bytes(FP4_OP_MX_FWD, M, K, N)) return FP4_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   if (!saved && K > 0 && N > 0 && mx_few_fuses(M, K, act_bits))

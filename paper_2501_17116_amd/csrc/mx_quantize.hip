@@ -398,6 +398,7 @@ void launch_tiles(const QuantArgs& a, int col_bits, hipStream_t s) {
 
 template <class T>
 int launch_quantize(const QuantArgs& a, int row_bits, int col_bits, hipStream_t s) {
+  if (row_bits == NO_AXIS && col_bits == NO_AXIS) return FP4_OK;
   if (col_bits == NO_AXIS) {
     const int per_row = (int)(mx_pitch_of(a.cols) / MX_PITCH);
     const int64_t units = a.rows * per_row;
