@@ -85,6 +85,7 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units
 // KiB at a time, columns of tiles read rows that far apart, and either may fall on a few of the memory's channels.  16384 x 4096 bf16, columns in
 // 4 bits 40.1 us with whole rows, 36.2 / 38.3 / 37.7 with 4 / 8 / 16; 8192 x 11008 51.0, 54.7 / 50.3 / 51.2; 4096 x 11008 fp32 46.4, 48.9 / 48.2 / 46.8.
 constexpr int GROUP_C = 16;
+constexpr int64_t NEAR_LD = 0xffffffffll / 32;   // bytes from row to row with which a tile's 32 rows stay within 2^32
 
 template <class T, int ROW, int COL, int TW>   // TW: waves
 __global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles_c, int64_t tiles) {
@@ -104,9 +105,11 @@ __global__ __launch_bounds__(TW * 64) void mx_tile_kernel(QuantArgs a, int tiles
   const int64_t row_pitch = mx_pitch_of(a.cols), col_pitch = mx_pitch_of(a.rows);
   const int piece = lane & 15, sub = lane >> 4;
   u32x4 w[8];
-  if (r0 + 32 <= a.rows && c0 + CW <= a.cols) {   // eight requests and nothing between them
+  // Inside: eight requests and nothing between them, with 32 bits for what lies between the tile's rows.  Rows too far apart for that go the
+  // edges' way, which counts in 64.
+  if (r0 + 32 <= a.rows && c0 + CW <= a.cols && a.ld <= NEAR_LD / E) {
     const uint8_t* const first = reinterpret_cast<const uint8_t*>(a.x) + (r0 * a.ld + c0) * E;
-    const uint32_t step = (uint32_t)a.ld * E;     // 32 rows are below 2^32 bytes
+    const uint32_t step = (uint32_t)a.ld * E;
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const u32x4*>(first + (i * 4 + sub) * step + piece * 16);
   } else {
