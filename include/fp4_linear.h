@@ -37,7 +37,8 @@
  *   - Every GEMM contracts over an axis whose length is a multiple of 32.
  *   - Workspaces: query with fp4_workspace_bytes(); contents on entry are ignored and
  *     on exit undefined.  Two calls may share a workspace only if stream order
- *     serializes them.  The query does not know alpha: it provides for residual
+ *     serializes them, all launches of the one before all of the other (two threads that
+ *     call on one stream need two).  The query does not know alpha: it provides for residual
  *     densities up to 20 %, i.e. alpha >= 0.9 (the paper uses 0.97 .. 0.999, Sec. 4.3).
  *     An alpha in (0.5, 0.9) is refused with FP4_ERR_ARG; outside (0.5, 1] likewise.
  *   - Residual capacity: the library never writes beyond `capacity` entries and never

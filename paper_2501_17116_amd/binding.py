@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 from typing import Optional, Tuple
 
 import torch
@@ -197,9 +198,11 @@ class Workspace:
     """A growable device byte buffer handed to the entry points as their workspace.
 
     One Workspace serves calls that stream order serializes (the ABI's workspace rule): use one
-    per stream.  Growing keeps the outgrown buffers alive until release(), because kernels
-    enqueued earlier may still be running in them and torch's allocator knows nothing of
-    streams other than the one a tensor was allocated on."""
+    per stream and thread, since a call is several launches and two threads' launches mix on a
+    stream, and one per captured graph that is replayed beside other calls.  Growing keeps the
+    outgrown buffers alive until release(), because kernels enqueued earlier may still be running
+    in them and torch's allocator knows nothing of streams other than the one a tensor was
+    allocated on."""
 
     def __init__(self, device="cuda"):
         self.device = device
@@ -218,15 +221,21 @@ class Workspace:
         self._outgrown.clear()
 
 
-_default_ws = {}   # (device index, stream handle) -> Workspace: never shared between streams
+_default_ws = {}   # (device index, stream handle, thread) -> Workspace: never shared between streams or threads
+
+
+def _default_workspace(device_index: int, stream: int) -> Workspace:
+    """The calling thread's for its stream.  (A thread that has ended leaves its own to the next one of its number, whose calls come later.)"""
+    key = (device_index, stream, threading.get_ident())
+    ws = _default_ws.get(key)
+    if ws is None:
+        ws = _default_ws[key] = Workspace(torch.device("cuda", device_index))
+    return ws
 
 
 def _ws(nbytes: int, ws: Optional[Workspace]) -> torch.Tensor:
     if ws is None:
-        key = (torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream)
-        ws = _default_ws.get(key)
-        if ws is None:
-            ws = _default_ws[key] = Workspace()
+        ws = _default_workspace(torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream)
     return ws.get(nbytes)
 
 
@@ -647,10 +656,7 @@ def _mx_ws(op: int, M: int, K: int, N: int, ws: Optional[Workspace], like: torch
         need = _mx_room[op, M, K, N] = workspace_bytes(op, M, K, N, FP4_BF16)
     stream = _stream_of(like)
     if ws is None:
-        key = (like.device.index, stream)
-        ws = _default_ws.get(key)
-        if ws is None:
-            ws = _default_ws[key] = Workspace(like.device)
+        ws = _default_workspace(like.device.index, stream)
     buf = ws.get(need)
     return buf.data_ptr(), buf.numel(), stream
 
