@@ -8,6 +8,7 @@ exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import threading
 from typing import Optional, Tuple
@@ -641,7 +642,9 @@ def _out(t: Optional[torch.Tensor], shape, dtype, device: torch.device, name: st
     return t
 
 
-_mx_room = {}   # (op, M, K, N) -> bytes: the query's answer does not change
+@functools.lru_cache(maxsize=1024)   # the answer to a query does not change; a server asks for ever new token counts
+def _mx_room(op: int, M: int, K: int, N: int) -> int:
+    return workspace_bytes(op, M, K, N, FP4_BF16)
 
 
 def _stream_of(t: torch.Tensor) -> int:
@@ -651,9 +654,7 @@ def _stream_of(t: torch.Tensor) -> int:
 
 def _mx_ws(op: int, M: int, K: int, N: int, ws: Optional[Workspace], like: torch.Tensor):
     """(workspace pointer, its bytes, stream handle) of an MX layer call."""
-    need = _mx_room.get((op, M, K, N))
-    if need is None:
-        need = _mx_room[op, M, K, N] = workspace_bytes(op, M, K, N, FP4_BF16)
+    need = _mx_room(op, M, K, N)
     stream = _stream_of(like)
     if ws is None:
         ws = _default_workspace(like.device.index, stream)
