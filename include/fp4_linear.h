@@ -13,7 +13,8 @@
  *
  * Conventions common to every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller unless a parameter
- *     says "host".  Matrices are row-major.  The library allocates no memory, keeps no
+ *     says "host"; they and `stream` belong to the calling thread's current device, to
+ *     which the kernels go.  Matrices are row-major.  The library allocates no memory, keeps no
  *     state between calls and never synchronizes: every call only enqueues kernels on
  *     `stream` (a hipStream_t passed as void*; NULL = the default stream), and on no
  *     other stream, so every entry point may be called while `stream` is being captured

@@ -178,11 +178,18 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _current(device: torch.device):
+    """Launches go to the current device, where another one's addresses mean nothing."""
+    if device.index != torch._C._cuda_getDevice():
+        raise ValueError("tensors and workspaces must live on the current device, cuda:%d; this one is on %s" % (torch._C._cuda_getDevice(), device))
+
+
 def _dev_check(*ts):
     for t in ts:
         if t is not None:
             if not t.is_cuda:
                 raise ValueError("tensors must live on the GPU")
+            _current(t.device)
             if not t.is_contiguous():
                 raise ValueError("tensors must be contiguous")
 
@@ -215,6 +222,8 @@ class Workspace:
             if self.buf.numel():
                 self._outgrown.append(self.buf)
             self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        if self.buf.is_cuda:
+            _current(self.buf.device)
         return self.buf
 
     def release(self) -> None:
@@ -648,7 +657,9 @@ def _mx_room(op: int, M: int, K: int, N: int) -> int:
 
 
 def _stream_of(t: torch.Tensor) -> int:
-    """Handle of the current stream of t's device.  (torch.cuda.current_stream() takes 4 us, as long as a small kernel.)"""
+    """Handle of the current stream of t's device, which has to be the current one.  (torch.cuda.current_stream() takes 4 us, as long as a
+    small kernel.)"""
+    _current(t.device)
     return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
@@ -713,7 +724,7 @@ def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, a
 def mx_gemm_by_tile(l: MxTensor, rt: MxTensor, tile: int, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mx_gemm by one kind of tile (16, 32, 64, 128, 192, 256), for tests and measuring; addend has the output's leading dimension."""
     out = _out(None, (l.lines, rt.lines), out_dtype, l.device, "out")
-    _check(lib().mx_gemm_by_tile(l.ref, rt.ref, _ptr(addend), _ptr(out), _dt(out), _ld(out, "out"), tile, _stream()), "mx_gemm_by_tile")
+    _check(lib().mx_gemm_by_tile(l.ref, rt.ref, _ptr(addend), _ptr(out), _dt(out), _ld(out, "out"), tile, _stream_of(out)), "mx_gemm_by_tile")
     return out
 
 
@@ -924,7 +935,8 @@ def fp4_host_round_codes(x_host):
 def fp4_device_round_codes(x):
     """fp32 CUDA tensor (numel a multiple of 8) -> uint8 codes, through the quantization kernels' packing routine."""
     import torch
-    assert x.is_cuda and x.dtype == torch.float32 and x.is_contiguous()
+    assert x.dtype == torch.float32
+    _dev_check(x)
     out = torch.empty(x.shape, dtype=torch.uint8, device=x.device)
     _check(lib().fp4_device_round_codes(x.data_ptr(), x.numel(), out.data_ptr(), _stream()), "fp4_device_round_codes")
     return out
@@ -935,6 +947,7 @@ def fp4_device_round_sweep(device="cuda:0") -> int:
     comparison-chain routine disagree; 0 is the only acceptable result."""
     import torch
     cnt = torch.zeros(1, dtype=torch.int64, device=device)
+    _dev_check(cnt)
     _check(lib().fp4_device_round_sweep(cnt.data_ptr(), _stream()), "fp4_device_round_sweep")
     return int(cnt.item())
 
