@@ -568,7 +568,7 @@ class MxTensor:
     codes [lines, mx_pitch(length) / 2] (4 bits) or [2, lines, mx_pitch(length) / 2] (8 bits), scales [lines, mx_pitch(length) / 32],
     uint8.  transposed: the lines are the columns of the matrix that the tensor stands for."""
 
-    __slots__ = ("_codes", "_scales", "_room", "bits", "lines", "length", "transposed", "device", "c", "ref")
+    __slots__ = ("_codes", "_scales", "_room", "bits", "lines", "length", "transposed", "device", "use", "c", "ref")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, length: int, transposed: bool = False):
         pitch, shape, lines = mx_pitch(length), tuple(codes.shape), scales.shape[0]
@@ -585,6 +585,7 @@ class MxTensor:
 
     def _set(self, codes, scales, bits, lines, length, transposed, device):
         self.bits, self.lines, self.length, self.transposed, self.device = bits, lines, length, transposed, device
+        self.use = None   # "fwd" or "bwd": which of a layer's two forms of its weights this is
         self.c = fp4_mx(codes, scales, lines, length, bits)
         self.ref = C.byref(self.c)
 
@@ -663,6 +664,16 @@ def _stream_of(t: torch.Tensor) -> int:
     return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
+def _along(t: MxTensor, transposed: bool, name: str):
+    if bool(t.transposed) != transposed:
+        raise ValueError("%s must %sbe marked transposed: %s" % (name, "" if transposed else "not ", "its lines are columns" if transposed else "its lines are rows"))
+
+
+def _weights_for(W: MxTensor, use: str):
+    if W.use is not None and W.use != use:
+        raise ValueError("these weights are laid out for the other pass: this one takes MxWeights.%s" % use)
+
+
 def _mx_ws(op: int, M: int, K: int, N: int, ws: Optional[Workspace], like: torch.Tensor):
     """(workspace pointer, its bytes, stream handle) of an MX layer call."""
     need = _mx_room(op, M, K, N)
@@ -674,7 +685,7 @@ def _mx_ws(op: int, M: int, K: int, N: int, ws: Optional[Workspace], like: torch
 
 
 def mx_quantize(x: torch.Tensor, axis: int, bits: int = 4, out: Optional[MxTensor] = None) -> MxTensor:
-    """x along its rows (FP4_AXIS_ROW) or along its columns, transposed (FP4_AXIS_COL)."""
+    """x along its rows (FP4_AXIS_ROW) or along its columns, transposed (FP4_AXIS_COL).  An `out` has bits and an orientation of its own."""
     if axis not in (FP4_AXIS_ROW, FP4_AXIS_COL):
         raise ValueError("MX blocks lie along rows or columns")
     ld = _ld(x, "x")
@@ -682,6 +693,7 @@ def mx_quantize(x: torch.Tensor, axis: int, bits: int = 4, out: Optional[MxTenso
     lines, length = (rows, cols) if axis == FP4_AXIS_ROW else (cols, rows)
     if out is None:
         out = mx_empty(lines, length, bits, axis == FP4_AXIS_COL, x.device)
+    _along(out, axis == FP4_AXIS_COL, "out")
     _same_device(x, out)
     _check(lib().mx_quantize(x.data_ptr(), _dt(x), rows, cols, ld, out.ref if axis == FP4_AXIS_ROW else None,
                              out.ref if axis == FP4_AXIS_COL else None, _stream_of(x)), "mx_quantize")
@@ -749,7 +761,8 @@ def mx_checkpoint_save(x: torch.Tensor, bits: int = 8) -> MxTensor:
 
 class MxWeights:
     """Both orientations of a layer's weights W [K, N]: fwd (lines N, length K) for the forward pass, bwd (lines K, length N) for the
-    activation gradient.  Made once per weight version."""
+    activation gradient.  Made once per weight version.  Those of mx_prepare_weights are refused by the other's pass, also where W is
+    square and their sizes agree."""
 
     def __init__(self, fwd: MxTensor, bwd: MxTensor):
         self.fwd, self.bwd = fwd, bwd
@@ -757,6 +770,7 @@ class MxWeights:
 
 def mx_prepare_weights(W: torch.Tensor) -> MxWeights:
     bwd, fwd = mx_quantize_both(W)
+    fwd.use, bwd.use = "fwd", "bwd"
     return MxWeights(fwd, bwd)
 
 
@@ -768,8 +782,11 @@ def mx_linear_fwd(A: torch.Tensor, W: MxTensor, act_bits: int = 4, saved: Option
     N = W.lines
     if W.length != K:
         raise ValueError("A [M,K] and W (lines N, length K) must agree in K")
-    if saved is not None and (saved.lines, saved.length) != (K, M):
-        raise ValueError("the checkpoint holds %d x %d activations, not %d x %d" % (saved.length, saved.lines, M, K))
+    _weights_for(W, "fwd")
+    if saved is not None:
+        if (saved.lines, saved.length) != (K, M):
+            raise ValueError("the checkpoint holds %d x %d activations, not %d x %d" % (saved.length, saved.lines, M, K))
+        _along(saved, True, "the checkpoint")
     _same_device(A, W, saved)
     Y = _out(Y, (M, N), A.dtype, A.device, "Y")
     room, nbytes, stream = _mx_ws(FP4_OP_MX_FWD, M, K, N, ws, A)
@@ -785,6 +802,7 @@ def mx_linear_bwd_dgrad(dY: torch.Tensor, W: MxTensor, dA: Optional[torch.Tensor
     K = W.lines
     if W.length != N:
         raise ValueError("dY [M,N] and W (lines K, length N) must agree in N")
+    _weights_for(W, "bwd")
     _same_device(dY, W)
     dA = _out(dA, (M, K), dY.dtype, dY.device, "dA")
     room, nbytes, stream = _mx_ws(FP4_OP_MX_DGRAD, M, K, N, ws, dY)
@@ -801,6 +819,7 @@ def mx_linear_bwd_wgrad(dY: torch.Tensor, saved: MxTensor, grad_bits: int = 4, d
     K = saved.lines
     if saved.length != M:
         raise ValueError("dY [M,N] and the checkpoint must agree in M")
+    _along(saved, True, "the checkpoint")
     if accumulate and dW is None:
         raise ValueError("accumulate needs the dW to add to")
     _same_device(dY, saved)
@@ -819,6 +838,8 @@ def mx_linear_bwd(dY: torch.Tensor, saved: MxTensor, W: MxTensor, grad_bits: int
     K = W.lines
     if W.length != N or (saved.lines, saved.length) != (K, M):
         raise ValueError("dY [M,N], W (lines K, length N) and the checkpoint must agree")
+    _weights_for(W, "bwd")
+    _along(saved, True, "the checkpoint")
     if accumulate and dW is None:
         raise ValueError("accumulate needs the dW to add to")
     _same_device(dY, W, saved)
