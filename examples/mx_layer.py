@@ -20,12 +20,13 @@ from paper_2501_17116_amd import binding as b  # noqa: E402
 
 
 class MxLinear(torch.nn.Module):
-    """Y = A W with W [K, N] an fp32 master; the weight gradient goes into W.grad by itself, micro-batch on micro-batch."""
+    """Y = A W with W [K, N] an fp32 master.  Its gradient comes by autograd, or with add_in_place is added to W.grad in the product's own
+    launch, which saves a pass over it for every micro-batch; hooks on W and torch.autograd.grad then do not see it."""
 
-    def __init__(self, K: int, N: int, generator: torch.Generator):
+    def __init__(self, K: int, N: int, generator: torch.Generator, add_in_place: bool = False):
         super().__init__()
         self.W = torch.nn.Parameter(torch.randn(K, N, generator=generator, device="cuda") / K ** 0.5)
-        self.W.grad = torch.zeros_like(self.W)
+        self.add_in_place = add_in_place
         self.prepare()
 
     def prepare(self):
@@ -33,20 +34,33 @@ class MxLinear(torch.nn.Module):
         self.wq = b.mx_prepare_weights(self.W.detach())
 
     def forward(self, A: torch.Tensor) -> torch.Tensor:
-        return _MxLinear.apply(A, self) if torch.is_grad_enabled() else b.mx_linear_fwd(A, self.wq.fwd)
+        return _MxLinear.apply(A, self.W, self) if torch.is_grad_enabled() else b.mx_linear_fwd(A, self.wq.fwd)
 
 
 class _MxLinear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, A, layer):
-        ctx.layer = layer
-        ctx.saved = b.mx_checkpoint(*A.shape)          # 8 bits an activation instead of the activation
-        return b.mx_linear_fwd(A, layer.wq.fwd, saved=ctx.saved)
+    def forward(ctx, A, W, layer):
+        ctx.layer, ctx.wq = layer, layer.wq            # the weights of this pass, whatever is prepared before its backward
+        ctx.saved = b.mx_checkpoint(*A.shape) if ctx.needs_input_grad[1] else None   # 8 bits an activation instead of the activation
+        return b.mx_linear_fwd(A, ctx.wq.fwd, saved=ctx.saved)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dY):
-        dA, _ = b.mx_linear_bwd(dY.contiguous(), ctx.saved, ctx.layer.wq.bwd, grad_bits=8, dW=ctx.layer.W.grad, accumulate=True)
-        return dA, None
+        need_a, need_w, _ = ctx.needs_input_grad
+        dY, W = dY.contiguous(), ctx.layer.W
+        into = W.grad if need_w and ctx.layer.add_in_place else None
+        add = {"grad_bits": 8, "dW": into, "accumulate": into is not None}
+        dA = dW = None
+        if need_a and need_w:
+            dA, dW = b.mx_linear_bwd(dY, ctx.saved, ctx.wq.bwd, **add)
+        elif need_w:
+            dW = b.mx_linear_bwd_wgrad(dY, ctx.saved, **add)
+        elif need_a:
+            dA = b.mx_linear_bwd_dgrad(dY, ctx.wq.bwd)
+        if need_w and ctx.layer.add_in_place:
+            W.grad, dW = dW, None
+        return dA, dW, None
 
 
 def _network(layers, A):
@@ -62,14 +76,14 @@ def train(layers, teacher, steps, tokens, micro_batches, width, seed, report=Non
     for step in range(steps):
         total = 0.0
         for _ in range(micro_batches):
-            A = torch.randn(tokens // micro_batches, width, generator=g, device="cuda").requires_grad_()
-            want = torch.nn.functional.silu(A.detach() @ teacher[0]) @ teacher[1]
+            A = torch.randn(tokens // micro_batches, width, generator=g, device="cuda")
+            want = torch.nn.functional.silu(A @ teacher[0]) @ teacher[1]
             loss = (_network(layers, A) - want).square().mean() / micro_batches
             loss.backward()
             total += float(loss.detach())
         opt.step()
+        opt.zero_grad()
         for l in layers:
-            l.W.grad.zero_()
             l.prepare()
         if step >= steps - max(1, steps // 10):
             last.append(total)
@@ -82,7 +96,6 @@ class _PlainLinear(torch.nn.Module):
     def __init__(self, W):
         super().__init__()
         self.W = torch.nn.Parameter(W.clone())
-        self.W.grad = torch.zeros_like(self.W)
 
     def prepare(self):
         pass
@@ -102,7 +115,7 @@ def main(argv=None, report=print):
     g = torch.Generator(device="cuda").manual_seed(1)
     teacher = [torch.randn(a.width, a.hidden, generator=g, device="cuda") / a.width ** 0.5,
                torch.randn(a.hidden, a.width, generator=g, device="cuda") / a.hidden ** 0.5]
-    layers = [MxLinear(a.width, a.hidden, g), MxLinear(a.hidden, a.width, g)]
+    layers = [MxLinear(a.width, a.hidden, g, add_in_place=True), MxLinear(a.hidden, a.width, g, add_in_place=True)]
     plain = [_PlainLinear(l.W.detach()) for l in layers]
     with torch.no_grad():
         A = torch.randn(a.tokens, a.width, generator=g, device="cuda")
