@@ -716,27 +716,34 @@ def mx_dequantize(t: MxTensor, dtype: torch.dtype = torch.bfloat16, out: Optiona
     return x
 
 
-def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None,
-            out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """l . rt^T over their lines' common length (+ addend)."""
+def _gemm_arguments(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype, addend: Optional[torch.Tensor], out: Optional[torch.Tensor]):
+    """(out, its leading dimension, the addend's address) of a product, checked."""
     if l.length != rt.length:
         raise ValueError("operands disagree in the contraction's length")
     _same_device(l, rt)
     out = _out(out, (l.lines, rt.lines), out.dtype if out is not None else out_dtype, l.device, "out")
     ldo = _ld(out, "out")
-    if addend is not None:
-        if addend.shape != out.shape or addend.dtype != torch.float32 or addend.device != out.device:
-            raise ValueError("addend must be %s float32 on %s" % (tuple(out.shape), out.device))
-        if _ld(addend, "addend") != ldo:
-            raise ValueError("addend and out must have the same leading dimension")
-    _check(lib().mx_gemm(l.ref, rt.ref, None if addend is None else addend.data_ptr(), out.data_ptr(), _dt(out), ldo, _stream_of(out)), "mx_gemm")
+    if addend is None:
+        return out, ldo, None
+    if addend.shape != out.shape or addend.dtype != torch.float32 or addend.device != out.device:
+        raise ValueError("addend must be %s float32 on %s" % (tuple(out.shape), out.device))
+    if _ld(addend, "addend") != ldo:
+        raise ValueError("addend and out must have the same leading dimension")
+    return out, ldo, addend.data_ptr()
+
+
+def mx_gemm(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """l . rt^T over their lines' common length (+ addend)."""
+    out, ldo, add = _gemm_arguments(l, rt, out_dtype, addend, out)
+    _check(lib().mx_gemm(l.ref, rt.ref, add, out.data_ptr(), _dt(out), ldo, _stream_of(out)), "mx_gemm")
     return out
 
 
 def mx_gemm_by_tile(l: MxTensor, rt: MxTensor, tile: int, out_dtype: torch.dtype = torch.float32, addend: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mx_gemm by one kind of tile (16, 32, 64, 128, 192, 256), for tests and measuring; addend has the output's leading dimension."""
-    out = _out(None, (l.lines, rt.lines), out_dtype, l.device, "out")
-    _check(lib().mx_gemm_by_tile(l.ref, rt.ref, _ptr(addend), _ptr(out), _dt(out), _ld(out, "out"), tile, _stream_of(out)), "mx_gemm_by_tile")
+    out, ldo, add = _gemm_arguments(l, rt, out_dtype, addend, None)
+    _check(lib().mx_gemm_by_tile(l.ref, rt.ref, add, out.data_ptr(), _dt(out), ldo, tile, _stream_of(out)), "mx_gemm_by_tile")
     return out
 
 
