@@ -162,12 +162,14 @@ def _check(status: int, where: str):
         raise Fp4Error(status, where)
 
 
+_DTYPES = {torch.float32: FP4_F32, torch.bfloat16: FP4_BF16}
+
+
 def _dt(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return FP4_F32
-    if t.dtype == torch.bfloat16:
-        return FP4_BF16
-    raise TypeError("dtype must be float32 or bfloat16, got %s" % t.dtype)
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise TypeError("dtype must be float32 or bfloat16, got %s" % t.dtype)
+    return dt
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -175,21 +177,24 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
 
 
-def _current(device: torch.device):
-    """Launches go to the current device, where another one's addresses mean nothing."""
-    if device.index != torch._C._cuda_getDevice():
-        raise ValueError("tensors and workspaces must live on the current device, cuda:%d; this one is on %s" % (torch._C._cuda_getDevice(), device))
+def _current(index: int) -> int:
+    """index, if that is the current device: launches go there, and another one's addresses mean nothing to them."""
+    if index != torch._C._cuda_getDevice():
+        raise ValueError("tensors and workspaces must live on the current device, cuda:%d; this one is on cuda:%d" % (torch._C._cuda_getDevice(), index))
+    return index
 
 
 def _dev_check(*ts):
+    current = None
     for t in ts:
         if t is not None:
             if not t.is_cuda:
                 raise ValueError("tensors must live on the GPU")
-            _current(t.device)
+            if t.device.index != current:
+                current = _current(t.device.index)
             if not t.is_contiguous():
                 raise ValueError("tensors must be contiguous")
 
@@ -218,12 +223,16 @@ class Workspace:
         self._outgrown = []
 
     def get(self, nbytes: int) -> torch.Tensor:
+        buf = self._sized(nbytes)
+        if buf.is_cuda:
+            _current(buf.device.index)
+        return buf
+
+    def _sized(self, nbytes: int) -> torch.Tensor:
         if self.buf.numel() < nbytes:
             if self.buf.numel():
                 self._outgrown.append(self.buf)
             self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        if self.buf.is_cuda:
-            _current(self.buf.device)
         return self.buf
 
     def release(self) -> None:
@@ -231,12 +240,13 @@ class Workspace:
         self._outgrown.clear()
 
 
+_thread = threading.get_ident
 _default_ws = {}   # (device index, stream handle, thread) -> Workspace: never shared between streams or threads
 
 
 def _default_workspace(device_index: int, stream: int) -> Workspace:
     """The calling thread's for its stream.  (A thread that has ended leaves its own to the next one of its number, whose calls come later.)"""
-    key = (device_index, stream, threading.get_ident())
+    key = (device_index, stream, _thread())
     ws = _default_ws.get(key)
     if ws is None:
         ws = _default_ws[key] = Workspace(torch.device("cuda", device_index))
@@ -245,7 +255,7 @@ def _default_workspace(device_index: int, stream: int) -> Workspace:
 
 def _ws(nbytes: int, ws: Optional[Workspace]) -> torch.Tensor:
     if ws is None:
-        ws = _default_workspace(torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream)
+        return _default_workspace(torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream)._sized(nbytes)
     return ws.get(nbytes)
 
 
@@ -626,17 +636,19 @@ def _ld(t: torch.Tensor, name: str) -> int:
     """Leading dimension of a matrix whose rows may lie apart."""
     if not t.is_cuda:
         raise ValueError("tensors must live on the GPU")
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError("%s must be a matrix" % name)
-    (rows, cols), (ld, step) = t.shape, t.stride()
+    (rows, cols), (ld, step) = shape, t.stride()
     if step != 1 and cols > 1:
         raise ValueError("%s's rows must be contiguous" % name)
     return ld if rows > 1 and cols > 0 else max(8, -(-cols // 8) * 8)
 
 
 def _same_device(x, *mx: Optional[MxTensor]):
+    device = x.device
     for t in mx:
-        if t is not None and t.device != x.device:
+        if t is not None and t.device != device:
             raise ValueError("all tensors must live on one device")
 
 
@@ -660,8 +672,10 @@ def _mx_room(op: int, M: int, K: int, N: int) -> int:
 def _stream_of(t: torch.Tensor) -> int:
     """Handle of the current stream of t's device, which has to be the current one.  (torch.cuda.current_stream() takes 4 us, as long as a
     small kernel.)"""
-    _current(t.device)
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+    index = t.device.index
+    if index != torch._C._cuda_getDevice():
+        _current(index)
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _along(t: MxTensor, transposed: bool, name: str):
@@ -669,18 +683,15 @@ def _along(t: MxTensor, transposed: bool, name: str):
         raise ValueError("%s must %sbe marked transposed: %s" % (name, "" if transposed else "not ", "its lines are columns" if transposed else "its lines are rows"))
 
 
-def _weights_for(W: MxTensor, use: str):
-    if W.use is not None and W.use != use:
-        raise ValueError("these weights are laid out for the other pass: this one takes MxWeights.%s" % use)
+def _other_pass(use: str):
+    raise ValueError("these weights are laid out for the other pass: this one takes MxWeights.%s" % use)
 
 
 def _mx_ws(op: int, M: int, K: int, N: int, ws: Optional[Workspace], like: torch.Tensor):
     """(workspace pointer, its bytes, stream handle) of an MX layer call."""
     need = _mx_room(op, M, K, N)
     stream = _stream_of(like)
-    if ws is None:
-        ws = _default_workspace(like.device.index, stream)
-    buf = ws.get(need)
+    buf = _default_workspace(like.device.index, stream)._sized(need) if ws is None else ws.get(need)
     return buf.data_ptr(), buf.numel(), stream
 
 
@@ -720,7 +731,8 @@ def _gemm_arguments(l: MxTensor, rt: MxTensor, out_dtype: torch.dtype, addend: O
     """(out, its leading dimension, the addend's address) of a product, checked."""
     if l.length != rt.length:
         raise ValueError("operands disagree in the contraction's length")
-    _same_device(l, rt)
+    if l.device != rt.device:
+        raise ValueError("all tensors must live on one device")
     out = _out(out, (l.lines, rt.lines), out.dtype if out is not None else out_dtype, l.device, "out")
     ldo = _ld(out, "out")
     if addend is None:
@@ -789,7 +801,8 @@ def mx_linear_fwd(A: torch.Tensor, W: MxTensor, act_bits: int = 4, saved: Option
     N = W.lines
     if W.length != K:
         raise ValueError("A [M,K] and W (lines N, length K) must agree in K")
-    _weights_for(W, "fwd")
+    if W.use == "bwd":
+        _other_pass("fwd")
     if saved is not None:
         if (saved.lines, saved.length) != (K, M):
             raise ValueError("the checkpoint holds %d x %d activations, not %d x %d" % (saved.length, saved.lines, M, K))
@@ -809,7 +822,8 @@ def mx_linear_bwd_dgrad(dY: torch.Tensor, W: MxTensor, dA: Optional[torch.Tensor
     K = W.lines
     if W.length != N:
         raise ValueError("dY [M,N] and W (lines K, length N) must agree in N")
-    _weights_for(W, "bwd")
+    if W.use == "fwd":
+        _other_pass("bwd")
     _same_device(dY, W)
     dA = _out(dA, (M, K), dY.dtype, dY.device, "dA")
     room, nbytes, stream = _mx_ws(FP4_OP_MX_DGRAD, M, K, N, ws, dY)
@@ -845,7 +859,8 @@ def mx_linear_bwd(dY: torch.Tensor, saved: MxTensor, W: MxTensor, grad_bits: int
     K = W.lines
     if W.length != N or (saved.lines, saved.length) != (K, M):
         raise ValueError("dY [M,N], W (lines K, length N) and the checkpoint must agree")
-    _weights_for(W, "bwd")
+    if W.use == "fwd":
+        _other_pass("bwd")
     _along(saved, True, "the checkpoint")
     if accumulate and dW is None:
         raise ValueError("accumulate needs the dW to add to")
