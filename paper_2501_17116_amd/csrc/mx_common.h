@@ -4,8 +4,9 @@
 // what is left at an eighth of the scale.  8 bits are two codes and not one E4M3 code because the matrix cores lose bits of 8-bit
 // products: beside a large product of the same instruction the small ones are cut off at 2^-13 or so of it (measured, normal data: 5e-6
 // of the result with one E4M3 operand, 1.5e-5 with two), while products of E2M1 codes come out exactly; two 4-bit instructions take as
-// long as one 8-bit one; and a uniform grid of sixteenths keeps more of the values: 37.5 dB on normal data (E4M3: 31.5), 34.8 on
-// Student-t with three degrees of freedom.
+// long as one 8-bit one; and their grid keeps more of the values: 37.5 dB on normal data (E4M3: 31.5), 34.8 on Student-t with three
+// degrees of freedom.  In units of s it has every sixteenth up to 2 1/4; beyond, sixteenths within a quarter of a code, eighths further from
+// one, and between 4 and 6 and above 6 quarters as well, with one gap of a half from 4 3/4 to 5 1/4; 6 3/4 is its largest value.
 //
 // A line's codes take pitch(length) elements, length rounded up to 512: a line of codes begins at a multiple of 256 bytes, its scales at
 // a multiple of 16, and no kernel meets a line's end inside a load.  What lies behind `length` is the code 0 under a finite scale.  The

@@ -5,7 +5,7 @@
 // the waves' order.  Each row of R is read by one workgroup for every 16 NT tokens; the fewer columns a workgroup has, the more
 // often the tokens are read.
 //
-// Measured (other weights each call): a launch that has next to nothing to do takes 3.4 us in a graph; one token, 4096 x 4096 5.3, 4096 x 11008 9.5 - 10,
+// Measured (other weights each call): a launch that has next to nothing to do takes 3.4 us in a graph; one token, inputs x outputs 4096 x 4096 5.3, 4096 x 11008 9.5 - 10,
 // 13824 x 5120 13.5 - 15, so beyond the launch the weights come at 3.5 - 4 TB/s.  24 tokens in 8 bits, 4096 x 11008 11.7 and 3.4 for their codes.  Tried:
 // tokens and weights of two units on their way in registers, 128 bytes of a row a unit where those run short: within 2 % at 4096 x 4096 and
 // 13824 x 5120, 5 - 10 % slower at 4096 x 11008; the smaller pieces cost what the waits gave.

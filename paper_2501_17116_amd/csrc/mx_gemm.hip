@@ -7,6 +7,8 @@
 // that add to the same accumulators.  Products of E2M1 codes are exact in the matrix core; sums are fp32; the one rounding to a narrower
 // output type is the store's.
 //
+// Sizes in this file are P x Q x contraction, outputs first.
+//
 // v_mfma_scale_f32_32x32x64_f8f6f4, operand layout (found with one-hot operands): lane (l32, h) holds elements 32 h .. 32 h + 31 of row
 // l32, sixteen bytes, and brings their scale, in the byte of its scale register that the instruction names.  A scale byte of 255 makes
 // the row NaN, also over zero codes.

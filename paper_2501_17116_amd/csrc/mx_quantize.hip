@@ -78,7 +78,9 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(QuantArgs a, int64_t units
 // A wave takes 32 rows x 256 bytes of columns, one block of every column, a workgroup eight waves' rows.  The columns' codes pass through LDS
 // once more, so that they leave as whole 128-byte lines (256 rows of 4-bit codes); four waves, half lines, were slower by a seventh (4 bits)
 // and a fifth (8 bits).  16384 x 4096 bf16: columns in 4 bits 35.8 us, in 8 bits 40.0, rows and columns in 4 bits 44.9, rows in 4 and columns in 8
-// 49.3 (4.6 - 5.1 TB/s); 4096 x 11008 fp32, both in 4 bits 53.4 (4.3).  Bound by memory; what remains above the rows' rate are some 700 vector
+// 49.3 (4.6 - 5.1 TB/s); 4096 x 11008 fp32, both in 4 bits 53.4 (4.3).  With one to six workgroups a CU, which load, compute and store
+// together, it stays below that: bf16, both in 4 bits 2048 x 5504 14.0 us (2.5 TB/s), 8192 x 5504 37.4 (3.7), in 4 and 8 bits 8192 x 2048 18.5 (3.2).
+// Bound by memory; what remains above the rows' rate are some 700 vector
 // instructions a wave, which four waves a SIMD do not hide altogether.  Tensors that do not give every CU such a workgroup are one wave's chain of requests and
 // instructions long; there a workgroup has two waves (1055 x 1384: rows and columns in 4 bits 5.7 us in the kernel).
 // What the order of the tiles costs (GROUP_C side by side before the next rows): whole rows of tiles write one line of the output every so many
