@@ -103,7 +103,11 @@ typedef enum {
   FP4_OP_MX_FWD = 9,   /* mx_linear_fwd                                                   */
   FP4_OP_MX_DGRAD = 10,/* mx_linear_bwd_dgrad                                             */
   FP4_OP_MX_WGRAD = 11,/* mx_linear_bwd_wgrad                                             */
-  FP4_OP_MX_BWD = 12   /* mx_linear_bwd                                                   */
+  FP4_OP_MX_BWD = 12,  /* mx_linear_bwd                                                   */
+  FP4_OP_HP_NORM_BWD = 13, /* hp_norm_bwd  (M, K = D, N ignored)                          */
+  FP4_OP_HP_EMBED_BWD = 14,/* hp_embed_bwd (M, K = D, N = V)                              */
+  FP4_OP_HP_HEAD_FWD = 15, /* hp_head_fwd  (M, K = D, N = V)                              */
+  FP4_OP_HP_HEAD_BWD = 16  /* hp_head_bwd  (M, K = D, N = V)                              */
 } fp4_op;
 
 /* What the forward pass leaves for the weight-gradient pass (Sec. 3.1 needs the
@@ -359,6 +363,70 @@ int mx_linear_bwd_wgrad(const void* dY, fp4_dtype dt, int64_t M, int64_t K, int6
 int mx_linear_bwd(const void* dY, fp4_dtype dt, int64_t M, int64_t K, int64_t N, int64_t ldy, const fp4_mx* W, const fp4_mx* saved,
                   int grad_bits, void* dA, int64_t lda, int accumulate, float* dW, int64_t ldw, void* workspace,
                   size_t workspace_bytes, void* stream);
+
+/* ---- what stays in high precision around the layers (Sec. 4.1: everything but the GEMMs of the blocks) ----
+ * The joints of a model's blocks (norms, gate, residual stream), its embedding, and its head with the loss.  Matrices of tokens are
+ * [M x D], D channels; base pointers 16-byte aligned, leading dimensions multiples of 8 as everywhere; what lies between D and a leading
+ * dimension is never written.  M and D from 0 on (0: sums become 0, or stay where they are accumulated to); dimensions above 2^21 are refused
+ * with FP4_ERR_LIMIT.  All sums are fp32, in an order that only the sizes decide: equal calls give equal bits.
+ *
+ * The joint of two blocks.  In fp32, each output rounded once:
+ *   u = block, or with w_after   block r_after w_after,   r_after = 1 / sqrt(mean(block^2) + eps)
+ *   h = scale x + u, or with a gate   scale x + gate u       the residual stream
+ *   y = h r_before w_before,   r_before = 1 / sqrt(mean(h^2) + eps)      what the next block reads (from h as it is before its rounding)
+ * D <= 16384. */
+typedef struct {
+  const void* w_before;   /* [D], or NULL: y is not formed                                                             */
+  const void* w_after;    /* [D], or NULL: the block's output is taken as it is                                        */
+  const void* gate;       /* NULL: 1; [D], one for all tokens, with ld_gate = 0; otherwise [M x D] with leading dimension ld_gate */
+  int64_t ld_gate;
+  float scale, eps;       /* eps > 0                                                                                   */
+} hp_norm;
+
+/* block NULL: h = scale x (then neither w_after nor gate).  h and y may be NULL, not both; y needs w_before.  r_before, r_after: optional,
+ * [M] each, for the backward pass.  h or y may be x or block themselves, with the same leading dimension.  Weights and gate have type dt. */
+int hp_norm_fwd(const hp_norm* norm, fp4_dtype dt, int64_t M, int64_t D, const void* x, int64_t ldx, const void* block, int64_t ld_block,
+                void* h, int64_t ldh, void* y, int64_t ldy, float* r_before, float* r_after, void* stream);
+
+/* dy, dh: gradients of y and of h (the stream's own way on); either may be NULL, not both.  h, block, r_before, r_after: of the forward
+ * pass (h and r_before with dy; block where a gradient needs it; r_after with w_after).  Each output may be NULL:
+ *   dx, dblock [M x D] of type dt; may be dh or dy themselves, with the same leading dimension
+ *   dgate      ld_gate = 0: fp32 [D]; otherwise [M x D] of type dt, leading dimension ld_dgate
+ *   dw_before, dw_after  fp32 [D]
+ * accumulate != 0 adds to what the sums over tokens (dw_before, dw_after, dgate [D]) hold.
+ * Workspace: fp4_workspace_bytes(FP4_OP_HP_NORM_BWD, M, D, 0, dt). */
+int hp_norm_bwd(const hp_norm* norm, fp4_dtype dt, int64_t M, int64_t D, const void* dy, int64_t ld_dy, const void* dh, int64_t ld_dh,
+                const void* h, int64_t ldh, const void* block, int64_t ld_block, const float* r_before, const float* r_after,
+                void* dx, int64_t ld_dx, void* dblock, int64_t ld_dblock, void* dgate, int64_t ld_dgate, float* dw_before, float* dw_after,
+                int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/* y[t] = scale table[ids[t]], table [V x D].  An id outside [0, V) (padding) gives zeros. */
+int hp_embed_fwd(const int64_t* ids, fp4_dtype dt, int64_t M, int64_t D, int64_t V, const void* table, int64_t ld_table, float scale,
+                 void* y, int64_t ldy, void* stream);
+
+/* dtable[v] (+)= scale sum of dy[t] over the tokens with ids[t] = v, in fp32, the tokens in order.  accumulate != 0 adds, and leaves the rows of absent ids
+ * alone; otherwise these become 0.  Ids outside [0, V) count nowhere.  dtable [V x D] fp32.
+ * Workspace: fp4_workspace_bytes(FP4_OP_HP_EMBED_BWD, M, D, V, dt). */
+int hp_embed_bwd(const int64_t* ids, fp4_dtype dt, int64_t M, int64_t D, int64_t V, const void* dy, int64_t ld_dy, float scale, int accumulate,
+                 float* dtable, int64_t ld_dtable, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The head and its loss.  Logits z[t, v] = x[t] . w[v], w [V x D] (the embedding's layout, which may be tied to it), bf16 both, D a
+ * multiple of 8, leading dimensions at most 2^21; they are formed in pieces and not kept.
+ *   lse[t]  = log sum over v of exp(z[t, v])
+ *   loss[t] = lse[t] - z[t, targets[t]];  0 where the target lies outside [0, V)
+ * Either output may be NULL, not both.  V >= 1.  Workspace: fp4_workspace_bytes(FP4_OP_HP_HEAD_FWD, M, D, V, dt). */
+int hp_head_fwd(const void* x, const void* w, const int64_t* targets, fp4_dtype dt, int64_t M, int64_t D, int64_t V, int64_t ldx, int64_t ldw,
+                float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients under dloss [M], each token's loss's; a target outside [0, V) leaves its token without one, whatever its dloss is.
+ *   dz[t, v] = dloss[t] (exp(z[t, v] - lse[t]) - [v = targets[t]]);   dx = dz w (bf16),   dw = dz^T x (dw_dt; fp32: accumulate != 0 adds)
+ * Either may be NULL, not both.  The products' operands are rounded to 11 bits (fp16 under powers of two: exact for w and for dloss x but
+ * for its product's rounding), sums are fp32: dw in fp32 is as near as that.  A target's entry below 2^-40 of 1 and weights below 2^-39
+ * of their largest are taken as 0.
+ * Workspace: fp4_workspace_bytes(FP4_OP_HP_HEAD_BWD, M, D, V, dt); dz takes at most 2^27 elements and 256 a token of it, twice. */
+int hp_head_bwd(const void* x, const void* w, const int64_t* targets, const float* lse, const float* dloss, fp4_dtype dt, int64_t M, int64_t D,
+                int64_t V, int64_t ldx, int64_t ldw, void* dx, int64_t ld_dx, void* dw, fp4_dtype dw_dt, int64_t ld_dw, int accumulate,
+                void* workspace, size_t workspace_bytes, void* stream);
 
 /* One 4-bit code per output byte (for inspecting packed tensors). */
 int fp4_unpack(const uint8_t* codes, int64_t rows, int64_t cols, uint8_t* one_per_byte,

@@ -11,7 +11,7 @@ import ctypes as C
 import functools
 import os
 import threading
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -23,6 +23,7 @@ FP4_AXIS_ROW, FP4_AXIS_COL, FP4_AXIS_TENSOR = 0, 1, 2
 FP4_OCC_TENSOR, FP4_OCC_TOKEN = 0, 1
 FP4_OP_QUANTIZE, FP4_OP_OCC, FP4_OP_FWD, FP4_OP_DGRAD, FP4_OP_WGRAD, FP4_OP_SPMM, FP4_OP_PREPARE, FP4_OP_FWD_MIXED, FP4_OP_BWD = range(9)
 FP4_OP_MX_FWD, FP4_OP_MX_DGRAD, FP4_OP_MX_WGRAD, FP4_OP_MX_BWD = range(9, 13)
+FP4_OP_HP_NORM_BWD, FP4_OP_HP_EMBED_BWD, FP4_OP_HP_HEAD_FWD, FP4_OP_HP_HEAD_BWD = range(13, 17)
 FP4_FMT_E2M1, FP4_FMT_E4M3 = 0, 1
 
 _lib = None
@@ -46,6 +47,11 @@ class fp4_weight_cache(C.Structure):
 
 class fp4_mx(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("lines", C.c_int64), ("length", C.c_int64), ("bits", C.c_int32)]
+
+
+class hp_norm(C.Structure):
+    _fields_ = [("w_before", C.c_void_p), ("w_after", C.c_void_p), ("gate", C.c_void_p), ("ld_gate", C.c_int64), ("scale", C.c_float),
+                ("eps", C.c_float)]
 
 
 def lib() -> C.CDLL:
@@ -104,6 +110,15 @@ def lib() -> C.CDLL:
         L.mx_gemm_by_tile.argtypes = [mx, mx, vp, vp, i32, i64, i32, vp]
         L.mx_gemm_tile.argtypes = [i64, i64, i64, i32, i32, i32, vp]
         for name in ("mx_gemm_by_tile", "mx_gemm_tile", "mx_quantize", "mx_dequantize", "mx_gemm", "mx_linear_fwd", "mx_linear_bwd_dgrad", "mx_linear_bwd_wgrad", "mx_linear_bwd"):
+            getattr(L, name).restype = i32
+        hp = C.POINTER(hp_norm)
+        L.hp_norm_fwd.argtypes = [hp, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp]
+        L.hp_norm_bwd.argtypes = [hp, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]
+        L.hp_embed_fwd.argtypes = [vp, i32, i64, i64, i64, vp, i64, f32, vp, i64, vp]
+        L.hp_embed_bwd.argtypes = [vp, i32, i64, i64, i64, vp, i64, f32, i32, vp, i64, vp, sz, vp]
+        L.hp_head_fwd.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp, sz, vp]
+        L.hp_head_bwd.argtypes = [vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, i64, vp, i64, vp, i32, i64, i32, vp, sz, vp]
+        for name in ("hp_norm_fwd", "hp_norm_bwd", "hp_embed_fwd", "hp_embed_bwd", "hp_head_fwd", "hp_head_bwd"):
             getattr(L, name).restype = i32
         L.fp8_host_round_codes.argtypes = [vp, i64, vp]
         for name in ("fp8_quantize", "fp4_gemm_mixed", "fp4_linear_fwd_mixed", "fp8_host_round_codes"):
@@ -871,6 +886,242 @@ def mx_linear_bwd(dY: torch.Tensor, saved: MxTensor, W: MxTensor, grad_bits: int
     _check(lib().mx_linear_bwd(dY.data_ptr(), _dt(dY), M, K, N, ldy, W.ref, saved.ref, grad_bits, dA.data_ptr(), _ld(dA, "dA"), int(accumulate),
                                dW.data_ptr(), _ld(dW, "dW"), room, nbytes, stream), "mx_linear_bwd")
     return dA, dW
+
+
+def _hp_vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, device: torch.device, name: str):
+    """Address of a vector of so many elements, or None."""
+    if t is None:
+        return None
+    if t.shape != (n,) or t.dtype != dtype or t.device != device or not (n < 2 or t.stride(0) == 1):
+        raise ValueError("%s must be [%d] contiguous %s on %s" % (name, n, dtype, device))
+    return t.data_ptr()
+
+
+def _hp_matrix(t: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torch.device, name: str):
+    """(address, leading dimension) of an input matrix, or nothing."""
+    if t is None:
+        return None, 0
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be %s %s on %s" % (name, tuple(shape), dtype, device))
+    return t.data_ptr(), _ld(t, name)
+
+
+class HpNorm:
+    """The joint of two blocks: what hp_norm_fwd and hp_norm_bwd take besides the tokens.
+
+    w_before [D]: weights of the norm before the next block (None: there is none); w_after [D]: of the norm after the block; gate: [D], one
+    for all tokens, or [M, D], a row for each; scale: of the residual stream."""
+
+    __slots__ = ("w_before", "w_after", "gate", "scale", "eps")
+
+    def __init__(self, w_before: Optional[torch.Tensor] = None, w_after: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                 scale: float = 1.0, eps: float = 1e-5):
+        if not eps > 0:
+            raise ValueError("eps must be positive")
+        if gate is not None and gate.dim() not in (1, 2):
+            raise ValueError("a gate is [D] or [M, D]")
+        self.w_before, self.w_after, self.gate, self.scale, self.eps = w_before, w_after, gate, float(scale), float(eps)
+
+    def _arguments(self, x: torch.Tensor):
+        """The structure for tokens like x, checked."""
+        M, D = x.shape
+        gate, ld_gate = self.gate, 0
+        if gate is None:
+            at = None
+        elif gate.dim() == 1:
+            at = _hp_vector(gate, D, x.dtype, x.device, "gate")
+        else:
+            at, ld_gate = _hp_matrix(gate, x.shape, x.dtype, x.device, "gate")
+        return C.byref(hp_norm(_hp_vector(self.w_before, D, x.dtype, x.device, "w_before"), _hp_vector(self.w_after, D, x.dtype, x.device, "w_after"),
+                               at, ld_gate, self.scale, self.eps))
+
+
+class HpNormSaved:
+    """What the forward pass of a joint leaves for its backward pass: each token's inverse norms (fp32 [M])."""
+
+    __slots__ = ("r_before", "r_after")
+
+    def __init__(self, r_before: Optional[torch.Tensor], r_after: Optional[torch.Tensor] = None):
+        self.r_before, self.r_after = r_before, r_after
+
+
+def hp_norm_saved(norm: HpNorm, M: int, device="cuda") -> HpNormSaved:
+    """Room for them."""
+    return HpNormSaved(*(None if w is None else torch.empty(M, dtype=torch.float32, device=device) for w in (norm.w_before, norm.w_after)))
+
+
+def hp_norm_fwd(norm: HpNorm, x: torch.Tensor, block: Optional[torch.Tensor] = None, saved: Optional[HpNormSaved] = None,
+                h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None):
+    """(h, y): the residual stream scale x + gate norm(block), and it normed for the next block (None without w_before).  saved: filled for the
+    backward pass.  h or y may be x or block."""
+    px, ldx = x.data_ptr(), _ld(x, "x")
+    dt, stream = _dt(x), _stream_of(x)
+    M, D = x.shape
+    pb, ldb = _hp_matrix(block, x.shape, x.dtype, x.device, "block")
+    if block is None and (norm.w_after is not None or norm.gate is not None):
+        raise ValueError("a norm after a block or a gate needs the block")
+    if y is not None and norm.w_before is None:
+        raise ValueError("y needs w_before")
+    ref = norm._arguments(x)
+    h = _out(h, x.shape, x.dtype, x.device, "h")
+    if norm.w_before is not None:
+        y = _out(y, x.shape, x.dtype, x.device, "y")
+    rb = ra = None
+    if saved is not None:
+        rb = _hp_vector(saved.r_before, M, torch.float32, x.device, "r_before") if norm.w_before is not None else None
+        ra = _hp_vector(saved.r_after, M, torch.float32, x.device, "r_after") if norm.w_after is not None else None
+    _check(lib().hp_norm_fwd(ref, dt, M, D, px, ldx, pb, ldb, h.data_ptr(), _ld(h, "h"), None if y is None else y.data_ptr(),
+                             0 if y is None else _ld(y, "y"), rb, ra, stream), "hp_norm_fwd")
+    return h, y
+
+
+class HpNormGrads(NamedTuple):
+    """dx, dblock [M, D]; dgate: fp32 [D], or [M, D] of the tokens' type; dw_before, dw_after: fp32 [D]; None where the joint has none."""
+    dx: torch.Tensor
+    dblock: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dw_before: Optional[torch.Tensor]
+    dw_after: Optional[torch.Tensor]
+
+
+def hp_norm_bwd(norm: HpNorm, saved: HpNormSaved, h: torch.Tensor, dy: Optional[torch.Tensor] = None, dh: Optional[torch.Tensor] = None,
+                block: Optional[torch.Tensor] = None, into: Optional[HpNormGrads] = None, accumulate: bool = False,
+                ws: Optional[Workspace] = None) -> HpNormGrads:
+    """Gradients of a joint from those of y and of h (either may be None).  into: tensors to write them to; accumulate adds to its sums over
+    tokens (dw_before, dw_after, dgate [D])."""
+    if dy is None and dh is None:
+        raise ValueError("a gradient of y or of h is needed")
+    if dy is not None and norm.w_before is None:
+        raise ValueError("a gradient of y needs w_before")
+    if block is None and (norm.w_after is not None or norm.gate is not None):
+        raise ValueError("a norm after a block or a gate needs the block")
+    if accumulate and into is None:
+        raise ValueError("accumulate needs the gradients to add to")
+    ph, ldh = h.data_ptr(), _ld(h, "h")
+    dt, stream = _dt(h), _stream_of(h)
+    M, D = h.shape
+    like = (h.shape, h.dtype, h.device)
+    pdy, ld_dy = _hp_matrix(dy, *like, "dy")
+    pdh, ld_dh = _hp_matrix(dh, *like, "dh")
+    pb, ldb = _hp_matrix(block, *like, "block")
+    ref = norm._arguments(h)
+    rb = _hp_vector(saved.r_before, M, torch.float32, h.device, "r_before") if dy is not None else None
+    ra = _hp_vector(saved.r_after, M, torch.float32, h.device, "r_after") if norm.w_after is not None else None
+    if (dy is not None and rb is None) or (norm.w_after is not None and ra is None):
+        raise ValueError("the saved inverse norms are missing")
+    given = into if into is not None else HpNormGrads(None, None, None, None, None)
+
+    def sums(t, name):
+        if t is None:
+            if accumulate:
+                raise ValueError("accumulate needs the %s to add to" % name)
+            t = torch.empty(D, dtype=torch.float32, device=h.device)
+        _hp_vector(t, D, torch.float32, h.device, name)
+        return t
+
+    dx = _out(given.dx, *like, "dx")
+    dblock = None if block is None else _out(given.dblock, *like, "dblock")
+    dgate, ld_dgate = None, 0
+    if norm.gate is not None:
+        if norm.gate.dim() == 1:
+            dgate = sums(given.dgate, "dgate")
+        else:
+            dgate = _out(given.dgate, *like, "dgate")
+            ld_dgate = _ld(dgate, "dgate")
+    dw_before = sums(given.dw_before, "dw_before") if dy is not None else None
+    dw_after = sums(given.dw_after, "dw_after") if norm.w_after is not None else None
+    need = _mx_room(FP4_OP_HP_NORM_BWD, M, D, 0)
+    room = _default_workspace(h.device.index, stream)._sized(need) if ws is None else ws.get(need)
+    at = lambda t: None if t is None else t.data_ptr()
+    _check(lib().hp_norm_bwd(ref, dt, M, D, pdy, ld_dy, pdh, ld_dh, ph, ldh, pb, ldb, rb, ra, dx.data_ptr(), _ld(dx, "dx"), at(dblock),
+                             0 if dblock is None else _ld(dblock, "dblock"), at(dgate), ld_dgate, at(dw_before), at(dw_after), int(accumulate),
+                             room.data_ptr(), room.numel(), stream), "hp_norm_bwd")
+    return HpNormGrads(dx, dblock, dgate, dw_before, dw_after)
+
+
+def _hp_ids(ids: torch.Tensor, device: torch.device, name: str) -> int:
+    if ids.dim() != 1 or ids.dtype != torch.int64 or ids.device != device or not (ids.numel() < 2 or ids.stride(0) == 1):
+        raise ValueError("%s must be [M] contiguous int64 on %s" % (name, device))
+    return ids.data_ptr()
+
+
+def hp_embed_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale table[ids], table [V, D]; zeros for ids outside [0, V)."""
+    ldt, dt, stream = _ld(table, "table"), _dt(table), _stream_of(table)
+    at = _hp_ids(ids, table.device, "ids")
+    M, (V, D) = ids.shape[0], table.shape
+    y = _out(y, (M, D), table.dtype, table.device, "y")
+    _check(lib().hp_embed_fwd(at, dt, M, D, V, table.data_ptr(), ldt, scale, y.data_ptr(), _ld(y, "y"), stream), "hp_embed_fwd")
+    return y
+
+
+def hp_embed_bwd(dy: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0, dtable: Optional[torch.Tensor] = None, accumulate: bool = False,
+                 ws: Optional[Workspace] = None) -> torch.Tensor:
+    """The table's gradient [V, D] in fp32: scale times the sums of dy's rows by id.  accumulate adds them to dtable and leaves the other rows alone."""
+    ld, dt, stream = _ld(dy, "dy"), _dt(dy), _stream_of(dy)
+    at = _hp_ids(ids, dy.device, "ids")
+    M, D = dy.shape
+    if ids.shape[0] != M:
+        raise ValueError("dy [M,D] and ids [M] must agree in M")
+    if accumulate and dtable is None:
+        raise ValueError("accumulate needs the dtable to add to")
+    dtable = _out(dtable, (V, D), torch.float32, dy.device, "dtable")
+    need = _mx_room(FP4_OP_HP_EMBED_BWD, M, D, V)
+    room = _default_workspace(dy.device.index, stream)._sized(need) if ws is None else ws.get(need)
+    _check(lib().hp_embed_bwd(at, dt, M, D, V, dy.data_ptr(), ld, scale, int(accumulate), dtable.data_ptr(), _ld(dtable, "dtable"), room.data_ptr(),
+                              room.numel(), stream), "hp_embed_bwd")
+    return dtable
+
+
+def _head_arguments(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor):
+    ldx, ldw, stream = _ld(x, "x"), _ld(w, "w"), _stream_of(x)
+    if x.dtype != torch.bfloat16 or w.dtype != torch.bfloat16:
+        raise TypeError("the head takes bfloat16, got %s and %s" % (x.dtype, w.dtype))
+    if w.device != x.device:
+        raise ValueError("all tensors must live on one device")
+    M, D = x.shape
+    if w.shape[1] != D or targets.shape != (M,):
+        raise ValueError("x [M,D], w [V,D] and targets [M] must agree")
+    return ldx, ldw, stream, _hp_ids(targets, x.device, "targets")
+
+
+def hp_head_fwd(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                ws: Optional[Workspace] = None):
+    """(loss, lse), fp32 [M]: softmax cross entropy of logits x w^T, which are not kept, and the logarithm of their sum of exponentials.  Targets
+    outside [0, V) have a loss of 0."""
+    ldx, ldw, stream, at = _head_arguments(x, w, targets)
+    M, D = x.shape
+    V = w.shape[0]
+    loss = torch.empty(M, dtype=torch.float32, device=x.device) if loss is None else loss
+    lse = torch.empty(M, dtype=torch.float32, device=x.device) if lse is None else lse
+    to = (_hp_vector(loss, M, torch.float32, x.device, "loss"), _hp_vector(lse, M, torch.float32, x.device, "lse"))
+    need = _mx_room(FP4_OP_HP_HEAD_FWD, M, D, V)
+    room = _default_workspace(x.device.index, stream)._sized(need) if ws is None else ws.get(need)
+    _check(lib().hp_head_fwd(x.data_ptr(), w.data_ptr(), at, FP4_BF16, M, D, V, ldx, ldw, *to, room.data_ptr(), room.numel(), stream), "hp_head_fwd")
+    return loss, lse
+
+
+def hp_head_bwd(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                dw: Optional[torch.Tensor] = None, dw_dtype: torch.dtype = torch.float32, accumulate: bool = False, want_dx: bool = True,
+                want_dw: bool = True, ws: Optional[Workspace] = None):
+    """(dx, dw) from each loss's gradient dloss [M]; dw [V, D] in fp32 or bfloat16.  accumulate adds to an fp32 dw (that of a tied embedding, or
+    several micro-batches).  A head or an input that is not trained: want_dw or want_dx False, and None comes back."""
+    ldx, ldw, stream, at = _head_arguments(x, w, targets)
+    M, D = x.shape
+    V = w.shape[0]
+    if not want_dx and not want_dw:
+        raise ValueError("one of the gradients has to be wanted")
+    if accumulate and want_dw and (dw is None or dw.dtype != torch.float32):
+        raise ValueError("accumulate needs the fp32 dw to add to")
+    dx = _out(dx, x.shape, torch.bfloat16, x.device, "dx") if want_dx else None
+    dw = _out(dw, w.shape, dw.dtype if dw is not None else dw_dtype, x.device, "dw") if want_dw else None
+    given = (_hp_vector(lse, M, torch.float32, x.device, "lse"), _hp_vector(dloss, M, torch.float32, x.device, "dloss"))
+    need = _mx_room(FP4_OP_HP_HEAD_BWD, M, D, V)
+    room = _default_workspace(x.device.index, stream)._sized(need) if ws is None else ws.get(need)
+    _check(lib().hp_head_bwd(x.data_ptr(), w.data_ptr(), at, *given, FP4_BF16, M, D, V, ldx, ldw, None if dx is None else dx.data_ptr(),
+                             0 if dx is None else _ld(dx, "dx"), None if dw is None else dw.data_ptr(), FP4_BF16 if dw is None else _dt(dw),
+                             0 if dw is None else _ld(dw, "dw"), int(accumulate and want_dw), room.data_ptr(), room.numel(), stream), "hp_head_bwd")
+    return dx, dw
 
 
 def fp4_unpack(codes: torch.Tensor) -> torch.Tensor:

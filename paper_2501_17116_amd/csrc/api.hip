@@ -86,6 +86,7 @@ int fp4_launch_spmm(const int64_t* row_ptr, const int32_t* col_idx, const float*
                     int64_t P, int64_t Q, const void* D, int bf16, int64_t N, float* R, int32_t* scratch,
                     hipStream_t s, bool general = false);
 size_t mx_workspace_bytes(int op, int64_t M, int64_t K, int64_t N);
+size_t hp_workspace_bytes(int op, int64_t M, int64_t D, int64_t V);
 
 namespace {
 
@@ -274,6 +275,10 @@ extern "C" size_t fp4_workspace_bytes(int op, int64_t M, int64_t K, int64_t N, f
     case FP4_OP_MX_DGRAD:
     case FP4_OP_MX_WGRAD:
     case FP4_OP_MX_BWD: return mx_workspace_bytes(op, M, K, N);
+    case FP4_OP_HP_NORM_BWD:
+    case FP4_OP_HP_EMBED_BWD:
+    case FP4_OP_HP_HEAD_FWD:
+    case FP4_OP_HP_HEAD_BWD: return hp_workspace_bytes(op, M, K, N);
     default: return 0;
   }
   return c.off + 256;

@@ -1,0 +1,188 @@
+"""The head's loss and gradients against the formulas in 64 bits, within the roundings that its form takes, and against differences."""
+import pytest
+import torch
+
+from paper_2501_17116_amd import binding as b
+from tests import hp_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(M, D, V, seed=0, ignored=0.1, pad=1, lean=6.0, spread=0.02):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randn(V, D, generator=g) * spread
+    targets = torch.randint(0, V, (M,), generator=g)
+    x = torch.randn(M, D, generator=g) + torch.rand(M, 1, generator=g) * lean * w[targets] / (spread * spread * D)
+    out = torch.rand(M, generator=g) < ignored
+    targets[out] = torch.where(torch.rand(int(out.sum()), generator=g) < 0.5, -100, V)
+    dloss = (torch.rand(M, generator=g) + 0.5) / max(1, M)
+    return plain.matrix(x, pad=pad), plain.matrix(w, pad=2 * pad), targets.cuda(), dloss.cuda()
+
+
+def check(x, w, targets, dloss, dw_dtype=torch.float32):
+    want = plain.head(x, w, targets, dloss)
+    loss, lse = b.hp_head_fwd(x, w, targets)
+    plain.close(lse, *want["lse"], "lse")
+    plain.close(loss, *want["loss"], "loss")
+    dx, dw = b.hp_head_bwd(x, w, targets, lse, dloss, dw_dtype=dw_dtype)
+    for name, got in (("dx", dx), ("dw", dw)):
+        value, tol = want[name]
+        plain.close(got, value, tol + plain.half_step(got.dtype) * (value.abs() + tol), name)
+    return loss, lse, dx, dw
+
+
+@pytest.mark.parametrize("M,D,V", [(1, 8, 1), (1, 8, 2), (1, 64, 1000), (2, 72, 77), (24, 256, 3001), (32, 200, 129), (33, 512, 640), (64, 136, 1025), (65, 128, 500),
+                                   (100, 1376, 999), (129, 64, 128), (300, 192, 1500), (511, 648, 2049), (1055, 328, 4099)])
+def test_small(M, D, V):
+    check(*inputs(M, D, V))
+
+
+@pytest.mark.parametrize("M,D,V", [(700, 512, 12000), (1300, 320, 9000)])
+def test_large_tiles(M, D, V):
+    check(*inputs(M, D, V), dw_dtype=torch.bfloat16)
+
+
+def test_several_pieces_of_the_vocabulary():
+    check(*inputs(40, 16384, 9001, pad=0))
+
+
+def test_several_pieces_of_short_rows():
+    M, D, V = 260, 16, 460_000
+    check(*inputs(M, D, V, pad=0, lean=0.5), dw_dtype=torch.bfloat16)
+
+
+def test_sharp_and_flat_rows():
+    x, w, targets, dloss = inputs(200, 256, 700, spread=0.5, lean=40.0)
+    x[:50] *= 4.0
+    x[50:60] = 0.0
+    loss, lse, dx, dw = check(x, w, targets, dloss)
+    assert float((lse[50:60] - torch.log(torch.tensor(700.0))).abs().max()) <= 1e-5
+
+
+def test_far_logits():
+    """Sums of exponentials that only their maximum keeps in range."""
+    M, D, V = 64, 64, 300
+    x, w, targets, dloss = inputs(M, D, V, spread=1.0, lean=0.0, ignored=0.0)
+    x *= 100.0
+    loss, lse, _, _ = check(x, w, targets, dloss)
+    assert float(lse.max()) > 1000.0 and bool(torch.isfinite(loss).all())
+    w *= -1.0
+    w -= 100.0
+    x.abs_()
+    loss, lse, _, _ = check(x, w, targets, dloss)
+    assert float(lse.max()) < -1000.0 and bool(torch.isfinite(loss).all())
+
+
+def test_no_targets_at_all():
+    M, D, V = 70, 128, 300
+    x, w, targets, dloss = inputs(M, D, V)
+    targets.fill_(-1)
+    dloss[3] = float("nan")
+    loss, lse = b.hp_head_fwd(x, w, targets)
+    dx, dw = b.hp_head_bwd(x, w, targets, lse, dloss)
+    assert bool((loss == 0).all()) and bool((dx == 0).all()) and bool((dw == 0).all())
+    plain.close(lse, *plain.head(x, w, targets)["lse"])
+
+
+def test_tokens_without_a_target_count_nowhere():
+    M, D, V = 90, 128, 300
+    x, w, targets, dloss = inputs(M, D, V, ignored=0.0)
+    targets[::3] = -100
+    dloss[::3] = 1e30
+    keep = torch.ones(M, dtype=torch.bool, device="cuda")
+    keep[::3] = False
+    loss, lse, dx, dw = check(x, w, targets, torch.where(keep, dloss, torch.zeros_like(dloss)))
+    dx2, dw2 = b.hp_head_bwd(x, w, targets, lse, dloss)
+    assert torch.equal(dx2, dx) and torch.equal(dw2, dw) and bool((dx[::3] == 0).all())
+
+
+def test_gradients_of_every_size():
+    """Tiny and huge weights of losses, and of the head's: powers of two change nothing but the exponents."""
+    M, D, V = 50, 96, 333
+    x, w, targets, dloss = inputs(M, D, V)
+    loss, lse = b.hp_head_fwd(x, w, targets)
+    dx, dw = b.hp_head_bwd(x, w, targets, lse, dloss)
+    for e in (-60, 40):
+        f = 2.0 ** e
+        dx2, dw2 = b.hp_head_bwd(x, w, targets, lse, dloss * f)
+        assert torch.equal(dw2, dw * f) and torch.equal(dx2, (dx.float() * f).bfloat16())
+
+
+def test_against_differences():
+    M, D, V = 5, 24, 37
+    x, w, targets, dloss = inputs(M, D, V, ignored=0.0, spread=0.3)
+    loss, lse = b.hp_head_fwd(x, w, targets)
+    dx, dw = b.hp_head_bwd(x, w, targets, lse, dloss)
+    g = torch.Generator().manual_seed(5)
+    sx, sw = torch.randn(M, D, generator=g, dtype=torch.float64).cuda(), torch.randn(V, D, generator=g, dtype=torch.float64).cuda()
+
+    def value(e):
+        z = (x.double() + e * sx) @ (w.double() + e * sw).t()
+        return float((dloss.double() * (torch.logsumexp(z, 1) - z.gather(1, targets[:, None])[:, 0])).sum())
+
+    e = 1e-5
+    want = (value(e) - value(-e)) / (2 * e)
+    got = float((dx.double() * sx).sum() + (dw.double() * sw).sum())
+    # dx is rounded to 2^-8 of itself, operands to 2^-11; the differences' own error is far below
+    allowed = float((dx.double() * sx).abs().sum() * 2.0 ** -8 + ((dx.double() * sx).abs().sum() + (dw.double() * sw).abs().sum()) * 2.0 ** -9)
+    assert abs(got - want) <= allowed, (got, want, allowed)
+
+
+def test_accumulates_frozen_sides_padding_and_repeats():
+    M, D, V = 150, 264, 700
+    x, w, targets, dloss = inputs(M, D, V)
+    loss, lse = b.hp_head_fwd(x, w, targets)
+    dx, dw = b.hp_head_bwd(x, w, targets, lse, dloss)
+    dx2, none = b.hp_head_bwd(x, w, targets, lse, dloss, want_dw=False)
+    none2, dw2 = b.hp_head_bwd(x, w, targets, lse, dloss, want_dx=False)
+    assert none is None and none2 is None and torch.equal(dx, dx2) and torch.equal(dw, dw2)
+    wide = torch.full((V, D + 16), 1.5, device="cuda")
+    b.hp_head_bwd(x, w, targets, lse, dloss, dw=wide[:, :D], accumulate=True)
+    plain.close(wide[:, :D], dw.double() + 1.5, plain.U * 4 * (dw.double().abs() + 1.5))
+    assert bool((wide[:, D:] == 1.5).all())
+    narrow = torch.full((M, D + 8), 3.0, dtype=torch.bfloat16, device="cuda")
+    b.hp_head_bwd(x, w, targets, lse, dloss, dx=narrow[:, :D], want_dw=False)
+    assert torch.equal(narrow[:, :D], dx) and bool((narrow[:, D:] == 3).all())
+    assert torch.equal(b.hp_head_bwd(x, w, targets, lse, dloss, dw_dtype=torch.bfloat16)[1], dw.bfloat16())
+
+
+def test_no_tokens():
+    x, w = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(5, 64, dtype=torch.bfloat16, device="cuda")
+    t, e = torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda")
+    loss, lse = b.hp_head_fwd(x, w, t)
+    assert loss.shape == lse.shape == (0,)
+    dx, dw = b.hp_head_bwd(x, w, t, lse, e)
+    assert dx.shape == (0, 64) and bool((dw == 0).all())
+    dw.fill_(2.0)
+    b.hp_head_bwd(x, w, t, lse, e, dw=dw, accumulate=True)
+    assert bool((dw == 2).all())
+
+
+def test_graphs_with_workspaces_of_their_own():
+    M, D, V = 300, 256, 2000
+    x, w, targets, dloss = inputs(M, D, V, pad=0)
+    ref_loss, ref_lse = b.hp_head_fwd(x, w, targets)
+    ref_dx, ref_dw = b.hp_head_bwd(x, w, targets, ref_lse, dloss)
+    runs = []
+    for _ in range(2):
+        ws = b.Workspace()
+        ws.get(max(b.workspace_bytes(op, M, D, V, b.FP4_BF16) for op in (b.FP4_OP_HP_HEAD_FWD, b.FP4_OP_HP_HEAD_BWD)))
+        out = [torch.empty_like(t) for t in (ref_loss, ref_lse, ref_dx, ref_dw)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            b.hp_head_fwd(x, w, targets, loss=out[0], lse=out[1], ws=ws)
+            b.hp_head_bwd(x, w, targets, out[1], dloss, dx=out[2], dw=out[3], ws=ws)
+        runs.append((graph, out, ws))
+    streams = [torch.cuda.Stream() for _ in runs]
+    for _ in range(3):
+        for _, out, _ in runs:
+            for t in out:
+                t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for s, (graph, _, _) in zip(streams, runs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for _, out, _ in runs:
+            assert all(torch.equal(a, c) for a, c in zip(out, (ref_loss, ref_lse, ref_dx, ref_dw)))
+        assert torch.equal(b.hp_head_bwd(x, w, targets, ref_lse, dloss)[1], ref_dw)

@@ -1,0 +1,244 @@
+"""The high-precision entry points refuse on the host what they cannot take, before anything is enqueued, and answer how much room they need.  No GPU:
+pointers that are not looked at, and stand-ins for tensors."""
+import ctypes as C
+import itertools
+import re
+
+import pytest
+import torch
+
+from paper_2501_17116_amd import binding as b
+from tests.test_other_device import On, Room
+
+NULL, SHAPE, DTYPE, ARG, WORKSPACE, LIMIT = -1, -2, -3, -4, -5, -8
+P = C.c_void_p(16)        # aligned, never looked at: every call below ends before
+ODD = C.c_void_p(24)
+BIG = 1 << 50
+FAR = (1 << 21) + 8
+
+
+def norm(w_before=16, w_after=None, gate=None, ld_gate=0, scale=1.0, eps=1e-5):
+    return C.byref(b.hp_norm(w_before, w_after, gate, ld_gate, scale, eps))
+
+
+def norm_fwd(n=None, dt=1, M=4, D=64, x=P, ldx=64, block=P, ldb=64, h=P, ldh=64, y=P, ldy=64, rb=None, ra=None):
+    return b.lib().hp_norm_fwd(norm() if n is None else n, dt, M, D, x, ldx, block, ldb, h, ldh, y, ldy, rb, ra, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=2), DTYPE), (dict(M=-1), SHAPE), (dict(D=-8), SHAPE), (dict(ldx=56), SHAPE), (dict(ldy=32), SHAPE), (dict(D=60, ldx=60), ARG), (dict(x=None), NULL),
+    (dict(x=ODD), ARG), (dict(h=ODD), ARG), (dict(block=ODD), ARG), (dict(h=None, y=None), NULL), (dict(M=FAR), LIMIT), (dict(D=16385, ldx=16392), LIMIT),
+    (dict(n=norm(None)), NULL), (dict(n=norm(None), y=None, rb=P), NULL), (dict(n=norm(24)), ARG), (dict(n=norm(eps=0.0)), ARG), (dict(n=norm(eps=float("nan"))), ARG),
+    (dict(n=norm(scale=float("inf"))), ARG), (dict(n=norm(w_after=16), block=None), ARG), (dict(n=norm(gate=16), block=None), ARG),
+    (dict(n=norm(gate=16, ld_gate=32)), SHAPE), (dict(n=norm(gate=16, ld_gate=68)), ARG),
+])
+def test_norm_forward_refuses(kw, status):
+    assert norm_fwd(**kw) == status
+
+
+def test_norm_does_nothing_with_nothing():
+    assert norm_fwd(M=0, x=None, block=None, h=None, y=None) == 0
+    assert norm_fwd(D=0, x=None, block=None, h=None, y=None) == 0
+    assert b.lib().hp_norm_fwd(None, 1, 1, 8, P, 8, None, 0, P, 8, None, 0, None, None, None) == NULL
+
+
+def norm_bwd(n=None, dt=1, M=4, D=64, dy=P, ld=64, dh=P, h=P, block=P, rb=P, ra=P, dx=P, dblock=P, dgate=None, ld_dgate=0, dwb=P, dwa=None, room=BIG, ws=P):
+    return b.lib().hp_norm_bwd(norm() if n is None else n, dt, M, D, dy, ld, dh, ld, h, ld, block, ld, rb, ra, dx, ld, dblock, ld, dgate, ld_dgate, dwb, dwa, 0, ws,
+                               room, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=7), DTYPE), (dict(dy=None, dh=None), NULL), (dict(h=None), NULL), (dict(rb=None), NULL), (dict(n=norm(None)), NULL), (dict(dy=None), NULL),
+    (dict(block=None), NULL), (dict(dgate=P), NULL), (dict(dwa=P), NULL), (dict(n=norm(w_after=16), ra=None), NULL), (dict(ld=40), SHAPE), (dict(dx=ODD), ARG),
+    (dict(dwb=ODD), ARG), (dict(n=norm(gate=16), dgate=ODD), ARG), (dict(n=norm(gate=16, ld_gate=64), dgate=P, ld_dgate=32), SHAPE), (dict(room=100), WORKSPACE),
+    (dict(ws=None), WORKSPACE), (dict(M=FAR), LIMIT),
+])
+def test_norm_backward_refuses(kw, status):
+    assert norm_bwd(**kw) == status
+
+
+def embed_fwd(ids=P, dt=1, M=4, D=64, V=10, table=P, ldt=64, scale=1.0, y=P, ldy=64):
+    return b.lib().hp_embed_fwd(ids, dt, M, D, V, table, ldt, scale, y, ldy, None)
+
+
+def embed_bwd(ids=P, dt=1, M=4, D=64, V=10, dy=P, ld=64, scale=1.0, dtable=P, ldt=64, ws=P, room=BIG):
+    return b.lib().hp_embed_bwd(ids, dt, M, D, V, dy, ld, scale, 0, dtable, ldt, ws, room, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(ids=None), NULL), (dict(dt=5), DTYPE), (dict(M=-1), SHAPE), (dict(V=-1), SHAPE), (dict(table=None), NULL), (dict(y=None), NULL), (dict(ldy=63), SHAPE),
+    (dict(ldt=68), ARG), (dict(y=ODD), ARG), (dict(scale=float("nan")), ARG), (dict(V=FAR), LIMIT), (dict(D=FAR, ldt=FAR, ldy=FAR), LIMIT),
+])
+def test_lookup_refuses(kw, status):
+    assert embed_fwd(**kw) == status
+    kw = {{"table": "dtable", "y": "dy", "ldy": "ld"}.get(k, k): v for k, v in kw.items()}
+    assert embed_bwd(**kw) == status
+
+
+def test_lookup_of_nothing():
+    assert embed_fwd(M=0, ids=None, y=None) == 0 and embed_fwd(D=0, table=None, y=None) == 0
+    assert embed_bwd(V=0, dtable=None) == 0 and embed_bwd(ws=None) == WORKSPACE and embed_bwd(room=10) == WORKSPACE
+
+
+def head_fwd(x=P, w=P, t=P, dt=1, M=4, D=64, V=10, ldx=64, ldw=64, loss=P, lse=P, ws=P, room=BIG):
+    return b.lib().hp_head_fwd(x, w, t, dt, M, D, V, ldx, ldw, loss, lse, ws, room, None)
+
+
+def head_bwd(x=P, w=P, t=P, dt=1, M=4, D=64, V=10, ldx=64, ldw=64, lse=P, dloss=P, dx=P, ld_dx=64, dw=P, dw_dt=0, ld_dw=64, acc=0, ws=P, room=BIG):
+    return b.lib().hp_head_bwd(x, w, t, lse, dloss, dt, M, D, V, ldx, ldw, dx, ld_dx, dw, dw_dt, ld_dw, acc, ws, room, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=0), DTYPE), (dict(M=-2), SHAPE), (dict(V=0), SHAPE), (dict(D=60), SHAPE), (dict(ldx=56), SHAPE), (dict(ldw=68), ARG), (dict(x=None), NULL),
+    (dict(w=None), NULL), (dict(t=None), NULL), (dict(x=ODD), ARG), (dict(w=ODD), ARG), (dict(V=FAR), LIMIT), (dict(ldw=FAR), LIMIT), (dict(ws=None), WORKSPACE),
+    (dict(room=64), WORKSPACE),
+])
+def test_head_refuses(kw, status):
+    assert head_fwd(**kw) == status
+    assert head_bwd(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dx=None, dw=None), NULL), (dict(lse=None), NULL), (dict(dloss=None), NULL), (dict(dw_dt=3), DTYPE), (dict(dw_dt=1, acc=1), ARG), (dict(dx=ODD), ARG),
+    (dict(ld_dx=32), SHAPE), (dict(ld_dw=60), SHAPE), (dict(dw=ODD), ARG),
+])
+def test_head_backward_refuses(kw, status):
+    assert head_bwd(**kw) == status
+
+
+def test_head_of_no_tokens():
+    assert head_fwd(M=0, x=None, t=None, loss=None, lse=None, ws=None) == 0
+    assert head_fwd(loss=None, lse=None) == NULL
+
+
+@pytest.mark.parametrize("op", range(13, 17))
+def test_room_grows_with_the_problem(op):
+    sizes = [0, 1, 8, 63, 64, 65, 256, 1000, 1024, 4096, 5000, 16384, 100_000, 1 << 21]
+    for a, k in itertools.product(sizes, sizes[:12]):
+        rooms = [b.workspace_bytes(op, a, k, v, 1) for v in sizes]
+        assert rooms == sorted(rooms), (op, a, k)
+        rooms = [b.workspace_bytes(op, v, k, a, 1) for v in sizes]
+        assert rooms == sorted(rooms), (op, a, k)
+        rooms = [b.workspace_bytes(op, a, v, k, 1) for v in sizes[:12]]
+        assert rooms == sorted(rooms), (op, a, k)
+    assert b.workspace_bytes(op, 64, 64, 64, 1) > 0
+
+
+# ---- the binding ---------------------------------------------------------------------------------------------------------------
+
+class Line(On):
+    """A vector."""
+
+    def __init__(self, index, n, dtype=torch.float32):
+        super().__init__(index, n, 1, dtype)
+        self.shape = (n,)
+
+    def dim(self):
+        return 1
+
+    def numel(self):
+        return self.shape[0]
+
+    def stride(self, i=None):
+        return 1 if i is not None else (1,)
+
+
+M, D, V = 8, 64, 32
+BF16, F32, I64 = torch.bfloat16, torch.float32, torch.int64
+
+
+def joint(i, **kw):
+    return b.HpNorm(Line(i, D, BF16), Line(i, D, BF16), Line(i, D, BF16), **kw)
+
+
+def grads(i):
+    return b.HpNormGrads(On(i, M, D), On(i, M, D), *(Line(i, D) for _ in range(3)))
+
+
+def saved(i):
+    return b.HpNormSaved(Line(i, M), Line(i, M))
+
+
+CALLS = {
+    "hp_norm_fwd": lambda i, j: b.hp_norm_fwd(joint(j), On(i, M, D), On(j, M, D), saved(j), h=On(i, M, D), y=On(j, M, D)),
+    "hp_norm_bwd": lambda i, j: b.hp_norm_bwd(joint(j), saved(j), On(i, M, D), On(j, M, D), On(j, M, D), On(j, M, D), into=grads(j), ws=Room0()),
+    "hp_embed_fwd": lambda i, j: b.hp_embed_fwd(Line(j, M, I64), On(i, V, D), y=On(j, M, D)),
+    "hp_embed_bwd": lambda i, j: b.hp_embed_bwd(On(i, M, D), Line(j, M, I64), V, dtable=On(j, V, D, F32), ws=Room0()),
+    "hp_head_fwd": lambda i, j: b.hp_head_fwd(On(i, M, D), On(j, V, D), Line(j, M, I64), Line(j, M), Line(j, M), ws=Room0()),
+    "hp_head_bwd": lambda i, j: b.hp_head_bwd(On(i, M, D), On(j, V, D), Line(j, M, I64), Line(j, M), Line(j, M), dx=On(j, M, D), dw=On(j, V, D, F32), ws=Room0()),
+}
+
+
+class Room0(Room):
+    def get(self, nbytes):
+        return On(0, 1, nbytes)
+
+
+@pytest.fixture
+def reached(monkeypatch):
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: calls.append(name) or 0
+
+    monkeypatch.setattr(b, "lib", Library)
+    monkeypatch.setattr(b, "_mx_room", lambda *shape: 4096)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0)
+    return calls
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_devices(reached, name):
+    CALLS[name](0, 0)
+    assert reached == [name]
+    reached.clear()
+    with pytest.raises(ValueError, match="current device"):
+        CALLS[name](1, 1)
+    with pytest.raises(ValueError, match=re.compile("on cuda:0|one device")):
+        CALLS[name](0, 1)
+    assert not reached
+
+
+BAD = {
+    "eps": lambda: b.HpNorm(Line(0, D, BF16), eps=0.0),
+    "a gate of three dimensions": lambda: b.HpNorm(gate=torch.ones(1, 1, 1)),
+    "a gate without a block": lambda: b.hp_norm_fwd(joint(0), On(0, M, D)),
+    "y without weights": lambda: b.hp_norm_fwd(b.HpNorm(), On(0, M, D), On(0, M, D), h=On(0, M, D), y=On(0, M, D)),
+    "weights of another width": lambda: b.hp_norm_fwd(b.HpNorm(Line(0, D + 8, BF16)), On(0, M, D), h=On(0, M, D), y=On(0, M, D)),
+    "weights of another type": lambda: b.hp_norm_fwd(b.HpNorm(Line(0, D, F32)), On(0, M, D), h=On(0, M, D), y=On(0, M, D)),
+    "a block of another shape": lambda: b.hp_norm_fwd(b.HpNorm(Line(0, D, BF16)), On(0, M, D), On(0, M + 1, D), h=On(0, M, D), y=On(0, M, D)),
+    "saved norms of other tokens": lambda: b.hp_norm_fwd(joint(0), On(0, M, D), On(0, M, D), b.HpNormSaved(Line(0, M + 1), Line(0, M)), h=On(0, M, D), y=On(0, M, D)),
+    "no gradient": lambda: b.hp_norm_bwd(joint(0), saved(0), On(0, M, D), block=On(0, M, D), into=grads(0)),
+    "a gradient of y without weights": lambda: b.hp_norm_bwd(b.HpNorm(), saved(0), On(0, M, D), dy=On(0, M, D), into=grads(0)),
+    "no saved norms": lambda: b.hp_norm_bwd(joint(0), b.HpNormSaved(None), On(0, M, D), dy=On(0, M, D), block=On(0, M, D), into=grads(0)),
+    "accumulation into nothing": lambda: b.hp_norm_bwd(joint(0), saved(0), On(0, M, D), dy=On(0, M, D), block=On(0, M, D), accumulate=True),
+    "accumulation into part": lambda: b.hp_norm_bwd(joint(0), saved(0), On(0, M, D), dy=On(0, M, D), block=On(0, M, D), into=grads(0)._replace(dw_after=None),
+                                                    accumulate=True),
+    "32-bit ids": lambda: b.hp_embed_fwd(Line(0, M, torch.int32), On(0, V, D), y=On(0, M, D)),
+    "ids of other tokens": lambda: b.hp_embed_bwd(On(0, M, D), Line(0, M + 1, I64), V, dtable=On(0, V, D, F32)),
+    "a narrow gradient of the table": lambda: b.hp_embed_bwd(On(0, M, D), Line(0, M, I64), V, dtable=On(0, V, D)),
+    "a table to add to": lambda: b.hp_embed_bwd(On(0, M, D), Line(0, M, I64), V, accumulate=True),
+    "targets of other tokens": lambda: b.hp_head_fwd(On(0, M, D), On(0, V, D), Line(0, M + 1, I64)),
+    "widths that disagree": lambda: b.hp_head_fwd(On(0, M, D), On(0, V, D + 8), Line(0, M, I64)),
+    "a wide loss": lambda: b.hp_head_fwd(On(0, M, D), On(0, V, D), Line(0, M, I64), loss=Line(0, M, torch.float64), lse=Line(0, M)),
+    "accumulation in bf16": lambda: b.hp_head_bwd(On(0, M, D), On(0, V, D), Line(0, M, I64), Line(0, M), Line(0, M), dx=On(0, M, D), dw=On(0, V, D), accumulate=True),
+    "no gradient of the head": lambda: b.hp_head_bwd(On(0, M, D), On(0, V, D), Line(0, M, I64), Line(0, M), Line(0, M), want_dx=False, want_dw=False),
+}
+
+
+@pytest.mark.parametrize("what", BAD)
+def test_bad_arguments(reached, what):
+    with pytest.raises(ValueError):
+        BAD[what]()
+    assert not reached
+
+
+def test_types_of_the_head(reached):
+    for x, w in ((F32, BF16), (BF16, F32), (torch.float16, torch.float16)):
+        with pytest.raises(TypeError):
+            b.hp_head_fwd(On(0, M, D, x), On(0, V, D, w), Line(0, M, I64))
+    with pytest.raises(TypeError):
+        b.hp_embed_fwd(Line(0, M, I64), On(0, V, D, torch.float16))
+    assert not reached
