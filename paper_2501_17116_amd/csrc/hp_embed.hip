@@ -3,7 +3,8 @@
 //   y[t] = s table[id_t]        dtable[v] (+)= s sum over t with id_t = v of dy[t], t ascending
 //
 // Gradient: (id, t) is sorted by id, stably, eight bits a pass: workgroup d of a pass takes the keys with digit d, which it counts, together with
-// those of smaller digits, and then copies to their place in order; no counters in memory, no atomics, one launch a pass.  The sorted rows are then cut into
+// those of smaller digits, and then copies to their place in order; no counters in memory, no atomics, one launch a pass (few tokens: all compared with
+// all, one launch).  The sorted rows are then cut into
 // spans of equal length, whoever they belong to, so that a frequent id costs no more than many rare ones: a workgroup adds up its span's runs of one id;
 // runs within a span are done, those over a border leave partial sums, which a second launch joins in order.  Bound: memory (dy once,
 // dtable once); below some thousand tokens the launches.
@@ -35,9 +36,9 @@ template <bool RAGGED>
 FP4_D f32x4 get4(const BF16*, const uint8_t* row, int64_t c, int64_t cols) {
   const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + c;
   f32x4 v;
-  if constexpr (RAGGED) {
+  if (RAGGED && c + 4 > cols) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? u2f((uint32_t)p[min((int64_t)e, cols - 1 - c)] << 16) : 0.0f;
+    for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? u2f((uint32_t)p[e] << 16) : 0.0f;
   } else {
     const u32x2 w = *reinterpret_cast<const u32x2*>(p);
     v = f32x4{u2f(w.x << 16), u2f(w.x & 0xffff0000u), u2f(w.y << 16), u2f(w.y & 0xffff0000u)};
@@ -47,20 +48,18 @@ FP4_D f32x4 get4(const BF16*, const uint8_t* row, int64_t c, int64_t cols) {
 template <bool RAGGED>
 FP4_D f32x4 get4(const F32*, const uint8_t* row, int64_t c, int64_t cols) {
   const float* p = reinterpret_cast<const float*>(row) + c;
-  if constexpr (!RAGGED) return *reinterpret_cast<const f32x4*>(p);
+  if (!RAGGED || c + 4 <= cols) return *reinterpret_cast<const f32x4*>(p);
   f32x4 v;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? p[min((int64_t)e, cols - 1 - c)] : 0.0f;
+  for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? p[e] : 0.0f;
   return v;
 }
 FP4_D void put4(float* row, int64_t c, int64_t cols, const f32x4& v) {
-  if (c + 4 <= cols) {
-    *reinterpret_cast<f32x4*>(row + c) = v;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e < cols) row[c + e] = v[e];
-  }
+  const int64_t left = cols - c;
+  if (left >= 4) *reinterpret_cast<f32x4*>(row + c) = v;
+  else if (left == 3) __builtin_memcpy(__builtin_assume_aligned(row + c, 16), &v, 12);
+  else if (left == 2) __builtin_memcpy(__builtin_assume_aligned(row + c, 16), &v, 8);
+  else if (left == 1) row[c] = v.x;
 }
 
 // A pass of the sort by workgroups 0 .. 255, of them digit's own each; those behind clear the table's gradient, or a part of it, meanwhile.
@@ -70,7 +69,7 @@ struct SortPass {
   const uint32_t *key_in, *pos_in;
   uint32_t *key_out, *pos_out;
   int64_t M, V;
-  int shift, sorters;        // sorters: 256, or 0
+  int shift, sorters;        // sorters: workgroups that sort
   float* table;
   int64_t D, ldt, zero_from, zero_rows;
 };
@@ -136,6 +135,41 @@ FP4_D void sort_pass(const SortPass& a) {
   }
 }
 
+// Few tokens: their places in the order at once, by comparing all with all, 64 tokens a workgroup whose four waves share the others; four
+// cycles a comparison and wave.
+FP4_D void sort_few(const SortPass& a) {
+  __shared__ uint32_t before[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int M = (int)a.M, t = (int)blockIdx.x * 64 + lane;
+  const auto key_at = [&](int i) {
+    const int64_t id = a.ids[min(i, M - 1)];
+    return (uint32_t)(id >= 0 && id < a.V ? id : a.V);
+  };
+  const uint32_t mine = key_at(t);
+  uint32_t count = 0;
+  for (int b = wave; b * 64 < M; b += 4) {
+    const uint32_t theirs = b * 64 + lane < M ? key_at(b * 64 + lane) : 0xffffffffu;   // behind all keys
+    if (b < (int)blockIdx.x) {
+#pragma unroll
+      for (int i = 0; i < 64; ++i) count += (uint32_t)__builtin_amdgcn_readlane(theirs, i) <= mine;
+    } else if (b > (int)blockIdx.x) {
+#pragma unroll
+      for (int i = 0; i < 64; ++i) count += (uint32_t)__builtin_amdgcn_readlane(theirs, i) < mine;
+    } else {
+      for (int i = 0; i < 64; ++i) {
+        const uint32_t k = __builtin_amdgcn_readlane(theirs, i);
+        count += k < mine || (k == mine && i < lane);
+      }
+    }
+  }
+  before[wave][lane] = count;
+  __syncthreads();
+  if (wave || t >= M) return;
+  const uint32_t at = before[0][lane] + before[1][lane] + before[2][lane] + before[3][lane];
+  a.key_out[at] = mine;
+  a.pos_out[at] = (uint32_t)t;
+}
+
 // One piece of four elements a thread, small workgroups: what is written together then lies together (32000 x 4096: 77 us; a workgroup of 256 a
 // row 89, one of 1024 for eight rows 93).
 FP4_D void zero_rows(const SortPass& a) {
@@ -144,6 +178,11 @@ FP4_D void zero_rows(const SortPass& a) {
     const int64_t row = n >> 32 ? i / pieces : (uint32_t)i / (uint32_t)pieces, c = (i - row * pieces) * 4;
     put4(a.table + (a.zero_from + row) * a.ldt, c, a.D, f32x4{0, 0, 0, 0});
   }
+}
+
+__global__ __launch_bounds__(256) void sort_few_kernel(SortPass a) {
+  if ((int)blockIdx.x < a.sorters) sort_few(a);
+  else zero_rows(a);
 }
 
 template <bool FIRST, int WAVES>
@@ -282,9 +321,10 @@ int hp_launch_embed_bwd(const int64_t* ids, int bf16, int64_t M, int64_t D, int6
   const size_t list = align_up((size_t)M * 4, 256);
   uint8_t* w = (uint8_t*)align_up((size_t)(uintptr_t)workspace, 256);
   uint32_t *key[2] = {(uint32_t*)w, (uint32_t*)(w + list)}, *pos[2] = {(uint32_t*)(w + 2 * list), (uint32_t*)(w + 3 * list)};
-  // Up to 32768 tokens the passes hide behind the clearing, in small workgroups as that wants them; beyond, and where nothing is cleared, sixteen waves
-  // share a digit.
-  const bool together = !accumulate && M > 0 && M <= 32768;
+  // Few tokens are ordered in one launch: 8192 in some 12 us, as two passes take (16384 in 24: clearing and sorting for 16384 x 4096 into 32000 rows 94 us, by
+  // two passes 89).  Up to 32768 the passes hide behind the clearing, in small workgroups as that wants them; beyond, and where nothing is
+  // cleared, sixteen waves share a digit.
+  const bool few = M > 0 && M <= 8192, together = !accumulate && M > 0 && M <= 32768;
   int from = 0, passes = 1;
   while (V >> (8 * passes)) ++passes;
   const auto clearing = [&](int64_t rows, int threads) { return (unsigned)std::min<int64_t>((rows * ((D + 3) / 4) + threads - 1) / threads, 1 << 22); };
@@ -294,7 +334,12 @@ int hp_launch_embed_bwd(const int64_t* ids, int bf16, int64_t M, int64_t D, int6
     sort_pass_kernel<true, 4><<<clearing(V, 256), 256, 0, s>>>(p);
     FP4_CHECK_LAUNCH();
   }
-  for (int i = 0; M > 0 && i < passes; ++i, from ^= 1) {
+  if (few) {
+    p = {ids, nullptr, nullptr, key[0], pos[0], M, V, 0, (int)((M + 63) / 64), table, D, ldt, 0, accumulate ? 0 : V};
+    sort_few_kernel<<<p.sorters + clearing(p.zero_rows, 256), 256, 0, s>>>(p);
+    FP4_CHECK_LAUNCH();
+  }
+  for (int i = 0; M > 0 && !few && i < passes; ++i, from ^= 1) {
     p = {ids, key[from], pos[from], key[from ^ 1], pos[from ^ 1], M, V, 8 * i, 256, table, D, ldt, 0, 0};
     if (together) {
       p.zero_from = V * i / passes;
