@@ -13,8 +13,7 @@
 #include "hp_gemm.h"
 
 #include <algorithm>
-
-int fp4_compute_units_of_current_device();
+#include <cstdint>
 
 namespace {
 
@@ -37,8 +36,8 @@ struct HeadTile {
   float2* part;              // STATS: [tiles_q][P] maximum and sum
   float* target_z;           // STATS: [P]
   const float* lse;          // DZ
-  uint16_t* dz;              // DZ: [P x ld], zeros from Q to ld
-  int64_t ld;
+  uint16_t *dz, *dz_across;  // DZ: [P x ld], zeros from Q to ld; [Q x ld_across], zeros from P to the next multiple of 8 at least.  Either may be NULL
+  int64_t ld, ld_across;
   float* sums;               // ADD: [splits][P x Q]
   bool add;                  // ADD, OUT: to what is there
   const uint32_t* amax;      // ADD, OUT: of the operand under a power of two
@@ -156,6 +155,18 @@ FP4_D void dz_epilogue(const HeadTile& a, const HpTile& tile, const hp_f32x16 (&
         }
         d[k] = pack_f16(e[0], e[1]);
       }
+      if (a.dz_across) {   // a lane and its neighbour have two rows' elements of two columns: each takes one column's, four bytes of a line
+        const int64_t col0 = q0 + i * 32 + h * 4 + (lane & 1), line = p0 + (l32 & ~1);
+        const uint32_t choose = lane & 1 ? 0x03020706u : 0x05040100u;   // bytes of {the neighbour's word, its own}
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)d[k], 0xB1, 0xf, 0xf, true);   // lane ^ 1
+          const uint32_t two = __builtin_amdgcn_perm(other, d[k], choose);
+          const int64_t col = col0 + k / 2 * 8 + k % 2 * 2;
+          if (col < a.g.Q && line < a.ld_across) *reinterpret_cast<uint32_t*>(a.dz_across + col * a.ld_across + line) = two;
+        }
+      }
+      if (!a.dz) continue;
       spread16(d);
       const int64_t col = q0 + i * 32 + unit * 8;
       if (col < a.ld) {
@@ -240,34 +251,49 @@ __global__ __launch_bounds__(S::WAVES * 64) void head_tile_kernel(HeadTile a) {
   }
 }
 
-// The tiles' maxima and sums of sixteen rows, each sixty-fourth of them by one thread, joined in order.
+// The tiles' maxima and sums of ROWS rows, each 1024 / ROWS-th of them by one thread, joined in order.
+template <int ROWS>
 __global__ __launch_bounds__(1024) void head_join_kernel(const float2* part, int tiles, int64_t M, int64_t V, const int64_t* targets, const float* target_z,
                                                          float* loss, float* lse) {
-  __shared__ float2 lds[64][16];
-  const int r = threadIdx.x & 15, k = threadIdx.x >> 4;
-  const int64_t p = (int64_t)blockIdx.x * 16 + r;
+  constexpr int SHARES = 1024 / ROWS, AT_ONCE = 4;
+  __shared__ float2 lds[SHARES][ROWS];
+  const int r = threadIdx.x % ROWS, k = threadIdx.x / ROWS;
+  const int64_t p = (int64_t)blockIdx.x * ROWS + r, row = min(p, M - 1);
   float m = -INFINITY, s = 0.0f;
   const auto join = [&](float2 o) {
-    const float top = fmaxf(m, o.x);
     if (o.y > 0.0f) {
+      const float top = fmaxf(m, o.x);
       s = s * (m == top ? 1.0f : __builtin_amdgcn_exp2f((m - top) * LOG2E)) + o.y * (o.x == top ? 1.0f : __builtin_amdgcn_exp2f((o.x - top) * LOG2E));
       m = top;
     }
   };
-  if (p < M)
-    for (int i = k; i < tiles; i += 64) join(part[(int64_t)i * M + p]);
+  for (int i0 = k; i0 < tiles; i0 += SHARES * AT_ONCE) {
+    float2 o[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) o[u] = part[(int64_t)min(i0 + u * SHARES, tiles - 1) * M + row];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u)
+      if (i0 + u * SHARES < tiles) join(o[u]);
+  }
   lds[k][r] = float2{m, s};
-  __syncthreads();
+  for (int half = SHARES / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (k < half) {
+      m = lds[k][r].x;
+      s = lds[k][r].y;
+      join(lds[k + half][r]);
+      lds[k][r] = float2{m, s};
+    }
+  }
   if (k || p >= M) return;
-  for (int i = 1; i < 64; ++i) join(lds[i][r]);
   const float l = m + logf(s);
   if (lse) lse[p] = l;
   const int64_t t = targets[p];
   if (loss) loss[p] = t >= 0 && t < V ? l - target_z[p] : 0.0f;
 }
 
-__global__ void clear_words_kernel(uint32_t* x, int n) {
-  if ((int)threadIdx.x < n) x[threadIdx.x] = 0;
+__global__ __launch_bounds__(256) void clear_words_kernel(uint32_t* x, int n) {
+  for (int i = threadIdx.x; i < n; i += 256) x[i] = 0;
 }
 
 FP4_D float row_weight(const float* weight, const int64_t* targets, int64_t V, int64_t row) {
@@ -277,26 +303,38 @@ FP4_D float row_weight(const float* weight, const int64_t* targets, int64_t V, i
 }
 
 // Largest magnitude of bf16 x [rows x cols], rows under a weight of their own where there are any; bits of the fp32 value.  A maximum does not depend on
-// the order of its atomics.  cols a multiple of 8.
-__global__ __launch_bounds__(256) void head_amax_kernel(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, const float* weight, const int64_t* targets,
-                                                        int64_t V, uint32_t* amax) {
+// the order of its atomics, of which there are few: they come one after another.  cols a multiple of 8.  A wave a row, eight pieces of it on their
+// way together.
+__global__ __launch_bounds__(1024) void head_amax_kernel(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, const float* weight, const int64_t* targets,
+                                                         int64_t V, uint32_t* amax) {
+  constexpr int AT_ONCE = 8;
+  __shared__ uint32_t lds[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t best = 0;
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+  for (int64_t r = (int64_t)blockIdx.x * 16 + wave; r < rows; r += (int64_t)gridDim.x * 16) {
     uint32_t m = 0;
-    for (int64_t c = (int64_t)threadIdx.x * 8; c < cols; c += 2048) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(x + r * ld + c);
+    for (int64_t c0 = (int64_t)lane * 8; c0 < cols + lane * 8; c0 += 512 * AT_ONCE) {
+      u32x4 w[AT_ONCE];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) m = max(m, max(w[i] << 16 & 0x7fffffffu, w[i] & 0x7fff0000u));
+      for (int k = 0; k < AT_ONCE; ++k) w[k] = *reinterpret_cast<const u32x4*>(x + r * ld + min(c0 + 512 * k, cols - 8));   // what is there counts twice
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = max(m, max(w[k][i] << 16 & 0x7fffffffu, w[k][i] & 0x7fff0000u));
     }
     best = max(best, f2u(u2f(m) * fabsf(row_weight(weight, targets, V, r))));
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o));
-  if ((threadIdx.x & 63) == 0 && best) atomicMax(amax, best);
+  if (lane == 0) lds[wave] = best;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int i = 1; i < 16; ++i) best = max(best, lds[i]);
+  if (best) atomicMax(amax, best);
 }
 
-// x [rows x cols] -> its transpose in fp16 [cols x pitch], zeros from rows to pitch.  x: bf16, under a power of two and rows' weights, or
-// (F16) fp16 as it is.  64 x 64 a workgroup, through LDS; pitch a multiple of 64.
+// x [rows x cols] -> its transpose in fp16 [cols x pitch], zeros from rows to pitch, under a power of two and rows' weights.  64 x 64 a
+// workgroup, through LDS; pitch a multiple of 64.
 struct Across {
   const uint16_t* x;
   int64_t rows, cols, ld;
@@ -307,12 +345,11 @@ struct Across {
   const int64_t* targets;
   int64_t V;
 };
-template <bool F16>
 __global__ __launch_bounds__(256) void head_across_kernel(Across a) {
   __shared__ uint16_t lds[64][66];
   const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
   const int chunk = threadIdx.x & 7;
-  const float scale = F16 ? 1.0f : scale_of(*a.amax, false);
+  const float scale = scale_of(*a.amax, false);
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int r = half * 32 + (threadIdx.x >> 3);
@@ -320,11 +357,9 @@ __global__ __launch_bounds__(256) void head_across_kernel(Across a) {
     u32x4 w = {0, 0, 0, 0};
     if (row < a.rows && col < a.cols) {
       w = *reinterpret_cast<const u32x4*>(a.x + row * a.ld + col);
-      if constexpr (!F16) {
-        const float f = row_weight(a.weight, a.targets, a.V, row);
+      const float f = row_weight(a.weight, a.targets, a.V, row);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = pack_f16(u2f(w[i] << 16) * f * scale, u2f(w[i] & 0xffff0000u) * f * scale);
-      }
+      for (int i = 0; i < 4; ++i) w[i] = pack_f16(u2f(w[i] << 16) * f * scale, u2f(w[i] & 0xffff0000u) * f * scale);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(&lds[r][chunk * 8 + 2 * i]) = w[i];
@@ -364,21 +399,34 @@ __global__ __launch_bounds__(256) void head_dx_kernel(const float* sums, int spl
 
 // ---- which tiles ---------------------------------------------------------------------------------------------------------------
 using Large = HpShape<2, 4, 4, 2, 2>;    // 256 x 256
-using Middle = HpShape<2, 2, 2, 2, 3>;   // 128 x 128
-using Few = HpShape<1, 4, 2, 1, 3>;      // 64 x 128
-using Fewest = HpShape<1, 4, 1, 1, 4>;   // 32 x 128
+using Middle = HpShape<2, 2, 2, 2, 2>;   // 128 x 128, two a CU
+using Few = HpShape<1, 4, 2, 1, 3>;      // 64 x 128, two a CU
+using Fewest = HpShape<1, 4, 1, 1, 4>;   // 32 x 128, two a CU
 constexpr int64_t LEAST_BQ = 128;
 
 enum { TILE_LARGE, TILE_MIDDLE, TILE_FEW, TILE_FEWEST };
-int tile_of(int64_t P, int64_t Q) {
-  if (P <= 32) return TILE_FEWEST;
-  if (P <= 64) return TILE_FEW;
-  const int64_t large = ((P + 255) / 256) * ((Q + 255) / 256);
-  return P <= 128 || large < 128 ? TILE_MIDDLE : TILE_LARGE;
-}
-void tile_size(int tile, int64_t& bp, int64_t& bq) {
-  bp = tile == TILE_LARGE ? 256 : tile == TILE_MIDDLE ? 128 : tile == TILE_FEW ? 64 : 32;
-  bq = tile == TILE_LARGE ? 256 : 128;
+struct Cut { int tile, splits; };
+
+// Few rows: the tiles that do not calculate much in vain, all of them waiting for w (64 x 32768 over 4096: 64 / 128 / 256 rows a tile 40 / 57 / 84 us;
+// 128 rows 55 / 59 / 85).  More: by rounds of the chip's workgroups, in hundredths of a us (measured): a step of 64 takes a 256 x 256 tile 1.41 with
+// half of the CUs at work, 1.74 with all of them (power), two 128 x 128 tiles of one CU 1.05, a single one about 0.65; a tile's start and end
+// 6 and 4.  Splitting the contraction (only where the sums can be added up later: most > 1) brings rounds and takes sums' bytes.
+Cut cut_of(int64_t P, int64_t Q, int64_t K, int most) {
+  const int64_t steps = (K + 63) / 64;
+  const auto tiles = [&](int64_t bp, int64_t bq) { return ((P + bp - 1) / bp) * ((Q + bq - 1) / bq); };
+  most = (int)std::max<int64_t>(1, std::min<int64_t>(most, steps / 4));
+  if (P <= 128) return {P <= 32 ? TILE_FEWEST : TILE_FEW, (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / std::max<int64_t>(1, tiles(P <= 32 ? 32 : 64, 128))))};
+  Cut best = {TILE_LARGE, 1};
+  int64_t least = INT64_MAX;
+  for (int s = 1; s <= most; ++s) {
+    const int64_t k = (steps + s - 1) / s, sums = s > 1 ? s * P * Q / 10000 : 0;   // in 1/100 us: 16 bytes a sum at 5 TB/s would be 3.2 a 10000
+    const int64_t nl = tiles(256, 256) * s, nm = tiles(128, 128) * s, rl = nl % 256, rm = nm % 512;
+    const int64_t large = nl / 256 * (174 * k + 600) + (rl ? (141 + 33 * rl / 256) * k + 600 : 0) + sums;
+    const int64_t middle = nm / 512 * (105 * k + 400) + (rm ? (rm > 256 ? 105 : 65) * k + 400 : 0) + sums;
+    if (large < least) least = large, best = {TILE_LARGE, s};
+    if (middle < least) least = middle, best = {TILE_MIDDLE, s};
+  }
+  return best;
 }
 
 template <class S, int EPI>
@@ -390,17 +438,19 @@ int launch(HeadTile& a, hipStream_t s) {
   return FP4_OK;
 }
 template <int EPI>
-int launch(HeadTile& a, hipStream_t s) {
-  const int tile = tile_of(a.g.P, a.g.Q);
+int launch(HeadTile& a, const Cut& cut, hipStream_t s) {
   const int64_t steps = (a.g.K + 63) / 64;
-  a.g.split_steps = (int)((steps + a.g.splits - 1) / a.g.splits);
-  switch (tile) {
+  a.g.splits = cut.splits;
+  a.g.split_steps = (int)((steps + cut.splits - 1) / cut.splits);
+  switch (cut.tile) {
     case TILE_LARGE: return launch<Large, EPI>(a, s);
     case TILE_MIDDLE: return launch<Middle, EPI>(a, s);
     case TILE_FEW: return launch<Few, EPI>(a, s);
     default: return launch<Fewest, EPI>(a, s);
   }
 }
+template <int EPI>
+int launch(HeadTile& a, hipStream_t s) { return launch<EPI>(a, cut_of(a.g.P, a.g.Q, a.g.K, 1), s); }
 
 // ---- sizes of the pieces and of what they need -----------------------------------------------------------------------------------
 constexpr int64_t PIECE = int64_t{1} << 27;   // elements of dz, and of w's transposed piece
@@ -414,15 +464,8 @@ int64_t piece_rows(int64_t M, int64_t D, int64_t V) {
 }
 size_t piece_room(int64_t lines, int64_t V) { return (size_t)std::min(lines * up(V, 64), PIECE + lines * 256) * 2; }   // never less for more lines
 
-// Parts of dx's contraction: where its tiles are few, so many that the chip is full, within 2^25 sums.
-int dx_splits(int64_t M, int64_t D, int64_t piece) {
-  int64_t bp, bq;
-  tile_size(tile_of(M, D), bp, bq);
-  const int64_t tiles = ((M + bp - 1) / bp) * ((D + bq - 1) / bq), steps = (piece + 63) / 64;
-  int64_t s = std::min<int64_t>(std::min<int64_t>(64, 512 / std::max<int64_t>(1, tiles)), steps / 4);
-  s = std::min(s, (int64_t{1} << 25) / std::max<int64_t>(1, M * D));
-  return (int)std::max<int64_t>(1, s);
-}
+// Parts of dx's contraction: at most 64, within 2^25 sums.
+int most_splits(int64_t M, int64_t D) { return (int)std::max<int64_t>(1, std::min<int64_t>(64, (int64_t{1} << 25) / std::max<int64_t>(1, M * D))); }
 size_t sums_room(int64_t M, int64_t D) { return (size_t)std::max(M * D, std::min(64 * M * D, int64_t{1} << 25)) * 4; }
 
 }  // namespace
@@ -432,7 +475,8 @@ size_t hp_head_fwd_room(int64_t M, int64_t V) {
 }
 size_t hp_head_bwd_room(int64_t M, int64_t D, int64_t V) {
   const int64_t Mp = up(M, 64);
-  return 2 * align_up(piece_room(Mp, V), 256) + align_up(piece_room(D, V), 256) + align_up((size_t)D * Mp * 2, 256) + align_up(sums_room(M, D), 256) + 512;
+  return 2 * align_up(piece_room(Mp, V), 256) + align_up(piece_room(D, V), 256) + align_up((size_t)D * Mp * 2, 256) + align_up(sums_room(M, D), 256) +
+         align_up((size_t)(V / 256 + 2) * 4, 256) + 256;
 }
 
 int hp_launch_head_fwd(const uint16_t* x, const uint16_t* w, const int64_t* targets, int64_t M, int64_t D, int64_t V, int64_t ldx, int64_t ldw, float* loss,
@@ -446,7 +490,8 @@ int hp_launch_head_fwd(const uint16_t* x, const uint16_t* w, const int64_t* targ
   a.part = (float2*)(room + align_up((size_t)M * 4, 256));
   const int rc = launch<EPI_STATS>(a, s);
   if (rc) return rc;
-  head_join_kernel<<<(unsigned)((M + 15) / 16), 1024, 0, s>>>(a.part, a.g.tiles_q, M, V, targets, a.target_z, loss, lse);
+  if (M <= 256) head_join_kernel<4><<<(unsigned)((M + 3) / 4), 1024, 0, s>>>(a.part, a.g.tiles_q, M, V, targets, a.target_z, loss, lse);
+  else head_join_kernel<16><<<(unsigned)((M + 15) / 16), 1024, 0, s>>>(a.part, a.g.tiles_q, M, V, targets, a.target_z, loss, lse);
   FP4_CHECK_LAUNCH();
   return FP4_OK;
 }
@@ -461,65 +506,62 @@ int hp_launch_head_bwd(const uint16_t* x, const uint16_t* w, const int64_t* targ
     at += align_up(n, 256);
     return r;
   };
-  uint32_t* const amax = (uint32_t*)take(8);   // [0]: of c x, [1]: of the piece of w
+  const int pieces = (int)((V + piece - 1) / piece);
+  uint32_t* const amax = (uint32_t*)take((size_t)(pieces + 1) * 4);   // of each piece of w; behind them of c x
   uint16_t* const dz = (uint16_t*)take(piece_room(Mp, V));
   uint16_t* const dz_across = (uint16_t*)take(piece_room(Mp, V));
   uint16_t* const w_across = (uint16_t*)take(piece_room(D, V));
   uint16_t* const x_across = (uint16_t*)take((size_t)D * Mp * 2);
   float* const sums = (float*)take(sums_room(M, D));
-  const auto across = [&](auto f16, const Across& a) {
-    const dim3 grid((unsigned)(a.pitch / 64), (unsigned)((a.cols + 63) / 64));
-    head_across_kernel<decltype(f16)::value><<<grid, 256, 0, s>>>(a);
-  };
-  const auto largest = [&](const uint16_t* m, int64_t rows, int64_t ld, const float* weight, uint32_t* to) {
-    clear_words_kernel<<<1, 64, 0, s>>>(to, 1);
-    head_amax_kernel<<<(unsigned)std::min<int64_t>(rows, 2048), 256, 0, s>>>(m, rows, D, ld, weight, targets, V, to);
+  // A matrix's transpose under the power of two that suits it.
+  const auto across = [&](const uint16_t* m, int64_t rows, int64_t ld, const float* weight, uint16_t* out, int64_t pitch, uint32_t* largest) {
+    head_amax_kernel<<<(unsigned)std::min<int64_t>((rows + 15) / 16, 512), 1024, 0, s>>>(m, rows, D, ld, weight, targets, V, largest);
+    const dim3 grid((unsigned)(pitch / 64), (unsigned)((D + 63) / 64));
+    head_across_kernel<<<grid, 256, 0, s>>>(Across{m, rows, D, ld, out, pitch, largest, weight, targets, V});
   };
   int rc = FP4_OK;
-  if (M == 0) {   // dw's rows are sums of nothing
-    if (!dw) return FP4_OK;
-    clear_words_kernel<<<1, 64, 0, s>>>(amax, 2);
-  } else if (dw) {
-    largest(x, M, ldx, dloss, &amax[0]);
-    across(std::false_type{}, Across{x, M, D, ldx, x_across, Mp, &amax[0], dloss, targets, V});
-    FP4_CHECK_LAUNCH();
-  }
-  const int splits = dx_splits(M, D, piece);
-  for (int64_t first = 0; first < V; first += piece) {
-    const int64_t rows = std::min(piece, V - first), ld = up(rows, 64);
+  if (M == 0 && !dw) return FP4_OK;
+  clear_words_kernel<<<1, 256, 0, s>>>(amax, pieces + 1);
+  if (dw && M > 0) across(x, M, ldx, dloss, x_across, Mp, &amax[pieces]);
+  FP4_CHECK_LAUNCH();
+  const Cut dx_cut = cut_of(M, D, up(piece, 64), most_splits(M, D));   // one for all pieces: they add to the same sums
+  for (int i = 0; i < pieces; ++i) {
+    const int64_t first = i * piece, rows = std::min(piece, V - first), ld = up(rows, 64);
     const uint16_t* const wp = w + first * ldw;
-    HeadTile z = {};
-    z.g = {x, wp, M, rows, D, ldx, ldw, 0, 0, 1, 0};
-    z.targets = targets;
-    z.first = first;
-    z.V = V;
-    z.lse = lse;
-    z.dz = dz;
-    z.ld = ld;
-    if (M > 0 && (rc = launch<EPI_DZ>(z, s))) return rc;
-    if (dx && M > 0) {
-      largest(wp, rows, ldw, nullptr, &amax[1]);
-      across(std::false_type{}, Across{wp, rows, D, ldw, w_across, ld, &amax[1], nullptr, nullptr, 0});
-      HeadTile t = {};
-      t.g = {dz, w_across, M, D, ld, ld, ld, 0, 0, splits, 0};
-      t.sums = sums;
-      t.add = first > 0;
-      t.amax = &amax[1];
-      if ((rc = launch<EPI_ADD>(t, s))) return rc;
+    HeadTile t = {};
+    if (M > 0) {
+      t.g = {x, wp, M, rows, D, ldx, ldw, 0, 0, 1, 0};
+      t.targets = targets;
+      t.first = first;
+      t.V = V;
+      t.lse = lse;
+      t.dz = dx ? dz : nullptr;
+      t.ld = ld;
+      t.dz_across = dw ? dz_across : nullptr;
+      t.ld_across = Mp;
+      if ((rc = launch<EPI_DZ>(t, s))) return rc;
     }
-    if (dw) {
-      if (M > 0) across(std::true_type{}, Across{dz, M, rows, ld, dz_across, Mp, nullptr, nullptr, nullptr, 0});
-      HeadTile t = {};
-      t.g = {dz_across, x_across, rows, D, Mp, Mp, Mp, 0, 0, 1, 0};
+    if (dx && M > 0) {
+      across(wp, rows, ldw, nullptr, w_across, ld, &amax[i]);
+      t = {};
+      t.g = {dz, w_across, M, D, ld, ld, ld, 0, 0, 1, 0};
+      t.sums = sums;
+      t.add = i > 0;
+      t.amax = &amax[i];
+      if ((rc = launch<EPI_ADD>(t, dx_cut, s))) return rc;
+    }
+    if (dw) {   // without tokens sums of nothing
+      t = {};
+      t.g = {dz_across, x_across, rows, D, up(M, 8), Mp, Mp, 0, 0, 1, 0};   // the lines' zeros reach that far
       t.out = (uint8_t*)dw + first * ld_dw * (dw_bf16 ? 2 : 4);
       t.out_bf16 = dw_bf16 != 0;
       t.ld = ld_dw;
       t.add = accumulate != 0;
-      t.amax = &amax[0];
+      t.amax = &amax[pieces];
       if ((rc = launch<EPI_OUT>(t, s))) return rc;
     }
   }
-  if (dx && M > 0) head_dx_kernel<<<(unsigned)((M * (D / 8) + 255) / 256), 256, 0, s>>>(sums, splits, M, D, dloss, targets, V, dx, ld_dx);
+  if (dx && M > 0) head_dx_kernel<<<(unsigned)((M * (D / 8) + 255) / 256), 256, 0, s>>>(sums, dx_cut.splits, M, D, dloss, targets, V, dx, ld_dx);
   FP4_CHECK_LAUNCH();
   return FP4_OK;
 }
