@@ -892,18 +892,31 @@ def _hp_vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, device: to
     """Address of a vector of so many elements, or None."""
     if t is None:
         return None
-    if t.shape != (n,) or t.dtype != dtype or t.device != device or not (n < 2 or t.stride(0) == 1):
+    if t.shape != (n,) or t.dtype is not dtype or t.device != device or not (n < 2 or t.stride(0) == 1):
         raise ValueError("%s must be [%d] contiguous %s on %s" % (name, n, dtype, device))
     return t.data_ptr()
 
 
 def _hp_matrix(t: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torch.device, name: str):
-    """(address, leading dimension) of an input matrix, or nothing."""
+    """(address, leading dimension) of a matrix, or nothing."""
     if t is None:
         return None, 0
-    if t.shape != shape or t.dtype != dtype or t.device != device:
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
         raise ValueError("%s must be %s %s on %s" % (name, tuple(shape), dtype, device))
     return t.data_ptr(), _ld(t, name)
+
+
+def _hp_out(t: Optional[torch.Tensor], like: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torch.device, name: str):
+    """(the caller's output, checked, or a new one; its address; its leading dimension)."""
+    if t is not None:
+        return (t, *_hp_matrix(t, shape, dtype, device, name))
+    cols = shape[1]
+    ld = -(-cols // 8) * 8 or 8
+    if ld == cols and like is not None and like.is_contiguous():
+        t = torch.empty_like(like)   # half a microsecond less than by shape and type, of the ten that a short call takes
+    else:
+        t = torch.empty_strided(shape, (ld, 1), dtype=dtype, device=device)
+    return t, t.data_ptr(), ld
 
 
 class HpNorm:
@@ -922,18 +935,17 @@ class HpNorm:
             raise ValueError("a gate is [D] or [M, D]")
         self.w_before, self.w_after, self.gate, self.scale, self.eps = w_before, w_after, gate, float(scale), float(eps)
 
-    def _arguments(self, x: torch.Tensor):
-        """The structure for tokens like x, checked."""
-        M, D = x.shape
+    def _arguments(self, shape, dtype: torch.dtype, device: torch.device):
+        """The structure for tokens of that kind, checked."""
+        D = shape[1]
         gate, ld_gate = self.gate, 0
-        if gate is None:
-            at = None
-        elif gate.dim() == 1:
-            at = _hp_vector(gate, D, x.dtype, x.device, "gate")
-        else:
-            at, ld_gate = _hp_matrix(gate, x.shape, x.dtype, x.device, "gate")
-        return C.byref(hp_norm(_hp_vector(self.w_before, D, x.dtype, x.device, "w_before"), _hp_vector(self.w_after, D, x.dtype, x.device, "w_after"),
-                               at, ld_gate, self.scale, self.eps))
+        if gate is not None:
+            if gate.dim() == 1:
+                gate = _hp_vector(gate, D, dtype, device, "gate")
+            else:
+                gate, ld_gate = _hp_matrix(gate, shape, dtype, device, "gate")
+        return C.byref(hp_norm(_hp_vector(self.w_before, D, dtype, device, "w_before"), _hp_vector(self.w_after, D, dtype, device, "w_after"), gate, ld_gate,
+                               self.scale, self.eps))
 
 
 class HpNormSaved:
@@ -954,24 +966,25 @@ def hp_norm_fwd(norm: HpNorm, x: torch.Tensor, block: Optional[torch.Tensor] = N
                 h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None):
     """(h, y): the residual stream scale x + gate norm(block), and it normed for the next block (None without w_before).  saved: filled for the
     backward pass.  h or y may be x or block."""
-    px, ldx = x.data_ptr(), _ld(x, "x")
+    ldx = _ld(x, "x")
     dt, stream = _dt(x), _stream_of(x)
-    M, D = x.shape
-    pb, ldb = _hp_matrix(block, x.shape, x.dtype, x.device, "block")
+    shape, dtype, device = like = x.shape, x.dtype, x.device
+    M, D = shape
+    pb, ldb = _hp_matrix(block, *like, "block")
     if block is None and (norm.w_after is not None or norm.gate is not None):
         raise ValueError("a norm after a block or a gate needs the block")
-    if y is not None and norm.w_before is None:
-        raise ValueError("y needs w_before")
-    ref = norm._arguments(x)
-    h = _out(h, x.shape, x.dtype, x.device, "h")
+    ref = norm._arguments(*like)
+    h, ph, ldh = _hp_out(h, x, *like, "h")
+    py, ldy = None, 0
     if norm.w_before is not None:
-        y = _out(y, x.shape, x.dtype, x.device, "y")
+        y, py, ldy = _hp_out(y, x, *like, "y")
+    elif y is not None:
+        raise ValueError("y needs w_before")
     rb = ra = None
     if saved is not None:
-        rb = _hp_vector(saved.r_before, M, torch.float32, x.device, "r_before") if norm.w_before is not None else None
-        ra = _hp_vector(saved.r_after, M, torch.float32, x.device, "r_after") if norm.w_after is not None else None
-    _check(lib().hp_norm_fwd(ref, dt, M, D, px, ldx, pb, ldb, h.data_ptr(), _ld(h, "h"), None if y is None else y.data_ptr(),
-                             0 if y is None else _ld(y, "y"), rb, ra, stream), "hp_norm_fwd")
+        rb = _hp_vector(saved.r_before, M, torch.float32, device, "r_before") if norm.w_before is not None else None
+        ra = _hp_vector(saved.r_after, M, torch.float32, device, "r_after") if norm.w_after is not None else None
+    _check(lib().hp_norm_fwd(ref, dt, M, D, x.data_ptr(), ldx, pb, ldb, ph, ldh, py, ldy, rb, ra, stream), "hp_norm_fwd")
     return h, y
 
 
@@ -997,14 +1010,14 @@ def hp_norm_bwd(norm: HpNorm, saved: HpNormSaved, h: torch.Tensor, dy: Optional[
         raise ValueError("a norm after a block or a gate needs the block")
     if accumulate and into is None:
         raise ValueError("accumulate needs the gradients to add to")
-    ph, ldh = h.data_ptr(), _ld(h, "h")
+    ldh = _ld(h, "h")
     dt, stream = _dt(h), _stream_of(h)
+    like = h.shape, h.dtype, h.device
     M, D = h.shape
-    like = (h.shape, h.dtype, h.device)
     pdy, ld_dy = _hp_matrix(dy, *like, "dy")
     pdh, ld_dh = _hp_matrix(dh, *like, "dh")
     pb, ldb = _hp_matrix(block, *like, "block")
-    ref = norm._arguments(h)
+    ref = norm._arguments(*like)
     rb = _hp_vector(saved.r_before, M, torch.float32, h.device, "r_before") if dy is not None else None
     ra = _hp_vector(saved.r_after, M, torch.float32, h.device, "r_after") if norm.w_after is not None else None
     if (dy is not None and rb is None) or (norm.w_after is not None and ra is None):
@@ -1016,42 +1029,42 @@ def hp_norm_bwd(norm: HpNorm, saved: HpNormSaved, h: torch.Tensor, dy: Optional[
             if accumulate:
                 raise ValueError("accumulate needs the %s to add to" % name)
             t = torch.empty(D, dtype=torch.float32, device=h.device)
-        _hp_vector(t, D, torch.float32, h.device, name)
-        return t
+        return t, _hp_vector(t, D, torch.float32, h.device, name)
 
-    dx = _out(given.dx, *like, "dx")
-    dblock = None if block is None else _out(given.dblock, *like, "dblock")
-    dgate, ld_dgate = None, 0
+    dblock = dgate = dw_before = dw_after = pdblock = pdgate = pwb = pwa = None
+    ld_dblock = ld_dgate = 0
+    dx, pdx, ld_dx = _hp_out(given.dx, h, *like, "dx")
+    if block is not None:
+        dblock, pdblock, ld_dblock = _hp_out(given.dblock, h, *like, "dblock")
     if norm.gate is not None:
         if norm.gate.dim() == 1:
-            dgate = sums(given.dgate, "dgate")
+            dgate, pdgate = sums(given.dgate, "dgate")
         else:
-            dgate = _out(given.dgate, *like, "dgate")
-            ld_dgate = _ld(dgate, "dgate")
-    dw_before = sums(given.dw_before, "dw_before") if dy is not None else None
-    dw_after = sums(given.dw_after, "dw_after") if norm.w_after is not None else None
+            dgate, pdgate, ld_dgate = _hp_out(given.dgate, h, *like, "dgate")
+    if dy is not None:
+        dw_before, pwb = sums(given.dw_before, "dw_before")
+    if norm.w_after is not None:
+        dw_after, pwa = sums(given.dw_after, "dw_after")
     need = _mx_room(FP4_OP_HP_NORM_BWD, M, D, 0)
     room = _default_workspace(h.device.index, stream)._sized(need) if ws is None else ws.get(need)
-    at = lambda t: None if t is None else t.data_ptr()
-    _check(lib().hp_norm_bwd(ref, dt, M, D, pdy, ld_dy, pdh, ld_dh, ph, ldh, pb, ldb, rb, ra, dx.data_ptr(), _ld(dx, "dx"), at(dblock),
-                             0 if dblock is None else _ld(dblock, "dblock"), at(dgate), ld_dgate, at(dw_before), at(dw_after), int(accumulate),
-                             room.data_ptr(), room.numel(), stream), "hp_norm_bwd")
+    _check(lib().hp_norm_bwd(ref, dt, M, D, pdy, ld_dy, pdh, ld_dh, h.data_ptr(), ldh, pb, ldb, rb, ra, pdx, ld_dx, pdblock, ld_dblock, pdgate, ld_dgate, pwb, pwa,
+                             int(accumulate), room.data_ptr(), room.numel(), stream), "hp_norm_bwd")
     return HpNormGrads(dx, dblock, dgate, dw_before, dw_after)
 
 
 def _hp_ids(ids: torch.Tensor, device: torch.device, name: str) -> int:
-    if ids.dim() != 1 or ids.dtype != torch.int64 or ids.device != device or not (ids.numel() < 2 or ids.stride(0) == 1):
+    if ids.dim() != 1 or ids.dtype is not torch.int64 or ids.device != device or not (ids.stride(0) == 1 or ids.shape[0] < 2):
         raise ValueError("%s must be [M] contiguous int64 on %s" % (name, device))
     return ids.data_ptr()
 
 
 def hp_embed_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """scale table[ids], table [V, D]; zeros for ids outside [0, V)."""
-    ldt, dt, stream = _ld(table, "table"), _dt(table), _stream_of(table)
-    at = _hp_ids(ids, table.device, "ids")
+    ldt, dt, stream, device = _ld(table, "table"), _dt(table), _stream_of(table), table.device
+    at = _hp_ids(ids, device, "ids")
     M, (V, D) = ids.shape[0], table.shape
-    y = _out(y, (M, D), table.dtype, table.device, "y")
-    _check(lib().hp_embed_fwd(at, dt, M, D, V, table.data_ptr(), ldt, scale, y.data_ptr(), _ld(y, "y"), stream), "hp_embed_fwd")
+    y, py, ldy = _hp_out(y, None, (M, D), table.dtype, device, "y")
+    _check(lib().hp_embed_fwd(at, dt, M, D, V, table.data_ptr(), ldt, scale, py, ldy, stream), "hp_embed_fwd")
     return y
 
 
@@ -1065,11 +1078,11 @@ def hp_embed_bwd(dy: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0
         raise ValueError("dy [M,D] and ids [M] must agree in M")
     if accumulate and dtable is None:
         raise ValueError("accumulate needs the dtable to add to")
-    dtable = _out(dtable, (V, D), torch.float32, dy.device, "dtable")
+    dtable, pt, ld_table = _hp_out(dtable, None, (V, D), torch.float32, dy.device, "dtable")
     need = _mx_room(FP4_OP_HP_EMBED_BWD, M, D, V)
     room = _default_workspace(dy.device.index, stream)._sized(need) if ws is None else ws.get(need)
-    _check(lib().hp_embed_bwd(at, dt, M, D, V, dy.data_ptr(), ld, scale, int(accumulate), dtable.data_ptr(), _ld(dtable, "dtable"), room.data_ptr(),
-                              room.numel(), stream), "hp_embed_bwd")
+    _check(lib().hp_embed_bwd(at, dt, M, D, V, dy.data_ptr(), ld, scale, int(accumulate), pt, ld_table, room.data_ptr(), room.numel(), stream),
+           "hp_embed_bwd")
     return dtable
 
 
@@ -1113,15 +1126,18 @@ def hp_head_bwd(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: to
         raise ValueError("one of the gradients has to be wanted")
     if accumulate and want_dw and (dw is None or dw.dtype != torch.float32):
         raise ValueError("accumulate needs the fp32 dw to add to")
-    dx = _out(dx, x.shape, torch.bfloat16, x.device, "dx") if want_dx else None
-    dw = _out(dw, w.shape, dw.dtype if dw is not None else dw_dtype, x.device, "dw") if want_dw else None
+    pdx = pdw = None
+    ld_dx = ld_dw = 0
+    if want_dx:
+        dx, pdx, ld_dx = _hp_out(dx, x, x.shape, torch.bfloat16, x.device, "dx")
+    if want_dw:
+        dw, pdw, ld_dw = _hp_out(dw, None, w.shape, dw.dtype if dw is not None else dw_dtype, x.device, "dw")
     given = (_hp_vector(lse, M, torch.float32, x.device, "lse"), _hp_vector(dloss, M, torch.float32, x.device, "dloss"))
     need = _mx_room(FP4_OP_HP_HEAD_BWD, M, D, V)
     room = _default_workspace(x.device.index, stream)._sized(need) if ws is None else ws.get(need)
-    _check(lib().hp_head_bwd(x.data_ptr(), w.data_ptr(), at, *given, FP4_BF16, M, D, V, ldx, ldw, None if dx is None else dx.data_ptr(),
-                             0 if dx is None else _ld(dx, "dx"), None if dw is None else dw.data_ptr(), FP4_BF16 if dw is None else _dt(dw),
-                             0 if dw is None else _ld(dw, "dw"), int(accumulate and want_dw), room.data_ptr(), room.numel(), stream), "hp_head_bwd")
-    return dx, dw
+    _check(lib().hp_head_bwd(x.data_ptr(), w.data_ptr(), at, *given, FP4_BF16, M, D, V, ldx, ldw, pdx, ld_dx, pdw, _dt(dw) if want_dw else FP4_BF16, ld_dw,
+                             int(accumulate and want_dw), room.data_ptr(), room.numel(), stream), "hp_head_bwd")
+    return dx if want_dx else None, dw if want_dw else None
 
 
 def fp4_unpack(codes: torch.Tensor) -> torch.Tensor:
