@@ -43,6 +43,8 @@ struct HeadTile {
   const uint32_t* amax;      // ADD, OUT: of the operand under a power of two
   void* out;                 // OUT
   bool out_bf16;
+  uint32_t* clear;           // DZ: words that become 0
+  int clear_n;
 };
 
 template <class S>
@@ -242,7 +244,11 @@ __global__ __launch_bounds__(S::WAVES * 64) void head_tile_kernel(HeadTile a) {
   const HpTile tile = hp_tile_at(a.g);
   hp_tile_sums<S, EPI == EPI_ADD || EPI == EPI_OUT>(a.g, tile, smem, acc);
   if constexpr (EPI == EPI_STATS) stats_epilogue<S>(a, tile, smem, acc);
-  if constexpr (EPI == EPI_DZ) dz_epilogue<S>(a, tile, acc);
+  if constexpr (EPI == EPI_DZ) {
+    dz_epilogue<S>(a, tile, acc);
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x; i < a.clear_n; i += S::WAVES * 64) a.clear[i] = 0;
+  }
   if constexpr (EPI == EPI_ADD) f32_epilogue<S>(a, tile, acc, a.sums + (int64_t)tile.split * a.g.P * a.g.Q, a.g.Q, scale_of(*a.amax, true) / DZ_SCALE);
   if constexpr (EPI == EPI_OUT) {
     const float factor = scale_of(*a.amax, true) / DZ_SCALE;
@@ -302,27 +308,42 @@ FP4_D float row_weight(const float* weight, const int64_t* targets, int64_t V, i
   return t >= 0 && t < V ? weight[row] : 0.0f;
 }
 
-// Largest magnitude of bf16 x [rows x cols], rows under a weight of their own where there are any; bits of the fp32 value.  A maximum does not depend on
-// the order of its atomics, of which there are few: they come one after another.  cols a multiple of 8.  A wave a row, eight pieces of it on their
-// way together.
-__global__ __launch_bounds__(1024) void head_amax_kernel(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld, const float* weight, const int64_t* targets,
-                                                         int64_t V, uint32_t* amax) {
+// A matrix that is transposed into fp16 under a power of two: bf16 x [rows x cols], cols a multiple of 8, rows under a weight of their own where there
+// are any -> out [cols x pitch], pitch a multiple of 64, zeros from rows on.
+struct Across {
+  const uint16_t* x;
+  int64_t rows, cols, ld;
+  uint16_t* out;
+  int64_t pitch;
+  uint32_t* amax;            // bits of the largest magnitude, 0 before
+  const float* weight;
+  const int64_t* targets;
+  int64_t V;
+};
+struct AcrossBoth { Across m[2]; int groups; };   // workgroups of the first
+
+// Its largest magnitude.  A maximum does not depend on the order of its atomics, of which there are few: they come one after another.  A wave a
+// row, eight pieces of it on their way together.
+__global__ __launch_bounds__(1024) void head_amax_kernel(AcrossBoth both) {
   constexpr int AT_ONCE = 8;
   __shared__ uint32_t lds[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool second = (int)blockIdx.x >= both.groups;
+  const Across& a = both.m[second];
+  const int group = second ? blockIdx.x - both.groups : blockIdx.x, groups = second ? gridDim.x - both.groups : both.groups;
   uint32_t best = 0;
-  for (int64_t r = (int64_t)blockIdx.x * 16 + wave; r < rows; r += (int64_t)gridDim.x * 16) {
+  for (int64_t r = (int64_t)group * 16 + wave; r < a.rows; r += (int64_t)groups * 16) {
     uint32_t m = 0;
-    for (int64_t c0 = (int64_t)lane * 8; c0 < cols + lane * 8; c0 += 512 * AT_ONCE) {
+    for (int64_t c0 = (int64_t)lane * 8; c0 < a.cols + lane * 8; c0 += 512 * AT_ONCE) {
       u32x4 w[AT_ONCE];
 #pragma unroll
-      for (int k = 0; k < AT_ONCE; ++k) w[k] = *reinterpret_cast<const u32x4*>(x + r * ld + min(c0 + 512 * k, cols - 8));   // what is there counts twice
+      for (int k = 0; k < AT_ONCE; ++k) w[k] = *reinterpret_cast<const u32x4*>(a.x + r * a.ld + min(c0 + 512 * k, a.cols - 8));   // the last piece may count again
 #pragma unroll
       for (int k = 0; k < AT_ONCE; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = max(m, max(w[k][i] << 16 & 0x7fffffffu, w[k][i] & 0x7fff0000u));
     }
-    best = max(best, f2u(u2f(m) * fabsf(row_weight(weight, targets, V, r))));
+    best = max(best, f2u(u2f(m) * fabsf(row_weight(a.weight, a.targets, a.V, r))));
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o));
@@ -330,24 +351,16 @@ __global__ __launch_bounds__(1024) void head_amax_kernel(const uint16_t* x, int6
   __syncthreads();
   if (threadIdx.x) return;
   for (int i = 1; i < 16; ++i) best = max(best, lds[i]);
-  if (best) atomicMax(amax, best);
+  if (best) atomicMax(a.amax, best);
 }
 
-// x [rows x cols] -> its transpose in fp16 [cols x pitch], zeros from rows to pitch, under a power of two and rows' weights.  64 x 64 a
-// workgroup, through LDS; pitch a multiple of 64.
-struct Across {
-  const uint16_t* x;
-  int64_t rows, cols, ld;
-  uint16_t* out;
-  int64_t pitch;
-  const uint32_t* amax;
-  const float* weight;
-  const int64_t* targets;
-  int64_t V;
-};
-__global__ __launch_bounds__(256) void head_across_kernel(Across a) {
+// The transpose, 64 x 64 a workgroup, through LDS.
+__global__ __launch_bounds__(256) void head_across_kernel(AcrossBoth both) {
   __shared__ uint16_t lds[64][66];
-  const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+  const bool second = (int)blockIdx.x >= both.groups;
+  const Across& a = both.m[second];
+  const int group = second ? blockIdx.x - both.groups : blockIdx.x, lines = (int)(a.pitch / 64);
+  const int64_t r0 = (int64_t)(group % lines) * 64, c0 = (int64_t)(group / lines) * 64;
   const int chunk = threadIdx.x & 7;
   const float scale = scale_of(*a.amax, false);
 #pragma unroll
@@ -377,24 +390,117 @@ __global__ __launch_bounds__(256) void head_across_kernel(Across a) {
   }
 }
 
+// dx's sums for few tokens, w read once as it lies: 256 columns a workgroup, whose four waves share a part of the vocabulary.  A lane loads eight
+// rows of eight columns and turns them in its registers into eight operands, each eight rows of one column (matrix instruction f
+// takes columns 8 n + f), so that nothing passes through LDS.  w stays bf16; dz's 11 bits are the sum of two bf16, a product each: it is w's bytes that bound this.
+struct FewDx {
+  const uint16_t *dz, *w;
+  float* sums;               // [splits][M x D]
+  int64_t M, D, ld, ldw, rows;   // rows: of w, dz has zeros behind them
+  int64_t share;             // rows of a split, a multiple of 64
+  bool add;                  // to what is there
+};
+template <int PB>
+__global__ __launch_bounds__(256, PB == 1 ? 2 : 1) void head_dx_few_kernel(FewDx a) {
+  __shared__ __attribute__((aligned(16))) float lds[PB * 32][256];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
+  const int64_t m0 = (int64_t)blockIdx.z * (PB * 32), d0 = (int64_t)blockIdx.x * 256;
+  const int64_t from = blockIdx.y * a.share + wave * (a.share / 4), to = min(a.ld, from + a.share / 4);
+  const uint16_t* const w = a.w + min(d0 + l32 * 8, a.D - 8);
+  const uint16_t* z[PB];
+#pragma unroll
+  for (int b = 0; b < PB; ++b) z[b] = a.dz + min(m0 + b * 32 + l32, a.M - 1) * a.ld + 8 * h;
+  hp_f32x16 acc[PB][8];
+#pragma unroll
+  for (int b = 0; b < PB; ++b)
+#pragma unroll
+    for (int f = 0; f < 8; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[b][f][v] = 0.0f;
+  struct Step { u32x4 w[8], z[PB]; };
+  const auto load = [&](Step& s, int64_t v) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s.w[j] = *reinterpret_cast<const u32x4*>(w + min(v + 8 * h + j, a.rows - 1) * a.ldw);
+#pragma unroll
+    for (int b = 0; b < PB; ++b) s.z[b] = *reinterpret_cast<const u32x4*>(z[b] + v);
+  };
+  Step next;
+  if (from < to) load(next, from);
+  for (int64_t v = from; v < to; v += 16) {
+    const Step s = next;
+    load(next, min(v + 16, to - 16));
+    u32x4 high[PB], low[PB];
+#pragma unroll
+    for (int b = 0; b < PB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t two = s.z[b][i];
+        const hp_f16x2 x = __builtin_bit_cast(hp_f16x2, two);
+        const float x0 = (float)x.x, x1 = (float)x.y;
+        high[b][i] = hp_pack_bf16(x0, x1);
+        low[b][i] = hp_pack_bf16(x0 - u2f(high[b][i] << 16), x1 - u2f(high[b][i] & 0xffff0000u));
+      }
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+      u32x4 t;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) t[j] = __builtin_amdgcn_perm(s.w[2 * j + 1][f / 2], s.w[2 * j][f / 2], f % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int b = 0; b < PB; ++b) {
+        acc[b][f] = hp_mfma<false>(high[b], t, acc[b][f]);
+        acc[b][f] = hp_mfma<false>(low[b], t, acc[b][f]);
+      }
+    }
+  }
+  // The waves' sums in their order.  Register 4 b + e: row 8 b + 4 h + e of the tokens, columns 8 l32 + f.
+  for (int turn = 0; turn < 4; ++turn) {
+    if (wave == turn) {
+#pragma unroll
+      for (int b = 0; b < PB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          f32x4* const o = reinterpret_cast<f32x4*>(&lds[b * 32 + v / 4 * 8 + h * 4 + v % 4][l32 * 8]);
+          f32x4 x = {acc[b][0][v], acc[b][1][v], acc[b][2][v], acc[b][3][v]}, y = {acc[b][4][v], acc[b][5][v], acc[b][6][v], acc[b][7][v]};
+          if (turn > 0) {
+            x += o[0];
+            y += o[1];
+          }
+          o[0] = x;
+          o[1] = y;
+        }
+    }
+    __syncthreads();
+  }
+  float* const out = a.sums + (int64_t)blockIdx.y * a.M * a.D;
+  for (int i = threadIdx.x; i < PB * 32 * 64; i += 256) {
+    const int64_t m = m0 + i / 64, d = d0 + i % 64 * 4;
+    if (m >= a.M || d >= a.D) continue;
+    f32x4* const o = reinterpret_cast<f32x4*>(out + m * a.D + d);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(&lds[i / 64][i % 64 * 4]) * (1.0f / DZ_SCALE);
+    *o = a.add ? *o + x : x;
+  }
+}
+
 // dx[t] = c_t sum over the splits of sums[., t], rounded to bf16.  D a multiple of 8.
 __global__ __launch_bounds__(256) void head_dx_kernel(const float* sums, int splits, int64_t M, int64_t D, const float* dloss, const int64_t* targets, int64_t V,
                                                       uint16_t* dx, int64_t ld) {
-  const int64_t n = D / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= M * n) return;
-  const int64_t row = i / n, c = i % n * 8;
-  const float f = row_weight(dloss, targets, V, row);
-  float s[8];
+  constexpr int AT_ONCE = 8;
+  const int64_t n = D / 4;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * n; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / n, c = i % n * 4;
+    const float f = row_weight(dloss, targets, V, row);
+    f32x4 s = {0, 0, 0, 0};
+    for (int k0 = 0; k0 < splits; k0 += AT_ONCE) {
+      f32x4 r[AT_ONCE];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s[e] = 0.0f;
-  for (int k = 0; k < splits; ++k) {
-    const Raw8<F32> r = hp_load8<F32>(sums + ((int64_t)k * M + row) * D, c, D);
+      for (int k = 0; k < AT_ONCE; ++k) r[k] = *reinterpret_cast<const f32x4*>(sums + ((int64_t)min(k0 + k, splits - 1) * M + row) * D + c);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] += r.get(e);
+      for (int k = 0; k < AT_ONCE; ++k)
+        if (k0 + k < splits) s += r[k];
+    }
+    s = f == 0.0f ? f32x4{0, 0, 0, 0} : s * f;
+    *reinterpret_cast<u32x2*>(dx + row * ld + c) = u32x2{hp_pack_bf16(s.x, s.y), hp_pack_bf16(s.z, s.w)};
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) s[e] = f == 0.0f ? 0.0f : s[e] * f;
-  hp_store8<BF16>(dx + row * ld, c, D, s);
 }
 
 // ---- which tiles ---------------------------------------------------------------------------------------------------------------
@@ -456,9 +562,12 @@ int launch(HeadTile& a, hipStream_t s) { return launch<EPI>(a, cut_of(a.g.P, a.g
 constexpr int64_t PIECE = int64_t{1} << 27;   // elements of dz, and of w's transposed piece
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
+// Few tokens: their dx needs no transposed piece of w (both gradients, 4096 into 32000: 1 token 364 us with it, 213 without, 120 tokens 404 / 304).
+bool few_tokens(int64_t M) { return M <= 128; }
+
 // Rows of w a piece: as many as the room allows, the pieces alike.
 int64_t piece_rows(int64_t M, int64_t D, int64_t V) {
-  const int64_t most = std::max<int64_t>(256, PIECE / std::max(up(M, 64), D) / 256 * 256);
+  const int64_t most = std::max<int64_t>(256, PIECE / (few_tokens(M) ? std::max<int64_t>(64, up(M, 64)) : std::max(up(M, 64), D)) / 256 * 256);
   const int64_t pieces = (V + most - 1) / most;
   return std::min(up((V + pieces - 1) / pieces, 256), up(V, 64));
 }
@@ -470,7 +579,11 @@ size_t sums_room(int64_t M, int64_t D) { return (size_t)std::max(M * D, std::min
 
 }  // namespace
 
+// The forward pass goes over the tokens so many at a time, which bounds the tiles' maxima and sums.
+constexpr int64_t FWD_TOKENS = 32768;
+
 size_t hp_head_fwd_room(int64_t M, int64_t V) {
+  M = std::min(M, FWD_TOKENS);
   return align_up((size_t)((V + LEAST_BQ - 1) / LEAST_BQ) * (size_t)M * 8, 256) + align_up((size_t)M * 4, 256) + 256;
 }
 size_t hp_head_bwd_room(int64_t M, int64_t D, int64_t V) {
@@ -482,17 +595,22 @@ size_t hp_head_bwd_room(int64_t M, int64_t D, int64_t V) {
 int hp_launch_head_fwd(const uint16_t* x, const uint16_t* w, const int64_t* targets, int64_t M, int64_t D, int64_t V, int64_t ldx, int64_t ldw, float* loss,
                        float* lse, void* workspace, hipStream_t s) {
   uint8_t* room = (uint8_t*)align_up((size_t)(uintptr_t)workspace, 256);
-  HeadTile a = {};
-  a.g = {x, w, M, V, D, ldx, ldw, 0, 0, 1, 0};
-  a.targets = targets;
-  a.V = V;
-  a.target_z = (float*)room;
-  a.part = (float2*)(room + align_up((size_t)M * 4, 256));
-  const int rc = launch<EPI_STATS>(a, s);
-  if (rc) return rc;
-  if (M <= 256) head_join_kernel<4><<<(unsigned)((M + 3) / 4), 1024, 0, s>>>(a.part, a.g.tiles_q, M, V, targets, a.target_z, loss, lse);
-  else head_join_kernel<16><<<(unsigned)((M + 15) / 16), 1024, 0, s>>>(a.part, a.g.tiles_q, M, V, targets, a.target_z, loss, lse);
-  FP4_CHECK_LAUNCH();
+  for (int64_t first = 0; first < M; first += FWD_TOKENS) {
+    const int64_t m = std::min(FWD_TOKENS, M - first);
+    const int64_t* const t = targets + first;
+    HeadTile a = {};
+    a.g = {x + first * ldx, w, m, V, D, ldx, ldw, 0, 0, 1, 0};
+    a.targets = t;
+    a.V = V;
+    a.target_z = (float*)room;
+    a.part = (float2*)(room + align_up((size_t)m * 4, 256));
+    const int rc = launch<EPI_STATS>(a, s);
+    if (rc) return rc;
+    float *const to_loss = loss ? loss + first : nullptr, *const to_lse = lse ? lse + first : nullptr;
+    if (m <= 256) head_join_kernel<4><<<(unsigned)((m + 3) / 4), 1024, 0, s>>>(a.part, a.g.tiles_q, m, V, t, a.target_z, to_loss, to_lse);
+    else head_join_kernel<16><<<(unsigned)((m + 15) / 16), 1024, 0, s>>>(a.part, a.g.tiles_q, m, V, t, a.target_z, to_loss, to_lse);
+    FP4_CHECK_LAUNCH();
+  }
   return FP4_OK;
 }
 
@@ -513,18 +631,24 @@ int hp_launch_head_bwd(const uint16_t* x, const uint16_t* w, const int64_t* targ
   uint16_t* const w_across = (uint16_t*)take(piece_room(D, V));
   uint16_t* const x_across = (uint16_t*)take((size_t)D * Mp * 2);
   float* const sums = (float*)take(sums_room(M, D));
-  // A matrix's transpose under the power of two that suits it.
-  const auto across = [&](const uint16_t* m, int64_t rows, int64_t ld, const float* weight, uint16_t* out, int64_t pitch, uint32_t* largest) {
-    head_amax_kernel<<<(unsigned)std::min<int64_t>((rows + 15) / 16, 512), 1024, 0, s>>>(m, rows, D, ld, weight, targets, V, largest);
-    const dim3 grid((unsigned)(pitch / 64), (unsigned)((D + 63) / 64));
-    head_across_kernel<<<grid, 256, 0, s>>>(Across{m, rows, D, ld, out, pitch, largest, weight, targets, V});
+  // One or two matrices' transposes under the powers of two that suit them.
+  const auto across = [&](const Across& first, const Across* second) {
+    const auto rows_groups = [](const Across& a) { return (int)std::min<int64_t>((a.rows + 15) / 16, 512); };
+    const auto tiles = [](const Across& a) { return (int)(a.pitch / 64 * ((a.cols + 63) / 64)); };
+    AcrossBoth both = {{first, second ? *second : first}, rows_groups(first)};
+    head_amax_kernel<<<both.groups + (second ? rows_groups(*second) : 0), 1024, 0, s>>>(both);
+    both.groups = tiles(first);
+    head_across_kernel<<<both.groups + (second ? tiles(*second) : 0), 256, 0, s>>>(both);
   };
   int rc = FP4_OK;
   if (M == 0 && !dw) return FP4_OK;
-  clear_words_kernel<<<1, 256, 0, s>>>(amax, pieces + 1);
-  if (dw && M > 0) across(x, M, ldx, dloss, x_across, Mp, &amax[pieces]);
-  FP4_CHECK_LAUNCH();
-  const Cut dx_cut = cut_of(M, D, up(piece, 64), most_splits(M, D));   // one for all pieces: they add to the same sums
+  if (M == 0) {
+    clear_words_kernel<<<1, 256, 0, s>>>(amax, pieces + 1);
+    FP4_CHECK_LAUNCH();
+  }
+  const Across cx = {x, M, D, ldx, x_across, Mp, &amax[pieces], dloss, targets, V};
+  const bool few = few_tokens(M);
+  Cut dx_cut = cut_of(M, D, up(piece, 64), most_splits(M, D));   // one for all pieces: they add to the same sums
   for (int i = 0; i < pieces; ++i) {
     const int64_t first = i * piece, rows = std::min(piece, V - first), ld = up(rows, 64);
     const uint16_t* const wp = w + first * ldw;
@@ -539,10 +663,26 @@ int hp_launch_head_bwd(const uint16_t* x, const uint16_t* w, const int64_t* targ
       t.ld = ld;
       t.dz_across = dw ? dz_across : nullptr;
       t.ld_across = Mp;
+      t.clear = amax;
+      t.clear_n = i == 0 ? pieces + 1 : 0;
       if ((rc = launch<EPI_DZ>(t, s))) return rc;
+      const Across piece_of_w = {wp, rows, D, ldw, w_across, ld, &amax[i], nullptr, nullptr, 0};
+      if (dx && !few) across(piece_of_w, dw && i == 0 ? &cx : nullptr);
+      else if (dw && i == 0) across(cx, nullptr);
     }
-    if (dx && M > 0) {
-      across(wp, rows, ldw, nullptr, w_across, ld, &amax[i]);
+    if (dx && few && M > 0) {
+      const int slices = (int)((D + 255) / 256), blocks = M <= 64 ? 1 : 2;
+      const int64_t most = std::min<int64_t>(most_splits(M, D), std::max(1, 512 / (slices * blocks)));
+      const int64_t share = up((up(piece, 64) + most - 1) / most, 64);
+      const int splits = (int)((ld + share - 1) / share);
+      if (i == 0) dx_cut.splits = splits;   // a later piece has as many at most
+      const FewDx f = {dz, wp, sums, M, D, ld, ldw, rows, share, i > 0};
+      const dim3 grid((unsigned)slices, (unsigned)splits, (unsigned)blocks);
+      if (M <= 32) head_dx_few_kernel<1><<<grid, 256, 0, s>>>(f);
+      else head_dx_few_kernel<2><<<grid, 256, 0, s>>>(f);
+      FP4_CHECK_LAUNCH();
+    }
+    if (dx && !few && M > 0) {
       t = {};
       t.g = {dz, w_across, M, D, ld, ld, ld, 0, 0, 1, 0};
       t.sums = sums;
@@ -561,7 +701,7 @@ int hp_launch_head_bwd(const uint16_t* x, const uint16_t* w, const int64_t* targ
       if ((rc = launch<EPI_OUT>(t, s))) return rc;
     }
   }
-  if (dx && M > 0) head_dx_kernel<<<(unsigned)((M * (D / 8) + 255) / 256), 256, 0, s>>>(sums, dx_cut.splits, M, D, dloss, targets, V, dx, ld_dx);
+  if (dx && M > 0) head_dx_kernel<<<(unsigned)std::min<int64_t>((M * (D / 4) + 255) / 256, 1 << 22), 256, 0, s>>>(sums, dx_cut.splits, M, D, dloss, targets, V, dx, ld_dx);
   FP4_CHECK_LAUNCH();
   return FP4_OK;
 }

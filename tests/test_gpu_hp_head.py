@@ -51,6 +51,19 @@ def test_several_pieces_of_short_rows():
     check(*inputs(M, D, V, pad=0, lean=0.5), dw_dtype=torch.bfloat16)
 
 
+@pytest.mark.parametrize("M", [32768, 33001])
+def test_many_tokens(M):
+    """More than the forward pass takes at a time."""
+    check(*inputs(M, 32, 300, pad=0), dw_dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("M", [1, 31, 32, 33, 63, 64, 65, 96, 127, 128, 129])
+@pytest.mark.parametrize("D,V", [(8, 900), (264, 333), (520, 4100)])
+def test_few_tokens(M, D, V):
+    """The gradient of x around the sizes where another kernel takes over, widths that end inside its 256 columns."""
+    check(*inputs(M, D, V, seed=M))
+
+
 def test_sharp_and_flat_rows():
     x, w, targets, dloss = inputs(200, 256, 700, spread=0.5, lean=40.0)
     x[:50] *= 4.0
