@@ -423,7 +423,8 @@ int hp_head_fwd(const void* x, const void* w, const int64_t* targets, fp4_dtype 
  * Either may be NULL, not both.  The products' operands are rounded to 11 bits (fp16 under powers of two: exact for w and for dloss x but
  * for its product's rounding), sums are fp32: dw in fp32 is as near as that.  A target's entry below 2^-40 of 1 and weights below 2^-39
  * of their largest are taken as 0.
- * Workspace: fp4_workspace_bytes(FP4_OP_HP_HEAD_BWD, M, D, V, dt); dz takes at most 2^27 elements and 256 a token of it, twice. */
+ * Workspace: fp4_workspace_bytes(FP4_OP_HP_HEAD_BWD, M, D, V, dt); dz takes at most 2^28 fp16 elements and 256 a token of it,
+ * twice; w's transposed piece as many. */
 int hp_head_bwd(const void* x, const void* w, const int64_t* targets, const float* lse, const float* dloss, fp4_dtype dt, int64_t M, int64_t D,
                 int64_t V, int64_t ldx, int64_t ldw, void* dx, int64_t ld_dx, void* dw, fp4_dtype dw_dt, int64_t ld_dw, int accumulate,
                 void* workspace, size_t workspace_bytes, void* stream);

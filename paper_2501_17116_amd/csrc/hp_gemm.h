@@ -102,9 +102,9 @@ FP4_D HpTile hp_tile_at(const HpOperands& g) {
   return t;
 }
 
-// The sums of one tile.  smem is free of requests and of other waves' reads when it returns.
-template <class S, bool F16>
-FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, hp_f32x16 (&acc)[S::QI][S::PJ]) {
+// The sums of one tile.  smem is free of requests and of other waves' reads when it returns.  watch sees each slice's fragments.
+template <class S, bool F16, class Watch>
+FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, hp_f32x16 (&acc)[S::QI][S::PJ], Watch&& watch) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, h = lane >> 5;
   const int64_t P0 = (int64_t)tile.tp * S::BP, Q0 = (int64_t)tile.tq * S::BQ;
@@ -174,6 +174,7 @@ FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, 
       for (int i = 0; i < S::QI; ++i)
 #pragma unroll
         for (int j = 0; j < S::PJ; ++j) acc[i][j] = hp_mfma<F16>(fr[i], fl[j], acc[i][j]);
+      watch(fl, fr);
     }
     asm volatile("" ::: "memory");
   }

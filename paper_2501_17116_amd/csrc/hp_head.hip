@@ -43,8 +43,8 @@ struct HeadTile {
   const uint32_t* amax;      // ADD, OUT: of the operand under a power of two
   void* out;                 // OUT
   bool out_bf16;
-  uint32_t* clear;           // DZ: words that become 0
-  int clear_n;
+  uint32_t *amax_w, *amax_x; // DZ: largest magnitudes of w's piece and of c x, bits, 0 before; either may be NULL
+  const float* dloss;        // c
 };
 
 template <class S>
@@ -237,18 +237,85 @@ FP4_D void bf16_epilogue(const HeadTile& a, const HpTile& tile, const hp_f32x16 
   }
 }
 
+FP4_D float row_weight(const float* weight, const int64_t* targets, int64_t V, int64_t row) {
+  if (!weight) return 1.0f;
+  const int64_t t = targets[row];
+  return t >= 0 && t < V ? weight[row] : 0.0f;
+}
+FP4_D uint32_t pk_max_u16(uint32_t a, uint32_t b) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+// Largest magnitudes of both operands, x's under its rows' weights, from the fragments that pass anyway, in one tile of each column of tiles (w)
+// and of each row (x): along the diagonal, since such tiles take longer and an XCD has whole rows of tiles.  (In launches of their own they took 50 us
+// a piece of 134 MB.)  A maximum does not depend on the order of its atomics, of which there are few: they come one after another.
+template <class S>
+struct Largest {
+  bool of_w, of_x;
+  uint32_t w = 0, x[S::PJ];   // two bf16's magnitudes each
+  static FP4_D bool w_here(const HeadTile& a, const HpTile& tile) { return a.amax_w && tile.tq % a.g.tiles_p == tile.tp; }
+  static FP4_D bool x_here(const HeadTile& a, const HpTile& tile) { return a.amax_x && tile.tp % a.g.tiles_q == tile.tq; }
+  FP4_D Largest(const HeadTile& a, const HpTile& tile) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    of_w = w_here(a, tile) && wave % S::WP == 0;
+    of_x = x_here(a, tile) && wave / S::WP == 0;
+#pragma unroll
+    for (int j = 0; j < S::PJ; ++j) x[j] = 0;
+  }
+  FP4_D void operator()(const u32x4 (&fl)[S::PJ], const u32x4 (&fr)[S::QI]) {
+    if (of_w) {
+#pragma unroll
+      for (int j = 0; j < S::QI; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w = pk_max_u16(w, fr[j][i] & 0x7fff7fffu);
+    }
+    if (of_x) {
+#pragma unroll
+      for (int j = 0; j < S::PJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[j] = pk_max_u16(x[j], fl[j][i] & 0x7fff7fffu);
+    }
+  }
+  static FP4_D uint32_t wider(uint32_t two) { return max(two << 16, two & 0xffff0000u); }
+  static FP4_D void leave(uint32_t best, uint32_t* to) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o));
+    if ((threadIdx.x & 63) == 0 && best) atomicMax(to, best);
+  }
+  FP4_D void leave(const HeadTile& a, const HpTile& tile) const {
+    if (of_w) leave(wider(w), a.amax_w);
+    if (of_x) {
+      const int wave_p = (threadIdx.x >> 6) % S::WP, l32 = threadIdx.x & 31;
+      uint32_t best = 0;
+#pragma unroll
+      for (int j = 0; j < S::PJ; ++j) {   // rows behind the edge repeat the last one
+        const int64_t p = min((int64_t)tile.tp * S::BP + wave_p * (S::PJ * 32) + j * 32 + l32, a.g.P - 1);
+        best = max(best, f2u(u2f(wider(x[j])) * fabsf(row_weight(a.dloss, a.targets, a.V, p))));
+      }
+      leave(best, a.amax_x);
+    }
+  }
+};
+
 template <class S, int EPI>
 __global__ __launch_bounds__(S::WAVES * 64) void head_tile_kernel(HeadTile a) {
   __shared__ __attribute__((aligned(16))) uint8_t smem[S::SMEM];
   hp_f32x16 acc[S::QI][S::PJ];
   const HpTile tile = hp_tile_at(a.g);
-  hp_tile_sums<S, EPI == EPI_ADD || EPI == EPI_OUT>(a.g, tile, smem, acc);
-  if constexpr (EPI == EPI_STATS) stats_epilogue<S>(a, tile, smem, acc);
   if constexpr (EPI == EPI_DZ) {
-    dz_epilogue<S>(a, tile, acc);
-    if (blockIdx.x == 0)
-      for (int i = threadIdx.x; i < a.clear_n; i += S::WAVES * 64) a.clear[i] = 0;
+    if (Largest<S>::w_here(a, tile) || Largest<S>::x_here(a, tile)) {   // the others' loop stays free of branches
+      Largest<S> largest(a, tile);
+      hp_tile_sums<S, false>(a.g, tile, smem, acc, largest);
+      largest.leave(a, tile);
+    } else {
+      hp_tile_sums<S, false>(a.g, tile, smem, acc, [](const auto&, const auto&) {});
+    }
+  } else {
+    hp_tile_sums<S, EPI != EPI_STATS>(a.g, tile, smem, acc, [](const auto&, const auto&) {});
   }
+  if constexpr (EPI == EPI_STATS) stats_epilogue<S>(a, tile, smem, acc);
+  if constexpr (EPI == EPI_DZ) dz_epilogue<S>(a, tile, acc);
   if constexpr (EPI == EPI_ADD) f32_epilogue<S>(a, tile, acc, a.sums + (int64_t)tile.split * a.g.P * a.g.Q, a.g.Q, scale_of(*a.amax, true) / DZ_SCALE);
   if constexpr (EPI == EPI_OUT) {
     const float factor = scale_of(*a.amax, true) / DZ_SCALE;
@@ -302,12 +369,6 @@ __global__ __launch_bounds__(256) void clear_words_kernel(uint32_t* x, int n) {
   for (int i = threadIdx.x; i < n; i += 256) x[i] = 0;
 }
 
-FP4_D float row_weight(const float* weight, const int64_t* targets, int64_t V, int64_t row) {
-  if (!weight) return 1.0f;
-  const int64_t t = targets[row];
-  return t >= 0 && t < V ? weight[row] : 0.0f;
-}
-
 // A matrix that is transposed into fp16 under a power of two: bf16 x [rows x cols], cols a multiple of 8, rows under a weight of their own where there
 // are any -> out [cols x pitch], pitch a multiple of 64, zeros from rows on.
 struct Across {
@@ -315,44 +376,12 @@ struct Across {
   int64_t rows, cols, ld;
   uint16_t* out;
   int64_t pitch;
-  uint32_t* amax;            // bits of the largest magnitude, 0 before
+  const uint32_t* amax;      // bits of the largest magnitude
   const float* weight;
   const int64_t* targets;
   int64_t V;
 };
 struct AcrossBoth { Across m[2]; int groups; };   // workgroups of the first
-
-// Its largest magnitude.  A maximum does not depend on the order of its atomics, of which there are few: they come one after another.  A wave a
-// row, eight pieces of it on their way together.
-__global__ __launch_bounds__(1024) void head_amax_kernel(AcrossBoth both) {
-  constexpr int AT_ONCE = 8;
-  __shared__ uint32_t lds[16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const bool second = (int)blockIdx.x >= both.groups;
-  const Across& a = both.m[second];
-  const int group = second ? blockIdx.x - both.groups : blockIdx.x, groups = second ? gridDim.x - both.groups : both.groups;
-  uint32_t best = 0;
-  for (int64_t r = (int64_t)group * 16 + wave; r < a.rows; r += (int64_t)groups * 16) {
-    uint32_t m = 0;
-    for (int64_t c0 = (int64_t)lane * 8; c0 < a.cols + lane * 8; c0 += 512 * AT_ONCE) {
-      u32x4 w[AT_ONCE];
-#pragma unroll
-      for (int k = 0; k < AT_ONCE; ++k) w[k] = *reinterpret_cast<const u32x4*>(a.x + r * a.ld + min(c0 + 512 * k, a.cols - 8));   // the last piece may count again
-#pragma unroll
-      for (int k = 0; k < AT_ONCE; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m = max(m, max(w[k][i] << 16 & 0x7fffffffu, w[k][i] & 0x7fff0000u));
-    }
-    best = max(best, f2u(u2f(m) * fabsf(row_weight(a.weight, a.targets, a.V, r))));
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o));
-  if (lane == 0) lds[wave] = best;
-  __syncthreads();
-  if (threadIdx.x) return;
-  for (int i = 1; i < 16; ++i) best = max(best, lds[i]);
-  if (best) atomicMax(a.amax, best);
-}
 
 // The transpose, 64 x 64 a workgroup, through LDS.
 __global__ __launch_bounds__(256) void head_across_kernel(AcrossBoth both) {
@@ -398,7 +427,6 @@ struct FewDx {
   float* sums;               // [splits][M x D]
   int64_t M, D, ld, ldw, rows;   // rows: of w, dz has zeros behind them
   int64_t share;             // rows of a split, a multiple of 64
-  bool add;                  // to what is there
 };
 template <int PB>
 __global__ __launch_bounds__(256, PB == 1 ? 2 : 1) void head_dx_few_kernel(FewDx a) {
@@ -475,9 +503,7 @@ __global__ __launch_bounds__(256, PB == 1 ? 2 : 1) void head_dx_few_kernel(FewDx
   for (int i = threadIdx.x; i < PB * 32 * 64; i += 256) {
     const int64_t m = m0 + i / 64, d = d0 + i % 64 * 4;
     if (m >= a.M || d >= a.D) continue;
-    f32x4* const o = reinterpret_cast<f32x4*>(out + m * a.D + d);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(&lds[i / 64][i % 64 * 4]) * (1.0f / DZ_SCALE);
-    *o = a.add ? *o + x : x;
+    *reinterpret_cast<f32x4*>(out + m * a.D + d) = *reinterpret_cast<const f32x4*>(&lds[i / 64][i % 64 * 4]) * (1.0f / DZ_SCALE);
   }
 }
 
@@ -487,17 +513,19 @@ __global__ __launch_bounds__(256) void head_dx_kernel(const float* sums, int spl
   constexpr int AT_ONCE = 8;
   const int64_t n = D / 4;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * n; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / n, c = i % n * 4;
+    const int64_t row = M * n >> 32 ? i / n : (uint32_t)i / (uint32_t)n, c = (i - row * n) * 4;
     const float f = row_weight(dloss, targets, V, row);
     f32x4 s = {0, 0, 0, 0};
-    for (int k0 = 0; k0 < splits; k0 += AT_ONCE) {
+    const auto at = [&](int k) { return *reinterpret_cast<const f32x4*>(sums + ((int64_t)k * M + row) * D + c); };
+    int k0 = 0;
+    for (; k0 + AT_ONCE <= splits; k0 += AT_ONCE) {
       f32x4 r[AT_ONCE];
 #pragma unroll
-      for (int k = 0; k < AT_ONCE; ++k) r[k] = *reinterpret_cast<const f32x4*>(sums + ((int64_t)min(k0 + k, splits - 1) * M + row) * D + c);
+      for (int k = 0; k < AT_ONCE; ++k) r[k] = at(k0 + k);
 #pragma unroll
-      for (int k = 0; k < AT_ONCE; ++k)
-        if (k0 + k < splits) s += r[k];
+      for (int k = 0; k < AT_ONCE; ++k) s += r[k];
     }
+    for (; k0 < splits; ++k0) s += at(k0);
     s = f == 0.0f ? f32x4{0, 0, 0, 0} : s * f;
     *reinterpret_cast<u32x2*>(dx + row * ld + c) = u32x2{hp_pack_bf16(s.x, s.y), hp_pack_bf16(s.z, s.w)};
   }
@@ -559,11 +587,13 @@ template <int EPI>
 int launch(HeadTile& a, hipStream_t s) { return launch<EPI>(a, cut_of(a.g.P, a.g.Q, a.g.K, 1), s); }
 
 // ---- sizes of the pieces and of what they need -----------------------------------------------------------------------------------
-constexpr int64_t PIECE = int64_t{1} << 27;   // elements of dz, and of w's transposed piece
+constexpr int64_t PIECE = int64_t{1} << 28;   // elements of dz, and of w's transposed piece
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // Few tokens: their dx needs no transposed piece of w (both gradients, 4096 into 32000: 1 token 364 us with it, 213 without, 120 tokens 404 / 304).
-bool few_tokens(int64_t M) { return M <= 128; }
+constexpr int64_t FEW_TOKENS = 128;
+static_assert(FEW_TOKENS * HP_MAX_DIM <= PIECE, "their dz is one piece");
+bool few_tokens(int64_t M) { return M <= FEW_TOKENS; }
 
 // Rows of w a piece: as many as the room allows, the pieces alike.
 int64_t piece_rows(int64_t M, int64_t D, int64_t V) {
@@ -633,19 +663,14 @@ int hp_launch_head_bwd(const uint16_t* x, const uint16_t* w, const int64_t* targ
   float* const sums = (float*)take(sums_room(M, D));
   // One or two matrices' transposes under the powers of two that suit them.
   const auto across = [&](const Across& first, const Across* second) {
-    const auto rows_groups = [](const Across& a) { return (int)std::min<int64_t>((a.rows + 15) / 16, 512); };
     const auto tiles = [](const Across& a) { return (int)(a.pitch / 64 * ((a.cols + 63) / 64)); };
-    AcrossBoth both = {{first, second ? *second : first}, rows_groups(first)};
-    head_amax_kernel<<<both.groups + (second ? rows_groups(*second) : 0), 1024, 0, s>>>(both);
-    both.groups = tiles(first);
+    const AcrossBoth both = {{first, second ? *second : first}, tiles(first)};
     head_across_kernel<<<both.groups + (second ? tiles(*second) : 0), 256, 0, s>>>(both);
   };
   int rc = FP4_OK;
   if (M == 0 && !dw) return FP4_OK;
-  if (M == 0) {
-    clear_words_kernel<<<1, 256, 0, s>>>(amax, pieces + 1);
-    FP4_CHECK_LAUNCH();
-  }
+  clear_words_kernel<<<1, 256, 0, s>>>(amax, pieces + 1);
+  FP4_CHECK_LAUNCH();
   const Across cx = {x, M, D, ldx, x_across, Mp, &amax[pieces], dloss, targets, V};
   const bool few = few_tokens(M);
   Cut dx_cut = cut_of(M, D, up(piece, 64), most_splits(M, D));   // one for all pieces: they add to the same sums
@@ -663,21 +688,21 @@ int hp_launch_head_bwd(const uint16_t* x, const uint16_t* w, const int64_t* targ
       t.ld = ld;
       t.dz_across = dw ? dz_across : nullptr;
       t.ld_across = Mp;
-      t.clear = amax;
-      t.clear_n = i == 0 ? pieces + 1 : 0;
+      t.amax_w = dx && !few ? &amax[i] : nullptr;
+      t.amax_x = dw && i == 0 ? &amax[pieces] : nullptr;
+      t.dloss = dloss;
       if ((rc = launch<EPI_DZ>(t, s))) return rc;
       const Across piece_of_w = {wp, rows, D, ldw, w_across, ld, &amax[i], nullptr, nullptr, 0};
       if (dx && !few) across(piece_of_w, dw && i == 0 ? &cx : nullptr);
       else if (dw && i == 0) across(cx, nullptr);
     }
-    if (dx && few && M > 0) {
+    if (dx && few && M > 0) {   // all of w is one piece
       const int slices = (int)((D + 255) / 256), blocks = M <= 64 ? 1 : 2;
       const int64_t most = std::min<int64_t>(most_splits(M, D), std::max(1, 512 / (slices * blocks)));
-      const int64_t share = up((up(piece, 64) + most - 1) / most, 64);
-      const int splits = (int)((ld + share - 1) / share);
-      if (i == 0) dx_cut.splits = splits;   // a later piece has as many at most
-      const FewDx f = {dz, wp, sums, M, D, ld, ldw, rows, share, i > 0};
-      const dim3 grid((unsigned)slices, (unsigned)splits, (unsigned)blocks);
+      const int64_t share = up((ld + most - 1) / most, 64);
+      dx_cut.splits = (int)((ld + share - 1) / share);
+      const FewDx f = {dz, wp, sums, M, D, ld, ldw, rows, share};
+      const dim3 grid((unsigned)slices, (unsigned)dx_cut.splits, (unsigned)blocks);
       if (M <= 32) head_dx_few_kernel<1><<<grid, 256, 0, s>>>(f);
       else head_dx_few_kernel<2><<<grid, 256, 0, s>>>(f);
       FP4_CHECK_LAUNCH();
