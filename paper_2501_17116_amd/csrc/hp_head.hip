@@ -383,39 +383,30 @@ struct Across {
 };
 struct AcrossBoth { Across m[2]; int groups; };   // workgroups of the first
 
-// The transpose, 64 x 64 a workgroup, through LDS.
+// 64 x 64 a wave: a lane turns eight rows of eight columns in its registers, of which both its loads and its stores are whole 128-byte lines of eight
+// lanes each.
 __global__ __launch_bounds__(256) void head_across_kernel(AcrossBoth both) {
-  __shared__ uint16_t lds[64][66];
   const bool second = (int)blockIdx.x >= both.groups;
   const Across& a = both.m[second];
-  const int group = second ? blockIdx.x - both.groups : blockIdx.x, lines = (int)(a.pitch / 64);
-  const int64_t r0 = (int64_t)(group % lines) * 64, c0 = (int64_t)(group / lines) * 64;
-  const int chunk = threadIdx.x & 7;
+  const int64_t lines = a.pitch / 64, tile = (int64_t)(second ? blockIdx.x - both.groups : blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t r0 = tile % lines * 64 + (threadIdx.x >> 3 & 7) * 8, c0 = tile / lines * 64 + (threadIdx.x & 7) * 8;
+  if (c0 >= a.cols) return;
   const float scale = scale_of(*a.amax, false);
+  u32x4 w[8];
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int r = half * 32 + (threadIdx.x >> 3);
-    const int64_t row = r0 + r, col = c0 + chunk * 8;
-    u32x4 w = {0, 0, 0, 0};
-    if (row < a.rows && col < a.cols) {
-      w = *reinterpret_cast<const u32x4*>(a.x + row * a.ld + col);
-      const float f = row_weight(a.weight, a.targets, a.V, row);
+  for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const u32x4*>(a.x + min(r0 + k, a.rows - 1) * a.ld + c0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = pack_f16(u2f(w[i] << 16) * f * scale, u2f(w[i] & 0xffff0000u) * f * scale);
-    }
+  for (int k = 0; k < 8; ++k) {
+    const float f = r0 + k < a.rows ? row_weight(a.weight, a.targets, a.V, r0 + k) : 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(&lds[r][chunk * 8 + 2 * i]) = w[i];
+    for (int i = 0; i < 4; ++i) w[k][i] = r0 + k < a.rows ? pack_f16(u2f(w[k][i] << 16) * f * scale, u2f(w[k][i] & 0xffff0000u) * f * scale) : 0u;
   }
-  __syncthreads();
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int c = half * 32 + (threadIdx.x >> 3);
-    const int64_t col = c0 + c, row = r0 + chunk * 8;
-    if (col >= a.cols) continue;
-    u32x4 w;
+  for (int c = 0; c < 8; ++c) {
+    u32x4 t;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = lds[chunk * 8 + 2 * i][c] | (uint32_t)lds[chunk * 8 + 2 * i + 1][c] << 16;
-    *reinterpret_cast<u32x4*>(a.out + col * a.pitch + row) = w;
+    for (int k = 0; k < 4; ++k) t[k] = __builtin_amdgcn_perm(w[2 * k + 1][c / 2], w[2 * k][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+    *reinterpret_cast<u32x4*>(a.out + (c0 + c) * a.pitch + r0) = t;
   }
 }
 
@@ -663,7 +654,7 @@ int hp_launch_head_bwd(const uint16_t* x, const uint16_t* w, const int64_t* targ
   float* const sums = (float*)take(sums_room(M, D));
   // One or two matrices' transposes under the powers of two that suit them.
   const auto across = [&](const Across& first, const Across* second) {
-    const auto tiles = [](const Across& a) { return (int)(a.pitch / 64 * ((a.cols + 63) / 64)); };
+    const auto tiles = [](const Across& a) { return (int)((a.pitch / 64 * ((a.cols + 63) / 64) + 3) / 4); };
     const AcrossBoth both = {{first, second ? *second : first}, tiles(first)};
     head_across_kernel<<<both.groups + (second ? tiles(*second) : 0), 256, 0, s>>>(both);
   };
