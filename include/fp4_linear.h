@@ -420,9 +420,9 @@ int hp_head_fwd(const void* x, const void* w, const int64_t* targets, fp4_dtype 
 
 /* Gradients under dloss [M], each token's loss's; a target outside [0, V) leaves its token without one, whatever its dloss is.
  *   dz[t, v] = dloss[t] (exp(z[t, v] - lse[t]) - [v = targets[t]]);   dx = dz w (bf16),   dw = dz^T x (dw_dt; fp32: accumulate != 0 adds)
- * Either may be NULL, not both.  The products' operands are rounded to 11 bits (fp16 under powers of two: exact for w and for dloss x but
- * for its product's rounding), sums are fp32: dw in fp32 is as near as that.  A target's entry below 2^-40 of 1 and weights below 2^-39
- * of their largest are taken as 0.
+ * Either may be NULL, not both.  lse is the forward pass's over the same x and w.  dz and dloss x enter the products rounded to 11 bits (fp16 under
+ * powers of two, which hold w's bf16 as they are), sums are fp32: dw in fp32 is as near as that.  Elements of dz below 2^-40, and of w and dloss x below 2^-39 of
+ * their largest, count as 0.
  * Workspace: fp4_workspace_bytes(FP4_OP_HP_HEAD_BWD, M, D, V, dt); dz takes at most 2^28 fp16 elements and 256 a token of it,
  * twice; w's transposed piece as many. */
 int hp_head_bwd(const void* x, const void* w, const int64_t* targets, const float* lse, const float* dloss, fp4_dtype dt, int64_t M, int64_t D,

@@ -157,7 +157,7 @@ extern "C" int hp_head_bwd(const void* x, const void* w, const int64_t* targets,
                            void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_head(x, w, targets, dt, M, D, V, ldx, ldw);
   if (rc) return rc;
-  if (!dx && !dw) return FP4_ERR_NULL;
+  if (!dx && !dw && M > 0 && D > 0) return FP4_ERR_NULL;   // what is empty has no address
   if (M > 0 && (!lse || !dloss)) return FP4_ERR_NULL;
   if (!dtype_ok(dw_dt)) return FP4_ERR_DTYPE;
   if (dw && accumulate && dw_dt != FP4_F32) return FP4_ERR_ARG;

@@ -298,6 +298,11 @@ struct Largest {
   }
 };
 
+// A tile of logits or of a gradient product.  256 x 256, measured: 8192 x 32000 over 2048 (maxima and sums) 0.90 ms, 1.19e15 operations/s; 16384 x 4096 over 8192 (dw) 0.91 ms,
+// 1.21e15; dz's tiles end with 128 KB of stores twice, 1.1e15 over 4096, 0.65e15 over 1376.  Bound by power: the clock falls to 1.9 GHz, the matrix
+// cores are busy in 50 - 59 % of the cycles, LDS conflicts are none.
+// Tried: waves of 128 x 128 sums, one a SIMD, in two stages of 64 or five of 32 elements, reads and requests between the matrix instructions: fewer
+// idle cycles at a lower clock, 945 against 922 us for 16384 x 4096 over 8192, and 1217 where lines lie 32 KiB apart.
 template <class S, int EPI>
 __global__ __launch_bounds__(S::WAVES * 64) void head_tile_kernel(HeadTile a) {
   __shared__ __attribute__((aligned(16))) uint8_t smem[S::SMEM];
@@ -383,7 +388,7 @@ struct Across {
 };
 struct AcrossBoth { Across m[2]; int groups; };   // workgroups of the first
 
-// 64 x 64 a wave: a lane turns eight rows of eight columns in its registers, of which both its loads and its stores are whole 128-byte lines of eight
+// 134 MB in 36 - 54 us, as what the launch before wrote still leaves the last-level cache.  64 x 64 a wave: a lane turns eight rows of eight columns in its registers, of which both its loads and its stores are whole 128-byte lines of eight
 // lanes each.
 __global__ __launch_bounds__(256) void head_across_kernel(AcrossBoth both) {
   const bool second = (int)blockIdx.x >= both.groups;
@@ -412,7 +417,8 @@ __global__ __launch_bounds__(256) void head_across_kernel(AcrossBoth both) {
 
 // dx's sums for few tokens, w read once as it lies: 256 columns a workgroup, whose four waves share a part of the vocabulary.  A lane loads eight
 // rows of eight columns and turns them in its registers into eight operands, each eight rows of one column (matrix instruction f
-// takes columns 8 n + f), so that nothing passes through LDS.  w stays bf16; dz's 11 bits are the sum of two bf16, a product each: it is w's bytes that bound this.
+// takes columns 8 n + f), so that nothing passes through LDS.  w stays bf16; dz's 11 bits are the sum of two bf16, a product each: it is w's bytes that bound this
+// (131072 x 4096 for one token 175 us, 6.1 TB/s).
 struct FewDx {
   const uint16_t *dz, *w;
   float* sums;               // [splits][M x D]
@@ -522,6 +528,12 @@ __global__ __launch_bounds__(256) void head_dx_kernel(const float* sums, int spl
   }
 }
 
+constexpr int64_t PIECE = int64_t{1} << 28;   // elements of dz, and of w's transposed piece
+// Few tokens: their dx needs no transposed piece of w (both gradients, 4096 into 32000: 1 token 364 us with it, 213 without, 120 tokens 404 / 304).
+constexpr int64_t FEW_TOKENS = 128;
+static_assert(FEW_TOKENS * HP_MAX_DIM <= PIECE, "their dz is one piece");
+bool few_tokens(int64_t M) { return M <= FEW_TOKENS; }
+
 // ---- which tiles ---------------------------------------------------------------------------------------------------------------
 using Large = HpShape<2, 4, 4, 2, 2>;    // 256 x 256
 using Middle = HpShape<2, 2, 2, 2, 2>;   // 128 x 128, two a CU
@@ -540,7 +552,7 @@ Cut cut_of(int64_t P, int64_t Q, int64_t K, int most) {
   const int64_t steps = (K + 63) / 64;
   const auto tiles = [&](int64_t bp, int64_t bq) { return ((P + bp - 1) / bp) * ((Q + bq - 1) / bq); };
   most = (int)std::max<int64_t>(1, std::min<int64_t>(most, steps / 4));
-  if (P <= 128) return {P <= 32 ? TILE_FEWEST : TILE_FEW, (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / std::max<int64_t>(1, tiles(P <= 32 ? 32 : 64, 128))))};
+  if (P <= FEW_TOKENS) return {P <= 32 ? TILE_FEWEST : TILE_FEW, 1};
   Cut best = {TILE_LARGE, 1};
   int64_t least = INT64_MAX;
   for (int s = 1; s <= most; ++s) {
@@ -567,24 +579,18 @@ int launch(HeadTile& a, const Cut& cut, hipStream_t s) {
   const int64_t steps = (a.g.K + 63) / 64;
   a.g.splits = cut.splits;
   a.g.split_steps = (int)((steps + cut.splits - 1) / cut.splits);
-  switch (cut.tile) {
-    case TILE_LARGE: return launch<Large, EPI>(a, s);
-    case TILE_MIDDLE: return launch<Middle, EPI>(a, s);
-    case TILE_FEW: return launch<Few, EPI>(a, s);
-    default: return launch<Fewest, EPI>(a, s);
+  if (cut.tile == TILE_LARGE) return launch<Large, EPI>(a, s);
+  if constexpr (EPI != EPI_ADD) {   // few tokens' dx is another kernel's
+    if (cut.tile == TILE_FEW) return launch<Few, EPI>(a, s);
+    if (cut.tile == TILE_FEWEST) return launch<Fewest, EPI>(a, s);
   }
+  return launch<Middle, EPI>(a, s);
 }
 template <int EPI>
 int launch(HeadTile& a, hipStream_t s) { return launch<EPI>(a, cut_of(a.g.P, a.g.Q, a.g.K, 1), s); }
 
 // ---- sizes of the pieces and of what they need -----------------------------------------------------------------------------------
-constexpr int64_t PIECE = int64_t{1} << 28;   // elements of dz, and of w's transposed piece
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
-
-// Few tokens: their dx needs no transposed piece of w (both gradients, 4096 into 32000: 1 token 364 us with it, 213 without, 120 tokens 404 / 304).
-constexpr int64_t FEW_TOKENS = 128;
-static_assert(FEW_TOKENS * HP_MAX_DIM <= PIECE, "their dz is one piece");
-bool few_tokens(int64_t M) { return M <= FEW_TOKENS; }
 
 // Rows of w a piece: as many as the room allows, the pieces alike.
 int64_t piece_rows(int64_t M, int64_t D, int64_t V) {

@@ -53,7 +53,7 @@ struct RowSums {
   }
 };
 
-// A workgroup a row: going from row to row, the next one's pieces requested ahead, takes longer here (16384 x 4096, gated: 125 against 95 us).
+// A workgroup a row (16384 x 4096, both norms and a gate: 97 us, 5.5 TB/s).  Going from row to row, the next one's pieces requested ahead, takes longer here: 125.
 template <class T, int CH>
 __global__ __launch_bounds__(1024) void norm_fwd_kernel(NormFwd a) {
   __shared__ float lds[2][16];
@@ -125,7 +125,8 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(NormFwd a) {
   }
 }
 
-// A workgroup goes from row to row and keeps the sums of its rows; AHEAD: the next row's pieces are requested before the present one's are used.
+// A workgroup goes from row to row and keeps the sums of its rows; AHEAD: the next row's pieces are requested before the present one's are used.  (8192 x
+// 5120: 102 us, 4.9 TB/s; with two pieces a thread, whose operands and sums spill, 1014.)
 template <class T, int CH, int THREADS, bool AHEAD>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormBwd a) {
   __shared__ float lds[2][16];

@@ -169,6 +169,49 @@ def test_no_tokens():
     dw.fill_(2.0)
     b.hp_head_bwd(x, w, t, lse, e, dw=dw, accumulate=True)
     assert bool((dw == 2).all())
+    assert b.hp_head_bwd(x, w, t, lse, e, want_dw=False)[0].shape == (0, 64)
+
+
+def test_no_channels():
+    """All logits 0."""
+    x, w = torch.empty(5, 0, dtype=torch.bfloat16, device="cuda"), torch.empty(700, 0, dtype=torch.bfloat16, device="cuda")
+    t = torch.tensor([0, 699, -1, 700, 3], device="cuda")
+    loss, lse = b.hp_head_fwd(x, w, t)
+    plain.close(lse, torch.full((5,), 700.0, dtype=torch.float64, device="cuda").log(), torch.full((5,), 260 * plain.U, device="cuda"))
+    assert loss[2] == loss[3] == 0 and torch.equal(loss[[0, 1, 4]], lse[[0, 1, 4]])
+    dx, dw = b.hp_head_bwd(x, w, t, lse, torch.ones(5, device="cuda"))
+    assert dx.shape == (5, 0) and dw.shape == (700, 0)
+
+
+def test_weights_past_2_to_32_bytes():
+    """A vocabulary whose weights, and their gradient, end beyond: tokens that aim at its ends, the rest of it empty."""
+    M, D, V = 3, 8192, 270_000
+    w = torch.zeros(V, D, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(3)
+    for v in (0, V - 2, V - 1):
+        w[v] = (torch.randn(D, generator=g) * 0.05).bfloat16().cuda()
+    x = torch.randn(M, D, generator=g).bfloat16().cuda()
+    t = torch.tensor([0, V - 1, V - 2], device="cuda")
+    dloss = torch.ones(M, device="cuda")
+    loss, lse = b.hp_head_fwd(x, w, t)
+    dx, dw = b.hp_head_bwd(x, w, t, lse, dloss, dw_dtype=torch.bfloat16)
+    # the rows in use, and all the others as one whose logit is 0
+    some = torch.cat([w[[0, V - 2, V - 1]].double(), torch.zeros(1, D, dtype=torch.float64, device="cuda")])
+    z = x.double() @ some.t().contiguous()
+    z[:, 3] = torch.log(torch.tensor(V - 3.0, dtype=torch.float64))
+    want = torch.logsumexp(z, 1)
+    off = (D + 1) * plain.U * (x.double().abs() @ some.abs().t().contiguous()).amax(1) + 260 * plain.U + (z.abs().amax(1) + want.abs()) * 4 * plain.U
+    plain.close(lse, want, off, "lse")
+    p = torch.exp(z - want[:, None])
+    p[[0, 1, 2], [0, 2, 1]] -= 1.0
+    rows = dw[[0, V - 2, V - 1]].double()
+    ref = p[:, :3].t().contiguous() @ x.double()
+    # dz and x to 11 bits each, the output to 8; the exponentials by the logits' error
+    tol = (2.0 ** -8 + 2.0 ** -10) * (p[:, :3].abs().t().contiguous() @ x.double().abs()) + (torch.exp(z - want[:, None])[:, :3] * 3 * off[:, None]).t().contiguous() @ x.double().abs()
+    plain.close(rows, ref, tol, "dw")
+    few = dw[1000:1003].double()
+    same = ((1.0 / torch.exp(want)) @ x.double()).expand(3, D)
+    plain.close(few, same, (2.0 ** -8 + 2.0 ** -10 + 4 * float(off.max())) * ((1.0 / torch.exp(want)) @ x.double().abs()).expand(3, D) + 2.0 ** -40 * x.double().abs().sum(0), "empty rows' dw")
 
 
 def test_graphs_with_workspaces_of_their_own():

@@ -131,7 +131,6 @@ def test_padding_is_left_alone_and_in_place():
     h, y = b.hp_norm_fwd(norm, x, blk, h=wide[:, :D], y=y_wide[:, :D])
     assert torch.equal(h, ref_h) and torch.equal(y, ref_y)
     assert bool((wide[:, D:] == 7).all()) and bool((y_wide[:, D:] == 7).all())
-    stream = x.clone(memory_format=torch.preserve_format) if x.is_contiguous() else plain.matrix(x)
     stream = plain.matrix(x)
     h2, y2 = b.hp_norm_fwd(norm, stream, blk, h=stream)
     assert h2.data_ptr() == stream.data_ptr() and torch.equal(stream, ref_h) and torch.equal(y2, ref_y)
@@ -146,6 +145,23 @@ def test_padding_is_left_alone_and_in_place():
     own = b.HpNormGrads(dh, dy, *(torch.zeros(D, device="cuda") for _ in range(3)))
     got = b.hp_norm_bwd(norm, saved, ref_h, dy, dh, blk, into=own)
     assert all(torch.equal(a, c) for a, c in zip(ref, got))
+
+
+@pytest.mark.parametrize("D", [648, 5000, 7000, 9001])
+def test_gradients_in_place(D):
+    """dx and dblock over dh and dy either way round, at the widths whose kernels hold a row, hold it in part, or read it again."""
+    M = 40
+    x, blk, wb, wa, gate, normal = inputs(M, D, torch.bfloat16)
+    norm = b.HpNorm(wb, wa, gate)
+    saved = b.hp_norm_saved(norm, M)
+    h, _ = b.hp_norm_fwd(norm, x, blk, saved)
+    dy, dh = normal(M, D), normal(M, D)
+    ref = b.hp_norm_bwd(norm, saved, h, plain.matrix(dy), plain.matrix(dh), blk)
+    for turned in (False, True):
+        a, c = plain.matrix(dy), plain.matrix(dh)
+        into = b.HpNormGrads(*((a, c) if turned else (c, a)), *(torch.empty(D, device="cuda") for _ in range(3)))
+        got = b.hp_norm_bwd(norm, saved, h, a, c, blk, into=into)
+        assert all(torch.equal(g, r) for g, r in zip(got, ref))
 
 
 def test_accumulates_and_repeats_its_bits():
