@@ -4,9 +4,9 @@
 //
 // fp32 sums of exact products.  What becomes of a tile is its epilogue's (hp_head.hip).
 //
-// v_mfma_f32_32x32x16: lane (l32, h) brings elements 8 h .. 8 h + 7 of row l32 of either operand.  A step is 64 elements, 128 bytes, of a row, of
-// which lane half h takes bytes 64 h .. 64 h + 63, sixteen a slice (it does not matter which elements of a row meet, only that
-// those of both operands do).  Result: lane (l32, h) holds, of row l32 of L, columns 8 b + 4 h + e of the block, in register 4 b + e.
+// v_mfma_f32_16x16x32: lane (l16, g) brings elements 8 g .. 8 g + 7 of row l16 of either operand.  A step is 64 elements, 128 bytes, of a row, in two
+// slices.  Result: lane (l16, g) holds, of row l16 of L, columns 4 g + e of the block, in register e.  (The 32 x 32 x 16 instruction reads half of the
+// operands for the same products, and yet draws more power, which is what bounds large products: 16384 x 4096 over 8192 895 against 829 us.)
 //
 // Operands come into LDS by direct loads, a ring of NST steps.  A row takes 128 bytes of a stage, its 16-byte chunk c in slot c ^ ((row >> 1) & 7),
 // so that sixteen rows reading one chunk touch sixteen different bank groups.  Chunks behind K arrive as zeros, rows behind the matrix's edge repeat its last one.
@@ -34,11 +34,11 @@ FP4_D void hp_static_for_impl(F&& f, std::integer_sequence<int, I...>) { (f(std:
 template <int N, class F>
 FP4_D void hp_static_for(F&& f) { hp_static_for_impl<N>(f, std::make_integer_sequence<int, N>{}); }
 
-// WP x WQ waves of PJ x QI blocks of 32 x 32.
+// WP x WQ waves of PJ x QI blocks of 16 x 16, a ring of NST stages.
 template <int WP_, int WQ_, int PJ_, int QI_, int NST_>
 struct HpShape {
   static constexpr int WP = WP_, WQ = WQ_, PJ = PJ_, QI = QI_, NST = NST_;
-  static constexpr int WAVES = WP * WQ, BP = WP * PJ * 32, BQ = WQ * QI * 32;
+  static constexpr int WAVES = WP * WQ, BP = WP * PJ * 16, BQ = WQ * QI * 16;
   static constexpr int LDL = BP / 8 / WAVES, LDR = BQ / 8 / WAVES, LOADS = LDL + LDR;   // of 64 chunks of 16 bytes, a wave and step
   static constexpr int OP_L = BP * 128, STAGE = (BP + BQ) * 128, SMEM = NST * STAGE;
   static_assert(LDL * 8 * WAVES == BP && LDR * 8 * WAVES == BQ, "rows a load");
@@ -66,9 +66,12 @@ FP4_D void hp_wait() {
   __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
 }
 template <bool F16>
-FP4_D hp_f32x16 hp_mfma(const u32x4& r, const u32x4& l, const hp_f32x16& c) {
-  if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(hp_f16x8, r), __builtin_bit_cast(hp_f16x8, l), c, 0, 0, 0);
-  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(hp_bf16x8, r), __builtin_bit_cast(hp_bf16x8, l), c, 0, 0, 0);
+FP4_D f32x4 hp_mfma(const u32x4& r, const u32x4& l, const f32x4& c) {
+  if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(hp_f16x8, r), __builtin_bit_cast(hp_f16x8, l), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(hp_bf16x8, r), __builtin_bit_cast(hp_bf16x8, l), c, 0, 0, 0);
+}
+FP4_D hp_f32x16 hp_mfma32(const u32x4& r, const u32x4& l, const hp_f32x16& c) {   // bf16, 32 x 32 x 16
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(hp_bf16x8, r), __builtin_bit_cast(hp_bf16x8, l), c, 0, 0, 0);
 }
 // Between the lanes' four groups of sixteen: the second and fourth group of a with the first and third of b; the upper two groups of a with
 // the lower two of b.
@@ -84,6 +87,11 @@ FP4_D float hp_other_half(float v) {   // of the lane 32 further
   uint32_t a = f2u(v), b = a;
   hp_swap32(a, b);
   return u2f((threadIdx.x & 32) ? a : b);
+}
+FP4_D float hp_other_sixteen(float v) {   // of the lane 16 further in its half
+  uint32_t a = f2u(v), b = a;
+  hp_swap16(a, b);
+  return u2f((threadIdx.x & 16) ? a : b);
 }
 
 // A workgroup's tile and its part of the contraction.  Workgroups go round the eight XCDs; each XCD takes a contiguous run of tiles, so
@@ -103,10 +111,12 @@ FP4_D HpTile hp_tile_at(const HpOperands& g) {
 }
 
 // The sums of one tile.  smem is free of requests and of other waves' reads when it returns.  watch sees each slice's fragments.
+// A slice's fragments are read while the matrix cores work on the slice before.  A step's barrier stands between its slices: by then every wave holds the
+// second slice's fragments, so that the stage is free for a later step, and the next step has landed, whose first fragments are read in the second slice's shadow.
 template <class S, bool F16, class Watch>
-FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, hp_f32x16 (&acc)[S::QI][S::PJ], Watch&& watch) {
+FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, f32x4 (&acc)[S::QI][S::PJ], Watch&& watch) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l32 = lane & 31, h = lane >> 5;
+  const int l16 = lane & 15, quarter = lane >> 4;
   const int64_t P0 = (int64_t)tile.tp * S::BP, Q0 = (int64_t)tile.tq * S::BQ;
   const int64_t rowL = g.ldL * 2, rowR = g.ldR * 2;
   const __amdgpu_buffer_rsrc_t rsrcL = hp_rsrc(g.L + P0 * g.ldL, min(g.P - P0, (int64_t)S::BP) * rowL);
@@ -143,40 +153,48 @@ FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, 
                   step * 128);
     }
   };
-  const int key = (l32 >> 1) & 7, wave_p = wave % S::WP, wave_q = wave / S::WP;
-  const int frag_l = (wave_p * (S::PJ * 32) + l32) * 128, frag_r = S::OP_L + (wave_q * (S::QI * 32) + l32) * 128;
+  const int key = (l16 >> 1) & 7, wave_p = wave % S::WP, wave_q = wave / S::WP;
+  const int at_l = (wave_p * (S::PJ * 16) + l16) * 128, at_r = S::OP_L + (wave_q * (S::QI * 16) + l16) * 128;
 #pragma unroll
   for (int i = 0; i < S::QI; ++i)
 #pragma unroll
-    for (int j = 0; j < S::PJ; ++j)
+    for (int j = 0; j < S::PJ; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+  if (T <= 0) return;
+  u32x4 fl[2][S::PJ], fr[2][S::QI];
+  const auto read = [&](int t, int s) {
+    const uint8_t* const stage = smem + t % S::NST * S::STAGE + ((4 * s + quarter) ^ key) * 16;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    for (int j = 0; j < S::QI; ++j) fr[s][j] = *reinterpret_cast<const u32x4*>(stage + at_r + j * 16 * 128);
 #pragma unroll
-  for (int t = 0; t < S::NST - 1; ++t)
+    for (int j = 0; j < S::PJ; ++j) fl[s][j] = *reinterpret_cast<const u32x4*>(stage + at_l + j * 16 * 128);
+  };
+  const auto multiply = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < S::QI; ++i)
+#pragma unroll
+      for (int j = 0; j < S::PJ; ++j) acc[i][j] = hp_mfma<F16>(fr[s][i], fl[s][j], acc[i][j]);
+    watch(fl[s], fr[s]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+#pragma unroll
+  for (int t = 0; t < S::NST; ++t)
     if (t < T) load_step(t);
+  if (T >= S::NST) hp_wait<(S::NST - 1) * S::LOADS>();
+  else hp_wait<0>();
+  __builtin_amdgcn_s_barrier();   // a bare one: a fence would wait for the other stages too
+  asm volatile("" ::: "memory");
+  read(0, 0);
   for (int t = 0; t < T; ++t) {
-    // Steps t + 1 .. t + NST - 2 may still be on their way; towards the end there are fewer, and then all have to have landed
-    if (t + S::NST - 2 < T) hp_wait<(S::NST - 2) * S::LOADS>();
+    read(t, 1);
+    multiply(0);
+    // Steps t + 2 .. t + NST - 1 may still be on their way; towards the end there are fewer, and then all have to have landed
+    if (t + S::NST - 1 < T) hp_wait<(S::NST - 2) * S::LOADS>();
     else hp_wait<0>();
-    __builtin_amdgcn_s_barrier();   // everyone's share of step t is there, and everyone is done with step t - 1
+    __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (t + S::NST - 1 < T) load_step(t + S::NST - 1);
-    const uint8_t* const stage = smem + t % S::NST * S::STAGE;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int slot = ((4 * h + s) ^ key) * 16;
-      u32x4 fl[S::PJ], fr[S::QI];
-#pragma unroll
-      for (int j = 0; j < S::QI; ++j) fr[j] = *reinterpret_cast<const u32x4*>(stage + frag_r + j * 32 * 128 + slot);
-#pragma unroll
-      for (int j = 0; j < S::PJ; ++j) fl[j] = *reinterpret_cast<const u32x4*>(stage + frag_l + j * 32 * 128 + slot);
-#pragma unroll
-      for (int i = 0; i < S::QI; ++i)
-#pragma unroll
-        for (int j = 0; j < S::PJ; ++j) acc[i][j] = hp_mfma<F16>(fr[i], fl[j], acc[i][j]);
-      watch(fl, fr);
-    }
-    asm volatile("" ::: "memory");
+    if (t + S::NST < T) load_step(t + S::NST);
+    if (t + 1 < T) read(t + 1, 0);
+    multiply(1);
   }
   __syncthreads();
 }

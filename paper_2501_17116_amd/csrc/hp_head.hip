@@ -48,48 +48,50 @@ struct HeadTile {
 };
 
 template <class S>
-FP4_D void stats_epilogue(const HeadTile& a, const HpTile& tile, uint8_t* smem, const hp_f32x16 (&acc)[S::QI][S::PJ]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
+FP4_D void stats_epilogue(const HeadTile& a, const HpTile& tile, uint8_t* smem, const f32x4 (&acc)[S::QI][S::PJ]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, quarter = lane >> 4;
   const int wave_p = wave % S::WP, wave_q = wave / S::WP;
-  const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 32), left = a.g.Q - q0;
+  const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 16), left = a.g.Q - q0;
   float2* const lds = reinterpret_cast<float2*>(smem);   // [WQ][BP]
 #pragma unroll
   for (int pj = 0; pj < S::PJ; ++pj) {
-    const int row = wave_p * (S::PJ * 32) + pj * 32 + l32;
+    const int row = wave_p * (S::PJ * 16) + pj * 16 + l16;
     const int64_t p = (int64_t)tile.tp * S::BP + row;
     const int64_t t = p < a.g.P ? a.targets[p] : -1;
     float m = -INFINITY;
-    if (left >= S::QI * 32) {
+    if (left >= S::QI * 16) {
 #pragma unroll
       for (int i = 0; i < S::QI; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[i][pj][v]);
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][pj][e]);
     } else {
 #pragma unroll
       for (int i = 0; i < S::QI; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) m = i * 32 + v / 4 * 8 + h * 4 + v % 4 < left ? fmaxf(m, acc[i][pj][v]) : m;
+        for (int e = 0; e < 4; ++e) m = i * 16 + quarter * 4 + e < left ? fmaxf(m, acc[i][pj][e]) : m;
     }
+    m = fmaxf(m, hp_other_sixteen(m));
     m = fmaxf(m, hp_other_half(m));
     const float ml = m == -INFINITY ? 0.0f : m * LOG2E;   // of nothing, or nothing finite
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < S::QI; ++i)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(acc[i][pj][v], LOG2E, -ml));
-        s += i * 32 + v / 4 * 8 + h * 4 + v % 4 < left ? e : 0.0f;
+      for (int e = 0; e < 4; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(acc[i][pj][e], LOG2E, -ml));
+        s += i * 16 + quarter * 4 + e < left ? x : 0.0f;
       }
+    s += hp_other_sixteen(s);
     s += hp_other_half(s);
-    if (h == 0) lds[wave_q * S::BP + row] = float2{m, s};
-    const bool here = t >= q0 && t < q0 + std::min<int64_t>(left, S::QI * 32);
+    if (quarter == 0) lds[wave_q * S::BP + row] = float2{m, s};
+    const bool here = t >= q0 && t < q0 + std::min<int64_t>(left, S::QI * 16);
     if (__ballot(here)) {
       const int at = (int)(t - q0);
 #pragma unroll
       for (int i = 0; i < S::QI; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (here && at == i * 32 + v / 4 * 8 + h * 4 + v % 4) a.target_z[p] = acc[i][pj][v];
+        for (int e = 0; e < 4; ++e)
+          if (here && at == i * 16 + quarter * 4 + e) a.target_z[p] = acc[i][pj][e];
     }
   }
   __syncthreads();
@@ -114,28 +116,35 @@ FP4_D uint32_t pack_f16(float a, float b) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// Sixteen sums of a 32 x 32 block as packed pairs -> two pieces of eight columns: of rows r16 and 16 + r16, columns 8 unit on, unit =
-// lane / 32 + 2 (lane / 16 % 2), so that a store is 64 bytes of a row.
-FP4_D void spread16(uint32_t (&d)[8]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    hp_swap32(d[i], d[2 + i]);
-    hp_swap32(d[4 + i], d[6 + i]);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) hp_swap16(d[i], d[4 + i]);
+// A row's four columns of one 16 x 16 block (a) and of the block beside it (b), two words each -> eight columns in a row: 8 unit on of the two blocks' 32,
+// unit = lane / 32 + 2 (lane / 16 % 2), so that a store is 64 bytes of a row.
+FP4_D u32x4 eight_columns(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
+  hp_swap16(a0, b0);
+  hp_swap16(a1, b1);
+  return u32x4{a0, a1, b0, b1};
+}
+FP4_D uint32_t from_lane(uint32_t x, std::integral_constant<int, 1>) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, true); }   // lane ^ 1
+FP4_D uint32_t from_lane(uint32_t x, std::integral_constant<int, 2>) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true); }   // lane ^ 2
+// Four lanes' rows of four 16-bit columns (two words) -> lane k of them has column k of the four rows.
+FP4_D u32x2 turn_four(uint32_t a, uint32_t b) {
+  const int lane = threadIdx.x & 3;
+  const uint32_t choose = lane & 1 ? 0x03020706u : 0x05040100u;   // bytes of {the neighbour's word, its own}
+  const uint32_t x = __builtin_amdgcn_perm(from_lane(a, std::integral_constant<int, 1>{}), a, choose);   // column 0 or 1 of two rows
+  const uint32_t y = __builtin_amdgcn_perm(from_lane(b, std::integral_constant<int, 1>{}), b, choose);   // column 2 or 3
+  const uint32_t got = from_lane(lane & 2 ? x : y, std::integral_constant<int, 2>{});
+  return lane & 2 ? u32x2{got, y} : u32x2{x, got};
 }
 
 template <class S>
-FP4_D void dz_epilogue(const HeadTile& a, const HpTile& tile, const hp_f32x16 (&acc)[S::QI][S::PJ]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
-  const int r16 = lane & 15, unit = (lane >> 5) + (lane >> 3 & 2);
+FP4_D void dz_epilogue(const HeadTile& a, const HpTile& tile, const f32x4 (&acc)[S::QI][S::PJ]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, quarter = lane >> 4;
+  const int unit = (lane >> 5) + (lane >> 3 & 2);
   const int wave_p = wave % S::WP, wave_q = wave / S::WP;
-  const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 32);
+  const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 16);
   const int64_t left = a.g.Q - q0;
 #pragma unroll
   for (int pj = 0; pj < S::PJ; ++pj) {
-    const int64_t p0 = (int64_t)tile.tp * S::BP + wave_p * (S::PJ * 32) + pj * 32, p = p0 + l32;
+    const int64_t p0 = (int64_t)tile.tp * S::BP + wave_p * (S::PJ * 16) + pj * 16, p = p0 + l16;
     const bool in = p < a.g.P;
     const int64_t t = in ? a.targets[p] : -1;
     const bool active = t >= 0 && t < a.V;
@@ -143,96 +152,76 @@ FP4_D void dz_epilogue(const HeadTile& a, const HpTile& tile, const hp_f32x16 (&
     const float shift = active ? fmaf(-a.lse[p], LOG2E, 15.0f) : -INFINITY;
     const int64_t at = active ? t - a.first - q0 : -1;
 #pragma unroll
-    for (int i = 0; i < S::QI; ++i) {
-      uint32_t d[8];
+    for (int i = 0; i < S::QI; i += 2) {
+      uint32_t d[2][2];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        float e[2];
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float x[2];
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const int e = 2 * k + v, q = (i + u) * 16 + quarter * 4 + e;
+            x[v] = __builtin_amdgcn_exp2f(fmaf(acc[i + u][pj][e], LOG2E, shift));
+            if (at == q) x[v] -= DZ_SCALE;
+            x[v] = active && q < left ? x[v] : 0.0f;
+          }
+          d[u][k] = pack_f16(x[0], x[1]);
+        }
+      if (a.dz_across) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int v = 2 * k + u, q = i * 32 + v / 4 * 8 + h * 4 + v % 4;
-          e[u] = __builtin_amdgcn_exp2f(fmaf(acc[i][pj][v], LOG2E, shift));
-          if (at == q) e[u] -= DZ_SCALE;
-          e[u] = active && q < left ? e[u] : 0.0f;
-        }
-        d[k] = pack_f16(e[0], e[1]);
-      }
-      if (a.dz_across) {   // a lane and its neighbour have two rows' elements of two columns: each takes one column's, four bytes of a line
-        const int64_t col0 = q0 + i * 32 + h * 4 + (lane & 1), line = p0 + (l32 & ~1);
-        const uint32_t choose = lane & 1 ? 0x03020706u : 0x05040100u;   // bytes of {the neighbour's word, its own}
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)d[k], 0xB1, 0xf, 0xf, true);   // lane ^ 1
-          const uint32_t two = __builtin_amdgcn_perm(other, d[k], choose);
-          const int64_t col = col0 + k / 2 * 8 + k % 2 * 2;
-          if (col < a.g.Q && line < a.ld_across) *reinterpret_cast<uint32_t*>(a.dz_across + col * a.ld_across + line) = two;
+          const int64_t col = q0 + (i + u) * 16 + quarter * 4 + (lane & 3), line = p0 + (l16 & ~3);
+          const u32x2 four = turn_four(d[u][0], d[u][1]);
+          if (col < a.g.Q && line < a.ld_across) *reinterpret_cast<u32x2*>(a.dz_across + col * a.ld_across + line) = four;
         }
       }
       if (!a.dz) continue;
-      spread16(d);
-      const int64_t col = q0 + i * 32 + unit * 8;
-      if (col < a.ld) {
-        if (p0 + r16 < a.g.P) *reinterpret_cast<u32x4*>(a.dz + (p0 + r16) * a.ld + col) = u32x4{d[0], d[1], d[2], d[3]};
-        if (p0 + 16 + r16 < a.g.P) *reinterpret_cast<u32x4*>(a.dz + (p0 + 16 + r16) * a.ld + col) = u32x4{d[4], d[5], d[6], d[7]};
-      }
+      const u32x4 eight = eight_columns(d[0][0], d[0][1], d[1][0], d[1][1]);
+      const int64_t col = q0 + i * 16 + unit * 8;
+      if (col < a.ld && in) *reinterpret_cast<u32x4*>(a.dz + p * a.ld + col) = eight;
     }
   }
 }
 
 // fp32 to [P x ldo], times a power of two, plus what is there.  Q is a multiple of 8.
 template <class S>
-FP4_D void f32_epilogue(const HeadTile& a, const HpTile& tile, const hp_f32x16 (&acc)[S::QI][S::PJ], float* out, int64_t ldo, float factor) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r16 = lane & 15, unit = (lane >> 5) + (lane >> 3 & 2);
+FP4_D void f32_epilogue(const HeadTile& a, const HpTile& tile, const f32x4 (&acc)[S::QI][S::PJ], float* out, int64_t ldo, float factor) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, quarter = lane >> 4;
   const int wave_p = wave % S::WP, wave_q = wave / S::WP;
-  const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 32);
+  const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 16) + quarter * 4;
 #pragma unroll
   for (int pj = 0; pj < S::PJ; ++pj) {
-    const int64_t p0 = (int64_t)tile.tp * S::BP + wave_p * (S::PJ * 32) + pj * 32;
+    const int64_t p = (int64_t)tile.tp * S::BP + wave_p * (S::PJ * 16) + pj * 16 + l16;
+    if (p >= a.g.P) continue;
 #pragma unroll
-    for (int j = 0; j < S::QI * 2; ++j) {   // columns 16 j + 4 unit on, of the first sixteen rows and of the others
-      f32x4 y[2];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t u = f2u(acc[j / 2][pj][(j % 2) * 8 + i]), w = f2u(acc[j / 2][pj][(j % 2) * 8 + 4 + i]);
-        hp_swap16(u, w);
-        y[0][i] = u2f(u) * factor;
-        y[1][i] = u2f(w) * factor;
-      }
-      const int64_t col = q0 + 16 * j + 4 * unit;
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        const int64_t p = p0 + 16 * v + r16;
-        if (p < a.g.P && col < a.g.Q) {
-          f32x4* const o = reinterpret_cast<f32x4*>(out + p * ldo + col);
-          if (a.add) y[v] += *o;
-          *o = y[v];
-        }
+    for (int i = 0; i < S::QI; ++i) {
+      const int64_t col = q0 + i * 16;
+      if (col < a.g.Q) {
+        f32x4* const o = reinterpret_cast<f32x4*>(out + p * ldo + col);
+        f32x4 y = acc[i][pj] * factor;
+        if (a.add) y += *o;
+        *o = y;
       }
     }
   }
 }
 template <class S>
-FP4_D void bf16_epilogue(const HeadTile& a, const HpTile& tile, const hp_f32x16 (&acc)[S::QI][S::PJ], float factor) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r16 = lane & 15, unit = (lane >> 5) + (lane >> 3 & 2);
+FP4_D void bf16_epilogue(const HeadTile& a, const HpTile& tile, const f32x4 (&acc)[S::QI][S::PJ], float factor) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15;
+  const int unit = (lane >> 5) + (lane >> 3 & 2);
   const int wave_p = wave % S::WP, wave_q = wave / S::WP;
-  const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 32);
+  const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 16) + unit * 8;
   uint16_t* const out = reinterpret_cast<uint16_t*>(a.out);
 #pragma unroll
   for (int pj = 0; pj < S::PJ; ++pj) {
-    const int64_t p0 = (int64_t)tile.tp * S::BP + wave_p * (S::PJ * 32) + pj * 32;
+    const int64_t p = (int64_t)tile.tp * S::BP + wave_p * (S::PJ * 16) + pj * 16 + l16;
 #pragma unroll
-    for (int i = 0; i < S::QI; ++i) {
-      uint32_t d[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) d[k] = hp_pack_bf16(acc[i][pj][2 * k] * factor, acc[i][pj][2 * k + 1] * factor);
-      spread16(d);
-      const int64_t col = q0 + i * 32 + unit * 8;
-      if (col < a.g.Q) {
-        if (p0 + r16 < a.g.P) *reinterpret_cast<u32x4*>(out + (p0 + r16) * a.ld + col) = u32x4{d[0], d[1], d[2], d[3]};
-        if (p0 + 16 + r16 < a.g.P) *reinterpret_cast<u32x4*>(out + (p0 + 16 + r16) * a.ld + col) = u32x4{d[4], d[5], d[6], d[7]};
-      }
+    for (int i = 0; i < S::QI; i += 2) {
+      const f32x4 x = acc[i][pj] * factor, y = acc[i + 1][pj] * factor;
+      const u32x4 eight = eight_columns(hp_pack_bf16(x.x, x.y), hp_pack_bf16(x.z, x.w), hp_pack_bf16(y.x, y.y), hp_pack_bf16(y.z, y.w));
+      const int64_t col = q0 + i * 16;
+      if (p < a.g.P && col < a.g.Q) *reinterpret_cast<u32x4*>(out + p * a.ld + col) = eight;
     }
   }
 }
@@ -286,11 +275,11 @@ struct Largest {
   FP4_D void leave(const HeadTile& a, const HpTile& tile) const {
     if (of_w) leave(wider(w), a.amax_w);
     if (of_x) {
-      const int wave_p = (threadIdx.x >> 6) % S::WP, l32 = threadIdx.x & 31;
+      const int wave_p = (threadIdx.x >> 6) % S::WP, l16 = threadIdx.x & 15;
       uint32_t best = 0;
 #pragma unroll
       for (int j = 0; j < S::PJ; ++j) {   // rows behind the edge repeat the last one
-        const int64_t p = min((int64_t)tile.tp * S::BP + wave_p * (S::PJ * 32) + j * 32 + l32, a.g.P - 1);
+        const int64_t p = min((int64_t)tile.tp * S::BP + wave_p * (S::PJ * 16) + j * 16 + l16, a.g.P - 1);
         best = max(best, f2u(u2f(wider(x[j])) * fabsf(row_weight(a.dloss, a.targets, a.V, p))));
       }
       leave(best, a.amax_x);
@@ -306,7 +295,7 @@ struct Largest {
 template <class S, int EPI>
 __global__ __launch_bounds__(S::WAVES * 64) void head_tile_kernel(HeadTile a) {
   __shared__ __attribute__((aligned(16))) uint8_t smem[S::SMEM];
-  hp_f32x16 acc[S::QI][S::PJ];
+  f32x4 acc[S::QI][S::PJ];
   const HpTile tile = hp_tile_at(a.g);
   if constexpr (EPI == EPI_DZ) {
     if (Largest<S>::w_here(a, tile) || Largest<S>::x_here(a, tile)) {   // the others' loop stays free of branches
@@ -472,8 +461,8 @@ __global__ __launch_bounds__(256, PB == 1 ? 2 : 1) void head_dx_few_kernel(FewDx
       for (int j = 0; j < 4; ++j) t[j] = __builtin_amdgcn_perm(s.w[2 * j + 1][f / 2], s.w[2 * j][f / 2], f % 2 ? 0x07060302u : 0x05040100u);
 #pragma unroll
       for (int b = 0; b < PB; ++b) {
-        acc[b][f] = hp_mfma<false>(high[b], t, acc[b][f]);
-        acc[b][f] = hp_mfma<false>(low[b], t, acc[b][f]);
+        acc[b][f] = hp_mfma32(high[b], t, acc[b][f]);
+        acc[b][f] = hp_mfma32(low[b], t, acc[b][f]);
       }
     }
   }
@@ -535,10 +524,10 @@ static_assert(FEW_TOKENS * HP_MAX_DIM <= PIECE, "their dz is one piece");
 bool few_tokens(int64_t M) { return M <= FEW_TOKENS; }
 
 // ---- which tiles ---------------------------------------------------------------------------------------------------------------
-using Large = HpShape<2, 4, 4, 2, 2>;    // 256 x 256
-using Middle = HpShape<2, 2, 2, 2, 2>;   // 128 x 128, two a CU
-using Few = HpShape<1, 4, 2, 1, 3>;      // 64 x 128, two a CU
-using Fewest = HpShape<1, 4, 1, 1, 4>;   // 32 x 128, two a CU
+using Large = HpShape<2, 4, 8, 4, 2>;    // 256 x 256
+using Middle = HpShape<2, 2, 4, 4, 2>;   // 128 x 128, two a CU
+using Few = HpShape<1, 4, 4, 2, 3>;      // 64 x 128, two a CU
+using Fewest = HpShape<1, 4, 2, 2, 4>;   // 32 x 128, two a CU
 constexpr int64_t LEAST_BQ = 128;
 
 enum { TILE_LARGE, TILE_MIDDLE, TILE_FEW, TILE_FEWEST };
