@@ -113,6 +113,8 @@ FP4_D HpTile hp_tile_at(const HpOperands& g) {
 // The sums of one tile.  smem is free of requests and of other waves' reads when it returns.  watch sees each slice's fragments.
 // A slice's fragments are read while the matrix cores work on the slice before.  A step's barrier stands between its slices: by then every wave holds the
 // second slice's fragments, so that the stage is free for a later step, and the next step has landed, whose first fragments are read in the second slice's shadow.
+// Reads stand one by one among the products and the steady loop has no branches: the compiler's own order, with all reads ahead of all products,
+// takes 449 against 425 us for 8192 x 8192 over 4096 in 256 x 256 tiles, and 52 against 43 for 2048 x 2048 in 128 x 128 ones.
 template <class S, bool F16, class Watch>
 FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, f32x4 (&acc)[S::QI][S::PJ], Watch&& watch) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -134,11 +136,11 @@ FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, 
     offR[j] = (uint32_t)((min(Q0 + row, g.Q - 1) - Q0) * rowR + chunk_of(row) * 16);
   }
   const int first = tile.split * g.split_steps, all = (int)((g.K + 63) / 64), T = min(all - first, g.split_steps);
-  const auto load_step = [&](int t) {
+  const auto load_step = [&](int t, auto whole) {
     const int step = first + t;
     uint8_t* const stage = smem + t % S::NST * S::STAGE;
     const int left = (int)(g.K / 8) - step * 8;   // chunks of a row from here on
-    if (left >= 8) {
+    if (decltype(whole)::value || left >= 8) {
 #pragma unroll
       for (int j = 0; j < S::LDL; ++j) hp_to_lds(rsrcL, stage + (wave * S::LDL + j) * 1024, offL[j], step * 128);
 #pragma unroll
@@ -174,27 +176,41 @@ FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, 
 #pragma unroll
       for (int j = 0; j < S::PJ; ++j) acc[i][j] = hp_mfma<F16>(fr[s][i], fl[s][j], acc[i][j]);
     watch(fl[s], fr[s]);
-    __builtin_amdgcn_sched_barrier(0);
   };
 #pragma unroll
   for (int t = 0; t < S::NST; ++t)
-    if (t < T) load_step(t);
+    if (t < T) load_step(t, std::false_type{});
   if (T >= S::NST) hp_wait<(S::NST - 1) * S::LOADS>();
   else hp_wait<0>();
   __builtin_amdgcn_s_barrier();   // a bare one: a fence would wait for the other stages too
   asm volatile("" ::: "memory");
   read(0, 0);
-  for (int t = 0; t < T; ++t) {
+  const auto among = [&] {   // one read, so many products, one read, ...
+    constexpr int READS = S::PJ + S::QI, PRODUCTS = S::PJ * S::QI / READS;
+    hp_static_for<READS>([&](auto) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS, 0);
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const auto step = [&](int t, auto steady) {
+    constexpr bool STEADY = decltype(steady)::value;
     read(t, 1);
     multiply(0);
+    if constexpr (STEADY) among();
+    asm volatile("" ::: "memory");
     // Steps t + 2 .. t + NST - 1 may still be on their way; towards the end there are fewer, and then all have to have landed
-    if (t + S::NST - 1 < T) hp_wait<(S::NST - 2) * S::LOADS>();
+    if (STEADY || t + S::NST - 1 < T) hp_wait<(S::NST - 2) * S::LOADS>();
     else hp_wait<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (t + S::NST < T) load_step(t + S::NST);
-    if (t + 1 < T) read(t + 1, 0);
+    if (STEADY || t + S::NST < T) load_step(t + S::NST, steady);
+    if (STEADY || t + 1 < T) read(t + 1, 0);
     multiply(1);
-  }
+    if constexpr (STEADY) among();
+  };
+  int t = 0;
+  for (; t < T - S::NST - 1; ++t) step(t, std::true_type{});   // free of branches: the steps it requests are whole ones
+  for (; t < T; ++t) step(t, std::false_type{});
   __syncthreads();
 }

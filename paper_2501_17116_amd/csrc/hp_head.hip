@@ -293,7 +293,7 @@ struct Largest {
 // Tried: waves of 128 x 128 sums, one a SIMD, in two stages of 64 or five of 32 elements, reads and requests between the matrix instructions: fewer
 // idle cycles at a lower clock, 945 against 922 us for 16384 x 4096 over 8192, and 1217 where lines lie 32 KiB apart.
 template <class S, int EPI>
-__global__ __launch_bounds__(S::WAVES * 64) void head_tile_kernel(HeadTile a) {
+__global__ __launch_bounds__(S::WAVES * 64, 2) void head_tile_kernel(HeadTile a) {
   __shared__ __attribute__((aligned(16))) uint8_t smem[S::SMEM];
   f32x4 acc[S::QI][S::PJ];
   const HpTile tile = hp_tile_at(a.g);
