@@ -113,8 +113,9 @@ FP4_D HpTile hp_tile_at(const HpOperands& g) {
 // The sums of one tile.  smem is free of requests and of other waves' reads when it returns.  watch sees each slice's fragments.
 // A slice's fragments are read while the matrix cores work on the slice before.  A step's barrier stands between its slices: by then every wave holds the
 // second slice's fragments, so that the stage is free for a later step, and the next step has landed, whose first fragments are read in the second slice's shadow.
-// Reads stand one by one among the products and the steady loop has no branches: the compiler's own order, with all reads ahead of all products,
-// takes 449 against 425 us for 8192 x 8192 over 4096 in 256 x 256 tiles, and 52 against 43 for 2048 x 2048 in 128 x 128 ones.
+// The steady loop has no branches, and requests and reads stand one by one among the products: with the compiler's own order, all reads ahead of all
+// products, 8192 x 8192 over 4096 takes 449 us in 256 x 256 tiles and 2048 x 2048 over 4096 takes 52 in 128 x 128 ones; so 418 and 42.  Requests behind
+// the reads gain another us there, but lose 5 % where rows lie 128 KiB apart and what is asked for comes late.
 template <class S, bool F16, class Watch>
 FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, f32x4 (&acc)[S::QI][S::PJ], Watch&& watch) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -185,19 +186,27 @@ FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, 
   __builtin_amdgcn_s_barrier();   // a bare one: a fence would wait for the other stages too
   asm volatile("" ::: "memory");
   read(0, 0);
-  const auto among = [&] {   // one read, so many products, one read, ...
-    constexpr int READS = S::PJ + S::QI, PRODUCTS = S::PJ * S::QI / READS;
-    hp_static_for<READS>([&](auto) {
+  constexpr int BETWEEN = S::PJ * S::QI >= 32 ? 2 : 1;
+  const auto reads_among = [] {   // a read, a product, a read, ...
+    hp_static_for<S::PJ + S::QI>([](auto) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     });
-    __builtin_amdgcn_sched_barrier(0);
+  };
+  const auto requests_among = [] {
+    hp_static_for<S::LOADS>([](auto) {
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, BETWEEN, 0);
+    });
   };
   const auto step = [&](int t, auto steady) {
     constexpr bool STEADY = decltype(steady)::value;
     read(t, 1);
     multiply(0);
-    if constexpr (STEADY) among();
+    if constexpr (STEADY) {
+      reads_among();
+      __builtin_amdgcn_sched_barrier(0);
+    }
     asm volatile("" ::: "memory");
     // Steps t + 2 .. t + NST - 1 may still be on their way; towards the end there are fewer, and then all have to have landed
     if (STEADY || t + S::NST - 1 < T) hp_wait<(S::NST - 2) * S::LOADS>();
@@ -207,7 +216,11 @@ FP4_D void hp_tile_sums(const HpOperands& g, const HpTile& tile, uint8_t* smem, 
     if (STEADY || t + S::NST < T) load_step(t + S::NST, steady);
     if (STEADY || t + 1 < T) read(t + 1, 0);
     multiply(1);
-    if constexpr (STEADY) among();
+    if constexpr (STEADY) {
+      requests_among();
+      reads_among();
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   int t = 0;
   for (; t < T - S::NST - 1; ++t) step(t, std::true_type{});   // free of branches: the steps it requests are whole ones
