@@ -134,6 +134,17 @@ FP4_D u32x2 turn_four(uint32_t a, uint32_t b) {
   const uint32_t got = from_lane(lane & 2 ? x : y, std::integral_constant<int, 2>{});
   return lane & 2 ? u32x2{got, y} : u32x2{x, got};
 }
+FP4_D uint32_t from_lane(uint32_t x, std::integral_constant<int, 4>) {   // lane ^ 4: ^ 7 and then ^ 3
+  return (uint32_t)__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xf, 0xf, true), 0x1B, 0xf, 0xf, true);
+}
+// Four rows of a column in each of two blocks of sixteen rows -> eight rows in a row of one of them, the first block's in lanes without bit 2.
+FP4_D u32x4 eight_rows(u32x2 a, u32x2 b) {
+  const bool second = threadIdx.x & 4;
+  const std::integral_constant<int, 4> four;
+  const u32x2 own = second ? b : a, others = second ? a : b;
+  const u32x2 got = {from_lane(others.x, four), from_lane(others.y, four)};
+  return second ? u32x4{got.x, got.y, own.x, own.y} : u32x4{own.x, own.y, got.x, got.y};
+}
 
 template <class S>
 FP4_D void dz_epilogue(const HeadTile& a, const HpTile& tile, const f32x4 (&acc)[S::QI][S::PJ]) {
@@ -143,43 +154,53 @@ FP4_D void dz_epilogue(const HeadTile& a, const HpTile& tile, const f32x4 (&acc)
   const int64_t q0 = (int64_t)tile.tq * S::BQ + wave_q * (S::QI * 16);
   const int64_t left = a.g.Q - q0;
 #pragma unroll
-  for (int pj = 0; pj < S::PJ; ++pj) {
-    const int64_t p0 = (int64_t)tile.tp * S::BP + wave_p * (S::PJ * 16) + pj * 16, p = p0 + l16;
-    const bool in = p < a.g.P;
-    const int64_t t = in ? a.targets[p] : -1;
-    const bool active = t >= 0 && t < a.V;
-    // e^(z - lse) 2^15; nothing of a row without a target
-    const float shift = active ? fmaf(-a.lse[p], LOG2E, 15.0f) : -INFINITY;
-    const int64_t at = active ? t - a.first - q0 : -1;
+  for (int pj = 0; pj < S::PJ; pj += 2) {
+    const int64_t p0 = (int64_t)tile.tp * S::BP + wave_p * (S::PJ * 16) + pj * 16;
+    bool active[2];
+    float shift[2];
+    int64_t at[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int64_t p = p0 + r * 16 + l16, t = p < a.g.P ? a.targets[p] : -1;
+      active[r] = t >= 0 && t < a.V;
+      // e^(z - lse) 2^15; nothing of a row without a target
+      shift[r] = active[r] ? fmaf(-a.lse[p], LOG2E, 15.0f) : -INFINITY;
+      at[r] = active[r] ? t - a.first - q0 : -1;
+    }
 #pragma unroll
     for (int i = 0; i < S::QI; i += 2) {
-      uint32_t d[2][2];
+      uint32_t d[2][2][2];   // of two blocks of rows, two of columns, two pairs of columns
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float x[2];
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const int e = 2 * k + v, q = (i + u) * 16 + quarter * 4 + e;
-            x[v] = __builtin_amdgcn_exp2f(fmaf(acc[i + u][pj][e], LOG2E, shift));
-            if (at == q) x[v] -= DZ_SCALE;
-            x[v] = active && q < left ? x[v] : 0.0f;
+          for (int k = 0; k < 2; ++k) {
+            float x[2];
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              const int e = 2 * k + v, q = (i + u) * 16 + quarter * 4 + e;
+              x[v] = __builtin_amdgcn_exp2f(fmaf(acc[i + u][pj + r][e], LOG2E, shift[r]));
+              if (at[r] == q) x[v] -= DZ_SCALE;
+              x[v] = active[r] && q < left ? x[v] : 0.0f;
+            }
+            d[r][u][k] = pack_f16(x[0], x[1]);
           }
-          d[u][k] = pack_f16(x[0], x[1]);
-        }
       if (a.dz_across) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int64_t col = q0 + (i + u) * 16 + quarter * 4 + (lane & 3), line = p0 + (l16 & ~3);
-          const u32x2 four = turn_four(d[u][0], d[u][1]);
-          if (col < a.g.Q && line < a.ld_across) *reinterpret_cast<u32x2*>(a.dz_across + col * a.ld_across + line) = four;
+          const int64_t col = q0 + (i + u) * 16 + quarter * 4 + (lane & 3), line = p0 + (lane & 4) * 4 + (lane & 8);
+          const u32x4 eight = eight_rows(turn_four(d[0][u][0], d[0][u][1]), turn_four(d[1][u][0], d[1][u][1]));
+          if (col < a.g.Q && line < a.ld_across) *reinterpret_cast<u32x4*>(a.dz_across + col * a.ld_across + line) = eight;
         }
       }
       if (!a.dz) continue;
-      const u32x4 eight = eight_columns(d[0][0], d[0][1], d[1][0], d[1][1]);
-      const int64_t col = q0 + i * 16 + unit * 8;
-      if (col < a.ld && in) *reinterpret_cast<u32x4*>(a.dz + p * a.ld + col) = eight;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const u32x4 eight = eight_columns(d[r][0][0], d[r][0][1], d[r][1][0], d[r][1][1]);
+        const int64_t p = p0 + r * 16 + l16, col = q0 + i * 16 + unit * 8;
+        if (col < a.ld && p < a.g.P) *reinterpret_cast<u32x4*>(a.dz + p * a.ld + col) = eight;
+      }
     }
   }
 }
