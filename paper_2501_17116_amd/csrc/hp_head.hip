@@ -555,8 +555,9 @@ enum { TILE_LARGE, TILE_MIDDLE, TILE_FEW, TILE_FEWEST };
 struct Cut { int tile, splits; };
 
 // Few rows: the tiles that do not calculate much in vain, all of them waiting for w (64 x 32768 over 4096: 64 / 128 / 256 rows a tile 40 / 57 / 84 us;
-// 128 rows 55 / 59 / 85).  More: by rounds of the chip's workgroups, in hundredths of a us (measured): a step of 64 takes a 256 x 256 tile 1.41 with
-// half of the CUs at work, 1.74 with all of them (power), two 128 x 128 tiles of one CU 1.05, a single one about 0.65; a tile's start and end
+// 128 rows 55 / 59 / 85).  More: by rounds of the chip's workgroups, in hundredths of a us (measured): a step of 64 takes a 256 x 256 tile 1.1, 1.25,
+// 1.5 and 1.8 with a quarter, half, three quarters and all of the CUs at work (power) and 1.6 over several rounds, which do not keep step; two
+// 128 x 128 tiles of one CU take 1.05, a single one about 0.63; a tile's start and end
 // 6 and 4.  Splitting the contraction (only where the sums can be added up later: most > 1) brings rounds and takes sums' bytes.
 Cut cut_of(int64_t P, int64_t Q, int64_t K, int most) {
   const int64_t steps = (K + 63) / 64;
@@ -568,8 +569,8 @@ Cut cut_of(int64_t P, int64_t Q, int64_t K, int most) {
   for (int s = 1; s <= most; ++s) {
     const int64_t k = (steps + s - 1) / s, sums = s > 1 ? s * P * Q / 10000 : 0;   // in 1/100 us: 16 bytes a sum at 5 TB/s would be 3.2 a 10000
     const int64_t nl = tiles(256, 256) * s, nm = tiles(128, 128) * s, rl = nl % 256, rm = nm % 512;
-    const int64_t large = nl / 256 * (174 * k + 600) + (rl ? (141 + 33 * rl / 256) * k + 600 : 0) + sums;
-    const int64_t middle = nm / 512 * (105 * k + 400) + (rm ? (rm > 256 ? 105 : 65) * k + 400 : 0) + sums;
+    const int64_t large = nl / 256 * (160 * k + 600) + (rl ? (100 + 75 * rl / 256) * k + 600 : 0) + sums;
+    const int64_t middle = nm / 512 * (105 * k + 400) + (rm ? (rm > 256 ? 105 : 63) * k + 400 : 0) + sums;
     if (large < least) least = large, best = {TILE_LARGE, s};
     if (middle < least) least = middle, best = {TILE_MIDDLE, s};
   }
