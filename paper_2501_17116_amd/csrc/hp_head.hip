@@ -308,11 +308,11 @@ struct Largest {
   }
 };
 
-// A tile of logits or of a gradient product.  256 x 256, measured: 8192 x 32000 over 2048 (maxima and sums) 0.90 ms, 1.19e15 operations/s; 16384 x 4096 over 8192 (dw) 0.91 ms,
-// 1.21e15; dz's tiles end with 128 KB of stores twice, 1.1e15 over 4096, 0.65e15 over 1376.  Bound by power: the clock falls to 1.9 GHz, the matrix
-// cores are busy in 50 - 59 % of the cycles, LDS conflicts are none.
-// Tried: waves of 128 x 128 sums, one a SIMD, in two stages of 64 or five of 32 elements, reads and requests between the matrix instructions: fewer
-// idle cycles at a lower clock, 945 against 922 us for 16384 x 4096 over 8192, and 1217 where lines lie 32 KiB apart.
+// A tile of logits or of a gradient product.  256 x 256, measured: 8192 x 32000 over 2048 (maxima and sums) 0.81 ms, 1.33e15 operations/s; 32768 x 4096 over 8192 (dw) 1.56 ms,
+// 1.41e15; dz's tiles end with 128 KB of stores twice, 1.2e15 over 4096, 0.64e15 over 1376.  Bound by power: in long runs the clock falls to 1.6 GHz, the matrix
+// cores are busy in 52 - 68 % of the cycles, LDS conflicts are none.  Two waves a SIMD: without that bound the compiler takes 512 registers for the
+// 128 x 128 tile and moves every fragment through accumulation registers.
+// Tried: waves of 128 x 128 sums, one a SIMD: at a lower clock and no faster with 32 x 32 x 16 instructions; with 16 x 16 x 32 ones they do not fit their registers.
 template <class S, int EPI>
 __global__ __launch_bounds__(S::WAVES * 64, 2) void head_tile_kernel(HeadTile a) {
   __shared__ __attribute__((aligned(16))) uint8_t smem[S::SMEM];
