@@ -126,7 +126,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(NormFwd a) {
 }
 
 // A workgroup goes from row to row and keeps the sums of its rows; AHEAD: the next row's pieces are requested before the present one's are used.  (8192 x
-// 5120: 102 us, 4.9 TB/s; with two pieces a thread, whose operands and sums spill, 1014.)
+// 5120: 94 us, 5.3 TB/s; with two pieces a thread, whose operands and sums spill, 1014.)
 template <class T, int CH, int THREADS, bool AHEAD>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormBwd a) {
   __shared__ float lds[2][16];
@@ -285,8 +285,9 @@ RowShape row_shape(int64_t D, bool two) {
   return two || n > 1024 ? RowShape{(int)((n + 127) / 128 * 64), 2} : RowShape{(int)((n + 63) / 64 * 64), 1};
 }
 RowShape fwd_shape(int64_t M, int64_t D) { return row_shape(D, M > 512 && D > 1024); }
-// Backward: workgroups, some 24 waves a CU.
-int64_t bwd_groups(int64_t M, const RowShape& s) { return std::min<int64_t>(M, 256 * std::max(1, std::min(4, 1536 / s.threads))); }
+// Backward: workgroups, as many as the registers let run at once (two bytes twelve waves a CU, four bytes eight), but no more than four a CU, whose partial
+// sums have to be joined.  Twice as many, in two rounds that ask for their first rows anew: 2048 x 4096 36 against 31 us with the join, 8192 x 5120 112 against 100.
+int64_t bwd_groups(int64_t M, const RowShape& s, bool two_bytes) { return std::min<int64_t>(M, 256 * std::max(1, std::min(4, (two_bytes ? 768 : 512) / s.threads))); }
 
 template <class T>
 void launch_fwd(const NormFwd& a, hipStream_t s) {
@@ -298,7 +299,7 @@ template <class T>
 void launch_bwd(const NormBwd& a, hipStream_t s) {
   constexpr bool HALF = HpSize<T>::value == 2;
   const RowShape r = row_shape(a.D, false);
-  const unsigned groups = (unsigned)bwd_groups(a.M, r);
+  const unsigned groups = (unsigned)bwd_groups(a.M, r, HALF);
   if (r.pieces == 2) norm_bwd_kernel<T, 2, 1024, false><<<groups, r.threads, 0, s>>>(a);
   else if (r.threads <= 512) norm_bwd_kernel<T, 1, 512, HALF><<<groups, r.threads, 0, s>>>(a);
   else if (r.threads <= 768) norm_bwd_kernel<T, 1, 768, HALF><<<groups, r.threads, 0, s>>>(a);
@@ -329,7 +330,7 @@ int hp_launch_norm_bwd(const hp_norm* n, int bf16, int64_t M, int64_t D, const v
   NormSums f = {part, {dw_before, dw_after, shared_gate ? (float*)dgate : nullptr}, 0, D, Dp, accumulate};
   for (int i = 0; i < 3; ++i) a.sums |= f.out[i] ? 1 << i : 0;
   if (M > 0) {
-    f.rows = bwd_groups(M, row_shape(D, false));
+    f.rows = bwd_groups(M, row_shape(D, false), bf16);
     if (bf16) launch_bwd<BF16>(a, s);
     else launch_bwd<F32>(a, s);
     FP4_CHECK_LAUNCH();
