@@ -923,7 +923,7 @@ class HpNorm:
     """The joint of two blocks: what hp_norm_fwd and hp_norm_bwd take besides the tokens.
 
     w_before [D]: weights of the norm before the next block (None: there is none); w_after [D]: of the norm after the block; gate: [D], one
-    for all tokens, or [M, D], a row for each; scale: of the residual stream."""
+    for all tokens, or [M, D], a row for each (a vector that was expanded to that is refused); scale: of the residual stream."""
 
     __slots__ = ("w_before", "w_after", "gate", "scale", "eps")
 
@@ -944,6 +944,8 @@ class HpNorm:
                 gate = _hp_vector(gate, D, dtype, device, "gate")
             else:
                 gate, ld_gate = _hp_matrix(gate, shape, dtype, device, "gate")
+                if ld_gate < D:   # 0 would be read as one vector, whose gradient is [D]
+                    raise ValueError("a gate's rows overlap: one vector for all tokens is given as [D], not expanded")
         return C.byref(hp_norm(_hp_vector(self.w_before, D, dtype, device, "w_before"), _hp_vector(self.w_after, D, dtype, device, "w_after"), gate, ld_gate,
                                self.scale, self.eps))
 

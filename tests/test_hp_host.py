@@ -242,3 +242,28 @@ def test_types_of_the_head(reached):
     with pytest.raises(TypeError):
         b.hp_embed_fwd(Line(0, M, I64), On(0, V, D, torch.float16))
     assert not reached
+
+
+class Expanded(On):
+    """One row that stands for all: expand()'s strides."""
+
+    def stride(self):
+        return (0, 1)
+
+
+@pytest.mark.parametrize("rows,width", [(M, D), (2, D), (M, 1)])
+def test_an_expanded_gate_is_refused(reached, rows, width):
+    """A leading dimension of 0 means one vector to the library, whose gradient is a sum over the tokens, not a row for each.  The vector itself is taken."""
+    gate = Expanded(0, rows, width)
+    norm = b.HpNorm(Line(0, width, BF16), gate=gate)
+    x = On(0, rows, width if width > 1 else 8)
+    if width == 1:   # rows of one channel, eight apart
+        x.shape, x.stride = (rows, 1), lambda: (8, 1)
+    with pytest.raises(ValueError, match="gate"):
+        b.hp_norm_fwd(norm, x, x, h=x, y=x)
+    with pytest.raises(ValueError, match="gate"):
+        b.hp_norm_bwd(norm, b.HpNormSaved(Line(0, rows)), x, x, x, x, into=b.HpNormGrads(x, x, x, Line(0, width), None), ws=Room0())
+    assert not reached
+    vector = b.HpNorm(Line(0, width, BF16), gate=Line(0, width, BF16))
+    b.hp_norm_bwd(vector, b.HpNormSaved(Line(0, rows)), x, x, x, x, into=b.HpNormGrads(x, x, Line(0, width), Line(0, width), None), ws=Room0())
+    assert reached == ["hp_norm_bwd"]
