@@ -4,7 +4,7 @@
 //   dz[t, v] = c_t (e^(z[t, v] - lse_t) - [v = target_t]),  c_t the gradient of loss_t;   dx = dz w,  dw = dz^T x
 //
 // Forward: tiles of z in registers, of which a tile leaves each row's maximum m and sum of e^(z - m), and the target's z; a second launch joins the tiles
-// in their order.
+// in their order.  A sum of 0 is that of no columns, or of logits of -inf; one that is NaN (a logit of NaN or +inf) is carried on into the row's lse and loss.
 // Backward, a piece of the vocabulary at a time: its logits again, of which e^(z - lse) - [target] is kept as fp16 under 2^15 (11 bits; its
 // values lie in [-1, 1], and below 2^-29 of 1 an element loses bits, below 2^-40 all of them); dx adds the product with the piece of w, dw's rows are the product
 // with c x.  Both contract over what lies across in memory, so transposed copies are made, and as they are made anyway they are made in fp16, under
@@ -105,7 +105,7 @@ FP4_D void stats_epilogue(const HeadTile& a, const HpTile& tile, uint8_t* smem, 
 #pragma unroll
     for (int i = 0; i < S::WQ; ++i) {
       const float2 o = lds[i * S::BP + row];
-      if (o.y > 0.0f) s += o.y * __builtin_amdgcn_exp2f((o.x - m) * LOG2E);
+      if (o.y != 0.0f) s += o.y * __builtin_amdgcn_exp2f((o.x - m) * LOG2E);
     }
     a.part[(int64_t)tile.tq * a.g.P + p] = float2{m, s};
   }
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(1024) void head_join_kernel(const float2* part, int
   const int64_t p = (int64_t)blockIdx.x * ROWS + r, row = min(p, M - 1);
   float m = -INFINITY, s = 0.0f;
   const auto join = [&](float2 o) {
-    if (o.y > 0.0f) {
+    if (o.y != 0.0f) {
       const float top = fmaxf(m, o.x);
       s = s * (m == top ? 1.0f : __builtin_amdgcn_exp2f((m - top) * LOG2E)) + o.y * (o.x == top ? 1.0f : __builtin_amdgcn_exp2f((o.x - top) * LOG2E));
       m = top;

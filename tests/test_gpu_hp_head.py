@@ -242,3 +242,51 @@ def test_graphs_with_workspaces_of_their_own():
         for _, out, _ in runs:
             assert all(torch.equal(a, c) for a, c in zip(out, (ref_loss, ref_lse, ref_dx, ref_dw)))
         assert torch.equal(b.hp_head_bwd(x, w, targets, ref_lse, dloss)[1], ref_dw)
+
+
+NOT_FINITE = [(3, 64, 200), (24, 256, 3001), (64, 136, 1025), (300, 192, 1500), (700, 512, 12000)]   # every tile, both joins
+
+
+@pytest.mark.parametrize("M,D,V", NOT_FINITE)
+def test_logits_that_are_not_finite_are_seen(M, D, V):
+    """In whichever column: the loss of their tokens is not finite, all others keep their bits."""
+    x, w, targets, _ = inputs(M, D, V, ignored=0.0)
+    x[:, 0] = 0.0
+    targets[:] = targets.clamp(max=V - 2)       # the columns below are never a target's but once
+    loss, lse = b.hp_head_fwd(x, w, targets)
+    for v in (0, V // 2, V - 1):
+        bad = w.clone()
+        bad[v, 1] = float("nan")
+        l2, e2 = b.hp_head_fwd(x, bad, targets)
+        assert bool(torch.isnan(e2).all()) and bool(torch.isnan(l2).all()), ("a row of w", v)
+        for t in (0, M - 1):
+            others = torch.arange(M, device="cuda") != t
+            huge, up = w.clone(), x.clone()
+            huge[v, 0], up[t, 0] = 3e38, 3e38    # their product alone leaves fp32
+            l2, e2 = b.hp_head_fwd(up, huge, targets)
+            assert not bool(torch.isfinite(e2[t])) and not bool(torch.isfinite(l2[t])), ("a logit of inf", v, t)
+            assert torch.equal(e2[others], lse[others]) and torch.equal(l2[others], loss[others])
+    for t in (0, M // 2, M - 1):
+        others = torch.arange(M, device="cuda") != t
+        bad = x.clone()
+        bad[t] = float("nan")
+        l2, e2 = b.hp_head_fwd(bad, w, targets)
+        assert bool(torch.isnan(e2[t])) and bool(torch.isnan(l2[t])), ("a row of x", t)
+        assert torch.equal(e2[others], lse[others]) and torch.equal(l2[others], loss[others])
+
+
+@pytest.mark.parametrize("M,D,V", NOT_FINITE)
+def test_logits_of_minus_infinity_count_nothing(M, D, V):
+    x, w, targets, _ = inputs(M, D, V, ignored=0.0)
+    x[:, 0] = 0.0
+    targets[:] = targets.clamp(min=V // 3 + 1)
+    t = M // 2
+    x[t, 0] = 3e38
+    few, far = w.clone(), w.clone()
+    few[:, 0], far[:, 0] = 0.0, 0.0
+    few[:V // 3 + 1, 0], far[:V // 3 + 1, 0] = -3e38, -1e-33     # -inf, and some -3e5, for whole tiles and a part of one
+    assert all(torch.equal(a, c) for a, c in zip(b.hp_head_fwd(x, few, targets), b.hp_head_fwd(x, far, targets)))
+    few[:, 0] = -3e38
+    loss, lse = b.hp_head_fwd(x, few, targets)
+    others = torch.arange(M, device="cuda") != t
+    assert float(lse[t]) == -float("inf") and bool(torch.isfinite(lse[others]).all()) and bool(torch.isfinite(loss[others]).all())
