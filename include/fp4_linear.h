@@ -419,7 +419,8 @@ int hp_embed_bwd(const int64_t* ids, fp4_dtype dt, int64_t M, int64_t D, int64_t
 int hp_head_fwd(const void* x, const void* w, const int64_t* targets, fp4_dtype dt, int64_t M, int64_t D, int64_t V, int64_t ldx, int64_t ldw,
                 float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Gradients under dloss [M], each token's loss's; a target outside [0, V) leaves its token without one, whatever its dloss is.
+/* Gradients under dloss [M], each token's loss's; a target outside [0, V) leaves its token without one, whatever its dloss, its lse and its row of x hold
+ * (NaN and infinities among them).
  *   dz[t, v] = dloss[t] (exp(z[t, v] - lse[t]) - [v = targets[t]]);   dx = dz w (bf16),   dw = dz^T x (dw_dt; fp32: accumulate != 0 adds)
  * Either may be NULL, not both.  lse is the forward pass's over the same x and w.  dz and dloss x enter the products rounded to 11 bits (fp16 under
  * powers of two, which hold w's bf16 as they are), sums are fp32: dw in fp32 is as near as that.  Elements of dz below 2^-40, and of w and dloss x below 2^-39 of

@@ -247,10 +247,14 @@ FP4_D void bf16_epilogue(const HeadTile& a, const HpTile& tile, const f32x4 (&ac
   }
 }
 
-FP4_D float row_weight(const float* weight, const int64_t* targets, int64_t V, int64_t row) {
-  if (!weight) return 1.0f;
+// Whether a row counts: without weights all do, otherwise those that have a target.
+FP4_D bool row_counts(const float* weight, const int64_t* targets, int64_t V, int64_t row) {
+  if (!weight) return true;
   const int64_t t = targets[row];
-  return t >= 0 && t < V ? weight[row] : 0.0f;
+  return t >= 0 && t < V;
+}
+FP4_D float row_weight(const float* weight, const int64_t* targets, int64_t V, int64_t row) {
+  return !row_counts(weight, targets, V, row) ? 0.0f : weight ? weight[row] : 1.0f;
 }
 FP4_D uint32_t pk_max_u16(uint32_t a, uint32_t b) {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -301,7 +305,8 @@ struct Largest {
 #pragma unroll
       for (int j = 0; j < S::PJ; ++j) {   // rows behind the edge repeat the last one
         const int64_t p = min((int64_t)tile.tp * S::BP + wave_p * (S::PJ * 16) + j * 16 + l16, a.g.P - 1);
-        best = max(best, f2u(u2f(wider(x[j])) * fabsf(row_weight(a.dloss, a.targets, a.V, p))));
+        const int64_t t = a.targets[p];
+        if (t >= 0 && t < a.V) best = max(best, f2u(u2f(wider(x[j])) * fabsf(a.dloss[p])));   // a row that does not count may hold anything
       }
       leave(best, a.amax_x);
     }
@@ -412,9 +417,10 @@ __global__ __launch_bounds__(256) void head_across_kernel(AcrossBoth both) {
   for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const u32x4*>(a.x + min(r0 + k, a.rows - 1) * a.ld + c0);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const float f = r0 + k < a.rows ? row_weight(a.weight, a.targets, a.V, r0 + k) : 0.0f;
+    const bool counts = r0 + k < a.rows && row_counts(a.weight, a.targets, a.V, r0 + k);   // zeros of the others, whatever they hold
+    const float f = counts && a.weight ? a.weight[r0 + k] : 1.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[k][i] = r0 + k < a.rows ? pack_f16(u2f(w[k][i] << 16) * f * scale, u2f(w[k][i] & 0xffff0000u) * f * scale) : 0u;
+    for (int i = 0; i < 4; ++i) w[k][i] = counts ? pack_f16(u2f(w[k][i] << 16) * f * scale, u2f(w[k][i] & 0xffff0000u) * f * scale) : 0u;
   }
 #pragma unroll
   for (int c = 0; c < 8; ++c) {

@@ -290,3 +290,22 @@ def test_logits_of_minus_infinity_count_nothing(M, D, V):
     loss, lse = b.hp_head_fwd(x, few, targets)
     others = torch.arange(M, device="cuda") != t
     assert float(lse[t]) == -float("inf") and bool(torch.isfinite(lse[others]).all()) and bool(torch.isfinite(loss[others]).all())
+
+
+@pytest.mark.parametrize("M,D,V", [(2, 64, 200), (90, 128, 300), (300, 192, 1500), (700, 512, 12000)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_what_tokens_without_a_target_hold_counts_nowhere(M, D, V, value):
+    x, w, targets, dloss = inputs(M, D, V, ignored=0.0)
+    targets[::3] = -100
+    targets[1::9] = V
+    out = (targets < 0) | (targets >= V)
+    clean, bad, c = x.clone(), x.clone(), dloss.clone()
+    clean[out] = 0.0
+    bad[out] = value
+    c[out] = value
+    loss, lse = b.hp_head_fwd(clean, w, targets)
+    l2, e2 = b.hp_head_fwd(bad, w, targets)
+    assert torch.equal(l2, loss) and torch.equal(e2[~out], lse[~out])
+    dx, dw = b.hp_head_bwd(clean, w, targets, lse, dloss)
+    dx2, dw2 = b.hp_head_bwd(bad, w, targets, e2, c)
+    assert bool(torch.isfinite(dw).all()) and torch.equal(dx2, dx) and torch.equal(dw2, dw)
