@@ -414,7 +414,8 @@ int hp_embed_bwd(const int64_t* ids, fp4_dtype dt, int64_t M, int64_t D, int64_t
  * multiple of 8, leading dimensions at most 2^21; they are formed in pieces and not kept.
  *   lse[t]  = log sum over v of exp(z[t, v])
  *   loss[t] = lse[t] - z[t, targets[t]];  0 where the target lies outside [0, V)
- * A token with a logit of NaN or +inf has lse = NaN, and loss = NaN if it has a target, so that they show what has diverged; the other tokens' are as without it.
+ * Losses are never negative.  A token with a logit of NaN, +inf or beyond 2^127 has lse = NaN, and loss = NaN if it has a target, so that they show what has
+ * diverged; the other tokens' are as without it.
  * Either output may be NULL, not both.  V >= 1.  Workspace: fp4_workspace_bytes(FP4_OP_HP_HEAD_FWD, M, D, V, dt). */
 int hp_head_fwd(const void* x, const void* w, const int64_t* targets, fp4_dtype dt, int64_t M, int64_t D, int64_t V, int64_t ldx, int64_t ldw,
                 float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);

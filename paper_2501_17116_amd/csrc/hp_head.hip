@@ -105,8 +105,11 @@ FP4_D void stats_epilogue(const HeadTile& a, const HpTile& tile, uint8_t* smem, 
 #pragma unroll
     for (int i = 0; i < S::WQ; ++i) {
       const float2 o = lds[i * S::BP + row];
-      if (o.y != 0.0f) s += o.y * __builtin_amdgcn_exp2f((o.x - m) * LOG2E);
+      // A wave's terms carry 2^off in common: what the rounding of its m log2 e left
+      const float off = fmaf(o.x, LOG2E, -(o.x * LOG2E));
+      if (o.y != 0.0f) s += o.y * __builtin_amdgcn_exp2f((o.x - m) * LOG2E - off);   // NaN too
     }
+    if (s > 0.0f && s < 1.0f) s = 1.0f;   // it holds the maximum's own term, so that no loss falls below 0
     a.part[(int64_t)tile.tq * a.g.P + p] = float2{m, s};
   }
 }

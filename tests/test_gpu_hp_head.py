@@ -309,3 +309,23 @@ def test_what_tokens_without_a_target_hold_counts_nowhere(M, D, V, value):
     dx, dw = b.hp_head_bwd(clean, w, targets, lse, dloss)
     dx2, dw2 = b.hp_head_bwd(bad, w, targets, e2, c)
     assert bool(torch.isfinite(dw).all()) and torch.equal(dx2, dx) and torch.equal(dw2, dw)
+
+
+@pytest.mark.parametrize("M,D,V", [(32, 64, 300), (512, 64, 300), (64, 128, 5000), (700, 512, 12000)])
+@pytest.mark.parametrize("shift", [0.0, -90.0, 700.0])
+def test_losses_are_not_negative(M, D, V, shift):
+    """Near-certain tokens, whose target's logit leads by 15 to 60 and may lie far from 0: the largest logit's own term is exactly 1."""
+    g = torch.Generator().manual_seed(M + V)
+    w = torch.randn(V, D, generator=g) * 0.05
+    w[:, 0] = 1.0
+    targets = torch.randint(0, V, (M,), generator=g)
+    wt = w[targets].clone()
+    wt[:, 0] = 0.0
+    x = wt * ((15.0 + 45.0 * torch.rand(M, 1, generator=g)) / wt.square().sum(1, keepdim=True))
+    x[:, 0] = shift
+    x, w, targets = plain.matrix(x), plain.matrix(w), targets.cuda()
+    want = plain.head(x, w, targets)
+    loss, lse = b.hp_head_fwd(x, w, targets)
+    plain.close(lse, *want["lse"], "lse")
+    plain.close(loss, *want["loss"], "loss")
+    assert bool((loss >= 0).all()), float(loss.min())
