@@ -229,8 +229,10 @@ class Workspace:
     per stream and thread, since a call is several launches and two threads' launches mix on a
     stream, and one per captured graph that is replayed beside other calls.  Growing keeps the
     outgrown buffers alive until release(), because kernels enqueued earlier may still be running
-    in them and torch's allocator knows nothing of streams other than the one a tensor was
-    allocated on."""
+    in them, captured graphs may replay in them, and torch's allocator knows nothing of streams
+    other than the one a tensor was allocated on.  A buffer that takes another's place is at least
+    half as large again, so that all of them together stay below 4.5 times what was asked for,
+    whatever the steps it comes in."""
 
     def __init__(self, device="cuda"):
         self.device = device
@@ -244,10 +246,15 @@ class Workspace:
         return buf
 
     def _sized(self, nbytes: int) -> torch.Tensor:
-        if self.buf.numel() < nbytes:
-            if self.buf.numel():
+        had = self.buf.numel()
+        if had < nbytes:
+            try:
+                buf = torch.empty(max(nbytes, had + had // 2), dtype=torch.uint8, device=self.device)
+            except torch.OutOfMemoryError:
+                buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            if had:
                 self._outgrown.append(self.buf)
-            self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.buf = buf
         return self.buf
 
     def release(self) -> None:
@@ -266,6 +273,20 @@ def _default_workspace(device_index: int, stream: int) -> Workspace:
     if ws is None:
         ws = _default_ws[key] = Workspace(torch.device("cuda", device_index))
     return ws
+
+
+_releasing = threading.Lock()
+
+
+def release_outgrown() -> None:
+    """Give back what the workspaces that calls take by themselves (ws=None) have outgrown, after waiting for the devices it is on.  Graphs that
+    were captured with such a workspace must not be replayed afterwards; those with a Workspace of their own are not concerned."""
+    with _releasing:
+        old = [(key[0], ws, len(ws._outgrown)) for key, ws in _default_ws.copy().items() if ws._outgrown]
+        for device in sorted({device for device, _, _ in old}):
+            torch.cuda.synchronize(device)
+        for _, ws, n in old:
+            del ws._outgrown[:n]     # what other threads have outgrown meanwhile stands behind
 
 
 def _ws(nbytes: int, ws: Optional[Workspace]) -> torch.Tensor:
