@@ -122,3 +122,21 @@ def test_tables_past_2_to_32_bytes():
     dt = b.hp_embed_bwd(dy, ids, V)
     assert [float(dt[i].min()) for i in (0, V - 2, V - 1)] == [1.0, 1.0, 2.0] == [float(dt[i].max()) for i in (0, V - 2, V - 1)]
     assert float(dt[1:V - 2].abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,D,V", [(8193, 24, 300), (32768, 16, 70000), (32769, 16, 70000), (33001, 23, 300), (70001, 8, 256)])
+@pytest.mark.parametrize("kind", ["even", "few", "padded"])
+def test_gradient_of_many_tokens(M, D, V, dtype, kind):
+    """Passes of small workgroups beside the clearing, and of large ones behind it or without it."""
+    ids, g = some(M, V, kind)
+    dy = plain.matrix(torch.randn(M, D, generator=g), dtype, 1)
+    want, tol = gradient(dy, ids, V, 0.3)
+    wide = torch.full((V, -(-D // 8) * 8 + 8), 7.0, device="cuda")
+    got = b.hp_embed_bwd(dy, ids, V, scale=0.3, dtable=wide[:, :D])
+    plain.close(got, want, tol)
+    assert bool((wide[:, D:] == 7).all()) and torch.equal(b.hp_embed_bwd(dy, ids, V, scale=0.3), got)
+    wide.fill_(2.0)
+    got = b.hp_embed_bwd(dy, ids, V, scale=0.3, dtable=wide[:, :D], accumulate=True)
+    plain.close(got, want + 2.0, tol + 2 * plain.U * (want.abs() + 2.0))
+    assert bool((wide[:, D:] == 2).all())

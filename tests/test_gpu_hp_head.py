@@ -329,3 +329,17 @@ def test_losses_are_not_negative(M, D, V, shift):
     plain.close(lse, *want["lse"], "lse")
     plain.close(loss, *want["loss"], "loss")
     assert bool((loss >= 0).all()), float(loss.min())
+
+
+@pytest.mark.parametrize("M,D,V", [(300, 1032, 12100), (1000, 2048, 8200)])
+def test_fp32_gradients_of_the_weights_in_large_tiles(M, D, V):
+    """More than 188 tiles of 256 x 256: alone, added to what is there, and rounded to bf16."""
+    x, w, targets, dloss = inputs(M, D, V)
+    loss, lse, dx, dw = check(x, w, targets, dloss)
+    wide = torch.full((V, D + 16), 1.5, device="cuda")
+    b.hp_head_bwd(x, w, targets, lse, dloss, dw=wide[:, :D], accumulate=True)
+    assert torch.equal(wide[:, :D], dw + 1.5) and bool((wide[:, D:] == 1.5).all())
+    wide.fill_(-2.0)
+    b.hp_head_bwd(x, w, targets, lse, dloss, dw=wide[:, :D])
+    assert torch.equal(wide[:, :D], dw) and bool((wide[:, D:] == -2).all())
+    assert torch.equal(b.hp_head_bwd(x, w, targets, lse, dloss, dw_dtype=torch.bfloat16)[1], dw.bfloat16())

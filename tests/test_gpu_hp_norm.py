@@ -238,3 +238,20 @@ def test_rows_past_2_to_32_bytes():
     d = b.hp_norm_bwd(norm, saved, h, dy=x)
     fd = b.hp_norm_bwd(norm, fs, fh, dy=few)
     assert torch.equal(d.dx[-1], fd.dx[1]) and torch.equal(d.dx[0], fd.dx[0])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,D", [(1500, 1377), (600, 4104), (600, 5120), (600, 6144), (600, 6145), (600, 7001), (600, 8192), (300, 8193), (300, 9001), (520, 16384)])
+@pytest.mark.parametrize("form", ["vector", "token"])
+def test_more_rows_than_workgroups(M, D, dtype, form):
+    """Each width's kernel of the backward pass, its workgroups going from row to row and summing over several."""
+    x, blk, wb, wa, gate, normal = inputs(M, D, dtype, gate=form, seed=M + D)
+    norm = b.HpNorm(wb, wa, gate, scale=0.7, eps=EPS)
+    saved = b.hp_norm_saved(norm, M)
+    h, y = b.hp_norm_fwd(norm, x, blk, saved)
+    check_forward(norm, x, blk, h, y, saved)
+    dy, dh = plain.matrix(normal(M, D) * 0.1, dtype, 1), plain.matrix(normal(M, D) * 0.1, dtype)
+    got = b.hp_norm_bwd(norm, saved, h, dy, dh, blk)
+    check_backward(norm, saved, h, dy, dh, blk, got, M)
+    again = b.hp_norm_bwd(norm, saved, h, dy, dh, blk)
+    assert all(torch.equal(a, c) for a, c in zip(got, again))
