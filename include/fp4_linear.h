@@ -389,7 +389,7 @@ int hp_norm_fwd(const hp_norm* norm, fp4_dtype dt, int64_t M, int64_t D, const v
                 void* h, int64_t ldh, void* y, int64_t ldy, float* r_before, float* r_after, void* stream);
 
 /* dy, dh: gradients of y and of h (the stream's own way on); either may be NULL, not both.  h, block, r_before, r_after: of the forward
- * pass (h and r_before with dy; block where a gradient needs it; r_after with w_after).  Each output may be NULL:
+ * pass (h and r_before with dy; block with w_after, a gate, or dblock; r_after with w_after).  Each output may be NULL:
  *   dx, dblock [M x D] of type dt; may be dh or dy themselves, with the same leading dimension
  *   dgate      ld_gate = 0: fp32 [D]; otherwise [M x D] of type dt, leading dimension ld_dgate
  *   dw_before, dw_after  fp32 [D]
@@ -424,7 +424,7 @@ int hp_head_fwd(const void* x, const void* w, const int64_t* targets, fp4_dtype 
  * (NaN and infinities among them).
  *   dz[t, v] = dloss[t] (exp(z[t, v] - lse[t]) - [v = targets[t]]);   dx = dz w (bf16),   dw = dz^T x (dw_dt; fp32: accumulate != 0 adds)
  * Either may be NULL, not both.  lse is the forward pass's over the same x and w.  dz and dloss x enter the products rounded to 11 bits (fp16 under
- * powers of two, which hold w's bf16 as they are), sums are fp32: dw in fp32 is as near as that.  Elements of dz below 2^-40, and of w and dloss x below 2^-39 of
+ * powers of two, which hold w's bf16 as they are), sums are fp32: dw in fp32 is as near as that, some 2e-4 of its norm.  Elements of dz below 2^-40, and of w and dloss x below 2^-39 of
  * their largest, count as 0.
  * Workspace: fp4_workspace_bytes(FP4_OP_HP_HEAD_BWD, M, D, V, dt); dz takes at most 2^28 fp16 elements and 256 a token of it,
  * twice; w's transposed piece as many. */

@@ -434,7 +434,7 @@ __global__ __launch_bounds__(256) void head_across_kernel(AcrossBoth both) {
   }
 }
 
-// dx's sums for few tokens, w read once as it lies: 256 columns a workgroup, whose four waves share a part of the vocabulary.  A lane loads eight
+// dx's sums for few tokens, w read as it lies, once for up to 64 of them and by two workgroups for more: 256 columns a workgroup, whose four waves share a part of the vocabulary.  A lane loads eight
 // rows of eight columns and turns them in its registers into eight operands, each eight rows of one column (matrix instruction f
 // takes columns 8 n + f), so that nothing passes through LDS.  w stays bf16; dz's 11 bits are the sum of two bf16, a product each: it is w's bytes that bound this
 // (131072 x 4096 for one token 175 us, 6.1 TB/s).
@@ -567,7 +567,10 @@ struct Cut { int tile, splits; };
 // 128 rows 55 / 59 / 85).  More: by rounds of the chip's workgroups, in hundredths of a us (measured): a step of 64 takes a 256 x 256 tile 1.1, 1.25,
 // 1.5 and 1.8 with a quarter, half, three quarters and all of the CUs at work (power) and 1.6 over several rounds, which do not keep step; two
 // 128 x 128 tiles of one CU take 1.05, a single one about 0.63; a tile's start and end
-// 6 and 4.  Splitting the contraction (only where the sums can be added up later: most > 1) brings rounds and takes sums' bytes.
+// 6 and 4.  A round that is full is charged 1.6 also where it is the only one: 128 x 128 tiles then mostly need two and lose against either.  Splitting the
+// contraction (only where the sums can be added up later: most > 1) brings rounds and takes sums' bytes.  dx's gradient calls, by the rule and by the best of both
+// tiles under 1 to 16 splits: 200 x 4096 into 32000 292 / 291 us, 512 x 2048 into 32000 206 / 205, 1055 x 1376 into 50003 418 / 409, 1024 x 4096 into 32000 558 / 557,
+// 2048 x 5120 into 32000 1245 / 1234, 4096 x 4096 into 32000 1735 / 1726; without splits the first four take 605, 493, 857 and 755.
 Cut cut_of(int64_t P, int64_t Q, int64_t K, int most) {
   const int64_t steps = (K + 63) / 64;
   const auto tiles = [&](int64_t bp, int64_t bq) { return ((P + bp - 1) / bp) * ((Q + bq - 1) / bq); };
@@ -576,7 +579,7 @@ Cut cut_of(int64_t P, int64_t Q, int64_t K, int most) {
   Cut best = {TILE_LARGE, 1};
   int64_t least = INT64_MAX;
   for (int s = 1; s <= most; ++s) {
-    const int64_t k = (steps + s - 1) / s, sums = s > 1 ? s * P * Q / 10000 : 0;   // in 1/100 us: 16 bytes a sum at 5 TB/s would be 3.2 a 10000
+    const int64_t k = (steps + s - 1) / s, sums = s > 1 ? s * P * Q / 10000 : 0;   // 5 bytes at 5 TB/s each: they are read again, their stores overlap
     const int64_t nl = tiles(256, 256) * s, nm = tiles(128, 128) * s, rl = nl % 256, rm = nm % 512;
     const int64_t large = nl / 256 * (160 * k + 600) + (rl ? (100 + 75 * rl / 256) * k + 600 : 0) + sums;
     const int64_t middle = nm / 512 * (105 * k + 400) + (rm ? (rm > 256 ? 105 : 63) * k + 400 : 0) + sums;

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormBwd a) {
   const float inv = 1.0f / (float)D;
   const int64_t c0 = (int64_t)threadIdx.x * 8, stride = (int64_t)blockDim.x * 8;
   struct Row { Raw8<T> dy[CH], dh[CH], h[CH], b[CH], g[CH]; float rb, ra; };
-  constexpr bool HOLD = THREADS < 1024;   // of the largest workgroups the registers do not hold them: each use reads them again
+  constexpr bool HOLD = THREADS < 1024;   // beyond 768 threads, 6144 channels, the registers do not hold them: each use reads them again
   Raw8<T> wb[CH], wa[CH], gate[CH];
   float sb[CH][8], sa[CH][8], sg[CH][8];
 #pragma unroll
@@ -277,8 +277,8 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(NormSums a) {
   out[c] = a.accumulate ? out[c] + s : s;
 }
 
-// Threads of a row, a piece of eight channels each or two.  Forward: two where there are rows enough to fill the chip.  Backward: two from
-// 8192 channels on only.
+// Threads of a row, a piece of eight channels each or two.  Forward: two where there are rows enough to fill the chip.  Backward: two
+// beyond 8192 channels only.
 struct RowShape { int threads, pieces; };
 RowShape row_shape(int64_t D, bool two) {
   const int64_t n = (D + 7) / 8;
